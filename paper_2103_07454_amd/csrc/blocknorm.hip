@@ -1,0 +1,521 @@
+// Norms before and after a block with its gate and residual scale, and their backward pass (include/evg_nn.h, evg_blocknorm_*).
+//
+// With the unit rows  ub = (b - mean_b) / s_b  and  ur = (r' - mean_r) / s_r  (RMS: no means),  after = ub * post + post_bias:
+//     r' = alpha r + beta gate after,    n = ur * pre + pre_bias
+// and, with q = dn * pre and p = da * post:
+//     dr = dr' + (q - mean(q) - ur mean(q ur)) / s_r           (RMS: no mean(q))
+//     d_residual = alpha dr,   d_gate = beta dr after summed over the rows that share it,   da = beta gate dr
+//     d_branch = (p - mean(p) - ub mean(p ub)) / s_b           (da itself without post)
+//     d_pre = sum dn ur,  d_pre_bias = sum dn,  d_post = sum da ub,  d_post_bias = sum da     over a worker's rows
+// The backward pass makes both norms anew from residual and branch: nothing has to be kept, and r' is not read in rounded form.
+//
+// Both passes are bound by memory.  A row stays in the registers of 64 to 1024 threads, at most 16 elements of each tensor in a
+// thread, so that each tensor is read once; the sums over a row go through the wavefront and one exchange in LDS.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <exception>
+#include <new>
+
+#include "nn_device.h"
+#include "nn_host.h"
+
+namespace evg {
+namespace {
+
+constexpr uint32_t kStripes = 1024;      // of all workers together, about
+constexpr int kV = 8;                    // elements of a thread that lie together
+
+struct NormArgs {
+  evg_blocknorm_in in;
+  evg_mat out, normed;                   // forward
+  evg_mat d_out, d_normed;               // backward
+  evg_blocknorm_grads d;
+  uint32_t width, workers;
+  float eps, alpha, beta, inv_width;
+  // backward: stripes of rows
+  uint32_t stripes, stripe_rows;         // of a worker
+  uint32_t group_stripes;                // stripes of a gate's group; 0: a stripe has whole groups
+  float* partials;                       // [workers][stripes][5][padded width]: pre, pre_bias, post, post_bias, gate
+  uint32_t padded;
+};
+
+template <typename T>
+__device__ __forceinline__ T* at(const evg_mat& m, uint32_t w, uint64_t row) {
+  return (T*)m.p + (int64_t)w * m.worker + (int64_t)row * m.row;
+}
+
+// The sums of two values over the threads that share a row.  `red` alternates between two sets, so one barrier is enough.
+template <int TPR>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float (*red)[2][TPR / 64], int& turn) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  if constexpr (TPR > 64) {
+    float(&set)[2][TPR / 64] = red[turn];
+    turn ^= 1;
+    const int wave = threadIdx.x % TPR / 64;
+    if (threadIdx.x % 64 == 0) { set[0][wave] = a; set[1][wave] = b; }
+    __syncthreads();
+    a = set[0][0];
+    b = set[1][0];
+#pragma unroll
+    for (int i = 1; i < TPR / 64; ++i) { a += set[0][i]; b += set[1][i]; }
+  }
+}
+
+template <int NV> struct Row { float v[NV * kV]; };
+
+template <int NV, int TPR, typename T>
+__device__ __forceinline__ void load_row(const T* p, int width, int lane, Row<NV>& r) {
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (k * TPR + lane) * kV;
+    load_upto<kV>(p + c, width - c, r.v + k * kV);
+  }
+}
+
+template <int NV, int TPR, typename T>
+__device__ __forceinline__ void store_row(T* p, int width, int lane, const Row<NV>& r) {
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (k * TPR + lane) * kV;
+    store_upto<kV>(p + c, width - c, r.v + k * kV);
+  }
+}
+
+// x becomes its unit row; the elements beyond the width stay 0.  Returns 1 / s.
+template <int NV, int TPR, bool LAYER, typename R>
+__device__ __forceinline__ float make_unit(Row<NV>& x, const NormArgs& g, int lane, R red, int& turn) {
+  if constexpr (LAYER) {
+    float s = 0.f, none = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV * kV; ++i) s += x.v[i];
+    row_sum2<TPR>(s, none, red, turn);
+    const float mean = s * g.inv_width;
+#pragma unroll
+    for (int i = 0; i < NV * kV; ++i) x.v[i] = ((i / kV) * TPR + lane) * kV + i % kV < (int)g.width ? x.v[i] - mean : 0.f;
+  }
+  float s = 0.f, none = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV * kV; ++i) s = fmaf(x.v[i], x.v[i], s);
+  row_sum2<TPR>(s, none, red, turn);
+  const float inv = 1.f / sqrtf(s * g.inv_width + g.eps);
+#pragma unroll
+  for (int i = 0; i < NV * kV; ++i) x.v[i] *= inv;
+  return inv;
+}
+
+// d becomes the gradient of the row whose unit row is u, d that of u on entry.
+template <int NV, int TPR, bool LAYER, typename R>
+__device__ __forceinline__ void unit_gradient(Row<NV>& d, const Row<NV>& u, float inv, const NormArgs& g, R red, int& turn) {
+  float s = 0.f, m = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV * kV; ++i) {
+    s = fmaf(d.v[i], u.v[i], s);
+    if (LAYER) m += d.v[i];
+  }
+  row_sum2<TPR>(s, m, red, turn);
+  s *= g.inv_width;
+  m = LAYER ? m * g.inv_width : 0.f;
+#pragma unroll
+  for (int i = 0; i < NV * kV; ++i) d.v[i] = (d.v[i] - m - u.v[i] * s) * inv;
+}
+
+template <typename T, int NV, int TPR, bool LAYER>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_blocknorm_forward(NormArgs g) {
+  constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;   // rows of a workgroup
+  __shared__ float shared[ROWS][2][2][TPR / 64];
+  int turn = 0;
+  const int lane = threadIdx.x % TPR;
+  float(*red)[2][TPR / 64] = shared[threadIdx.x / TPR];
+  const uint64_t row0 = (uint64_t)blockIdx.x * ROWS + threadIdx.x / TPR, all = (uint64_t)g.workers * g.in.rows;
+  const bool real = row0 < all;
+  const uint64_t row = real ? row0 : all - 1;       // all threads of a workgroup meet at its barriers
+  const uint32_t w = (uint32_t)(row / g.in.rows), t = (uint32_t)(row % g.in.rows);
+  const int width = (int)g.width;
+  Row<NV> r;
+  load_row<NV, TPR>(at<const T>(g.in.residual, w, t), width, lane, r);
+  if (g.in.branch.p) {
+    Row<NV> b, k;
+    load_row<NV, TPR>(at<const T>(g.in.branch, w, t), width, lane, b);
+    if (g.in.post.p) {
+      make_unit<NV, TPR, LAYER>(b, g, lane, red, turn);
+      load_row<NV, TPR>(at<const T>(g.in.post, w, 0), width, lane, k);
+#pragma unroll
+      for (int i = 0; i < NV * kV; ++i) b.v[i] *= k.v[i];
+      if (LAYER && g.in.post_bias.p) {
+        load_row<NV, TPR>(at<const T>(g.in.post_bias, w, 0), width, lane, k);
+#pragma unroll
+        for (int i = 0; i < NV * kV; ++i) b.v[i] += k.v[i];
+      }
+    }
+    if (g.in.gate.p) {
+      load_row<NV, TPR>(at<const T>(g.in.gate, w, t / g.in.gate_rows), width, lane, k);
+#pragma unroll
+      for (int i = 0; i < NV * kV; ++i) b.v[i] *= k.v[i];
+    }
+#pragma unroll
+    for (int i = 0; i < NV * kV; ++i) r.v[i] = fmaf(g.alpha, r.v[i], g.beta * b.v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV * kV; ++i) r.v[i] *= g.alpha;
+  }
+  if (g.out.p && real) store_row<NV, TPR>(at<T>(g.out, w, t), width, lane, r);
+  if (!g.normed.p) return;
+  make_unit<NV, TPR, LAYER>(r, g, lane, red, turn);
+  Row<NV> k;
+  load_row<NV, TPR>(at<const T>(g.in.pre, w, 0), width, lane, k);
+#pragma unroll
+  for (int i = 0; i < NV * kV; ++i) r.v[i] *= k.v[i];
+  if (LAYER && g.in.pre_bias.p) {
+    load_row<NV, TPR>(at<const T>(g.in.pre_bias, w, 0), width, lane, k);
+#pragma unroll
+    for (int i = 0; i < NV * kV; ++i) r.v[i] += k.v[i];
+  }
+  if (real) store_row<NV, TPR>(at<T>(g.normed, w, t), width, lane, r);
+}
+
+// One stripe of a worker's rows: the rows' gradients, and the stripe's share of the weights' and the gate's.
+template <typename T, int NV, int TPR, bool LAYER>
+__global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
+  __shared__ float red[2][2][TPR / 64];
+  int turn = 0;
+  const int lane = threadIdx.x;
+  const uint32_t w = blockIdx.x / g.stripes, stripe = blockIdx.x % g.stripes;
+  const int width = (int)g.width;
+  uint32_t t0, t1;
+  if (g.group_stripes) {
+    const uint32_t group = stripe / g.group_stripes, end = min((uint64_t)g.in.rows, (uint64_t)(group + 1) * g.in.gate_rows);
+    t0 = min(end, group * g.in.gate_rows + stripe % g.group_stripes * g.stripe_rows);
+    t1 = min(end, t0 + g.stripe_rows);
+  } else {
+    t0 = min(g.in.rows, stripe * g.stripe_rows);
+    t1 = min(g.in.rows, t0 + g.stripe_rows);
+  }
+  constexpr int N = NV * kV;
+  Row<NV> s_pre, s_prebias, s_post, s_postbias, s_gate;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s_pre.v[i] = s_prebias.v[i] = s_post.v[i] = s_postbias.v[i] = s_gate.v[i] = 0.f;
+  for (uint32_t t = t0; t < t1; ++t) {
+    Row<NV> r, b, gate, k, d;
+    load_row<NV, TPR>(at<const T>(g.in.residual, w, t), width, lane, r);
+    float inv_b = 1.f, inv_r = 1.f;
+    Row<NV> after;
+    if (g.in.branch.p) {
+      load_row<NV, TPR>(at<const T>(g.in.branch, w, t), width, lane, b);
+      if (g.in.gate.p) load_row<NV, TPR>(at<const T>(g.in.gate, w, t / g.in.gate_rows), width, lane, gate);
+      if (g.in.post.p) {
+        inv_b = make_unit<NV, TPR, LAYER>(b, g, lane, red, turn);
+        load_row<NV, TPR>(at<const T>(g.in.post, w, 0), width, lane, k);
+#pragma unroll
+        for (int i = 0; i < N; ++i) after.v[i] = b.v[i] * k.v[i];
+        if (LAYER && g.in.post_bias.p) {
+          load_row<NV, TPR>(at<const T>(g.in.post_bias, w, 0), width, lane, k);
+#pragma unroll
+          for (int i = 0; i < N; ++i) after.v[i] += k.v[i];
+        }
+      } else {
+        after = b;
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) r.v[i] = fmaf(g.alpha, r.v[i], g.beta * (g.in.gate.p ? gate.v[i] * after.v[i] : after.v[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) r.v[i] *= g.alpha;
+    }
+    if (g.d_normed.p) {
+      inv_r = make_unit<NV, TPR, LAYER>(r, g, lane, red, turn);
+      load_row<NV, TPR>(at<const T>(g.d_normed, w, t), width, lane, d);
+      load_row<NV, TPR>(at<const T>(g.in.pre, w, 0), width, lane, k);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s_pre.v[i] = fmaf(d.v[i], r.v[i], s_pre.v[i]);
+        if (LAYER) s_prebias.v[i] += d.v[i];
+        d.v[i] *= k.v[i];
+      }
+      unit_gradient<NV, TPR, LAYER>(d, r, inv_r, g, red, turn);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) d.v[i] = 0.f;
+    }
+    if (g.d_out.p) {
+      load_row<NV, TPR>(at<const T>(g.d_out, w, t), width, lane, k);
+#pragma unroll
+      for (int i = 0; i < N; ++i) d.v[i] += k.v[i];
+    }
+    if (g.d.residual.p) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) k.v[i] = g.alpha * d.v[i];
+      store_row<NV, TPR>(at<T>(g.d.residual, w, t), width, lane, k);
+    }
+    if (!g.in.branch.p) continue;
+    if (g.in.gate.p) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s_gate.v[i] = fmaf(g.beta * d.v[i], after.v[i], s_gate.v[i]);
+      const bool ends = !g.group_stripes && (t + 1 == g.in.rows || (t + 1) % g.in.gate_rows == 0);
+      if (ends) {
+        if (g.d.gate.p) store_row<NV, TPR>(at<T>(g.d.gate, w, t / g.in.gate_rows), width, lane, s_gate);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s_gate.v[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) d.v[i] = g.beta * d.v[i] * gate.v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) d.v[i] *= g.beta;
+    }
+    if (g.in.post.p) {
+      load_row<NV, TPR>(at<const T>(g.in.post, w, 0), width, lane, k);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s_post.v[i] = fmaf(d.v[i], b.v[i], s_post.v[i]);
+        if (LAYER) s_postbias.v[i] += d.v[i];
+        d.v[i] *= k.v[i];
+      }
+      unit_gradient<NV, TPR, LAYER>(d, b, inv_b, g, red, turn);
+    }
+    if (g.d.branch.p) store_row<NV, TPR>(at<T>(g.d.branch, w, t), width, lane, d);
+  }
+  float* p = g.partials + ((uint64_t)w * g.stripes + stripe) * 5 * g.padded;
+  const int padded = (int)g.padded;
+  if (g.d.pre.p) store_row<NV, TPR>(p, padded, lane, s_pre);
+  if (LAYER && g.d.pre_bias.p) store_row<NV, TPR>(p + padded, padded, lane, s_prebias);
+  if (g.d.post.p) store_row<NV, TPR>(p + 2 * padded, padded, lane, s_post);
+  if (LAYER && g.d.post_bias.p) store_row<NV, TPR>(p + 3 * padded, padded, lane, s_postbias);
+  if (g.d.gate.p && g.group_stripes) store_row<NV, TPR>(p + 4 * padded, padded, lane, s_gate);
+}
+
+// Adds the stripes' shares, in their order: 64 columns to a workgroup, each of its wavefronts has every 16th stripe.
+constexpr int kJoinWaves = 16;
+template <typename T>
+__global__ __launch_bounds__(kJoinWaves * 64) void k_blocknorm_join(NormArgs g, uint32_t groups) {
+  __shared__ float part[kJoinWaves][64];
+  const uint32_t blocks = (g.width + 63) / 64, cell = blockIdx.x / blocks;   // cells: worker x (four weights, then the gate's groups)
+  const uint32_t w = cell / (4 + groups), which = cell % (4 + groups);
+  const evg_mat& out = which == 0 ? g.d.pre : which == 1 ? g.d.pre_bias : which == 2 ? g.d.post : which == 3 ? g.d.post_bias : g.d.gate;
+  if (!out.p) return;
+  const uint32_t s0 = which < 4 ? 0 : (which - 4) * g.group_stripes, s1 = which < 4 ? g.stripes : s0 + g.group_stripes;
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x % blocks * 64 + lane;
+  float sum = 0.f;
+  if (c < g.padded) {
+    const float* p = g.partials + ((uint64_t)w * g.stripes * 5 + min(which, 4u)) * g.padded + c;
+#pragma unroll 4
+    for (uint32_t s = s0 + wave; s < s1; s += kJoinWaves) sum += p[(uint64_t)s * 5 * g.padded];
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave || c >= g.width) return;
+#pragma unroll
+  for (int i = 1; i < kJoinWaves; ++i) sum += part[i][lane];
+  at<T>(out, w, which < 4 ? 0 : which - 4)[c] = from_f<T>(sum);
+}
+
+template <typename T, int NV, int TPR, bool LAYER>
+hipError_t launch_sized(const NormArgs& g, bool backward, hipStream_t s) {
+  if (!backward) {
+    constexpr int rows = TPR < 256 ? 256 / TPR : 1;
+    const uint64_t all = (uint64_t)g.workers * g.in.rows;
+    k_blocknorm_forward<T, NV, TPR, LAYER><<<(uint32_t)((all + rows - 1) / rows), TPR * rows, 0, s>>>(g);
+  } else if (g.stripes) {
+    k_blocknorm_backward<T, NV, TPR, LAYER><<<g.workers * g.stripes, TPR, 0, s>>>(g);
+  }
+  return hipGetLastError();
+}
+
+template <typename T, bool LAYER>
+hipError_t launch_kind(const NormArgs& g, bool backward, hipStream_t s) {
+  if (g.width <= 512) return launch_sized<T, 1, 64, LAYER>(g, backward, s);
+  if (g.width <= 1024) return launch_sized<T, 2, 64, LAYER>(g, backward, s);
+  if (g.width <= 2048) return launch_sized<T, 2, 128, LAYER>(g, backward, s);
+  if (g.width <= 4096) return launch_sized<T, 2, 256, LAYER>(g, backward, s);
+  if (g.width <= 8192) return launch_sized<T, 2, 512, LAYER>(g, backward, s);
+  return launch_sized<T, 2, 1024, LAYER>(g, backward, s);
+}
+
+template <typename T>
+hipError_t launch_blocknorm(const NormArgs& g, uint32_t kind, bool backward, hipStream_t s) {
+  hipError_t e = kind == EVG_NORM_LAYER ? launch_kind<T, true>(g, backward, s) : launch_kind<T, false>(g, backward, s);
+  if (e != hipSuccess || !backward) return e;
+  const uint32_t groups = g.d.gate.p && g.group_stripes ? g.stripes / g.group_stripes : 0;
+  if (!g.d.pre.p && !g.d.pre_bias.p && !g.d.post.p && !g.d.post_bias.p && !groups) return hipSuccess;
+  k_blocknorm_join<T><<<(g.width + 63) / 64 * g.workers * (4 + groups), kJoinWaves * 64, 0, s>>>(g, groups);
+  return hipGetLastError();
+}
+
+hipError_t launch_typed(const NormArgs& g, uint32_t type, uint32_t kind, bool backward, hipStream_t s) {
+  if (type == EVG_F32) return launch_blocknorm<float>(g, kind, backward, s);
+  if (type == EVG_F16) return launch_blocknorm<half_t>(g, kind, backward, s);
+  return launch_blocknorm<bf16_t>(g, kind, backward, s);
+}
+
+}  // namespace
+}  // namespace evg
+
+using namespace evg;
+
+struct evg_blocknorm {
+  evg_blocknorm_config cfg{};
+  hipStream_t stream = nullptr;
+  float* partials = nullptr;
+  uint64_t max_stripes = 0;   // of a worker
+  uint32_t padded = 0;
+};
+
+namespace {
+
+// Rows of a stripe such that all workers together have about kStripes of them.
+uint32_t stripe_rows(uint32_t workers, uint32_t rows) {
+  const uint64_t r = ((uint64_t)workers * rows + kStripes - 1) / kStripes;
+  return (uint32_t)(r < 1 ? 1 : r > rows ? (rows ? rows : 1) : r);
+}
+
+evg_status check_norm_in(const evg_blocknorm* c, const evg_blocknorm_in* in) {
+  const evg_blocknorm_config& f = c->cfg;
+  const uint32_t W = f.workers, D = f.width, ty = f.type;
+  if (in->rows > f.max_rows) return fail(EVG_ERR_INVALID, "rows exceeds the context's max_rows");
+  if (!in->branch.p && (in->gate.p || in->post.p || in->post_bias.p)) return fail(EVG_ERR_INVALID, "without a branch there is no gate and no norm after it");
+  if (in->gate.p && !in->gate_rows) return fail(EVG_ERR_INVALID, "gate_rows must be at least 1");
+  if ((in->post_bias.p && !in->post.p) || (in->pre_bias.p && !in->pre.p)) return fail(EVG_ERR_INVALID, "a bias needs its norm's weight");
+  if (f.kind == EVG_NORM_RMS && (in->post_bias.p || in->pre_bias.p)) return fail(EVG_ERR_INVALID, "RMS norms have no bias");
+  evg_status st;
+  if ((st = check_mat(&in->residual, W, in->rows, D, ty, false, "residual")) != EVG_OK) return st;
+  if (in->branch.p && (st = check_mat(&in->branch, W, in->rows, D, ty, false, "branch")) != EVG_OK) return st;
+  if (in->gate.p && (st = check_mat(&in->gate, W, ((uint64_t)in->rows + in->gate_rows - 1) / in->gate_rows, D, ty, false, "gate")) != EVG_OK) return st;
+  const struct { const evg_mat* m; const char* what; } vectors[] = {{&in->post, "post"}, {&in->post_bias, "post_bias"}, {&in->pre, "pre"}, {&in->pre_bias, "pre_bias"}};
+  for (const auto& v : vectors)
+    if (v.m->p && (st = check_mat(v.m, W, 1, D, ty, false, v.what)) != EVG_OK) return st;
+  return EVG_OK;
+}
+
+NormArgs norm_args(const evg_blocknorm* c, const evg_blocknorm_in* in) {
+  NormArgs g{};
+  g.in = *in;
+  g.width = c->cfg.width;
+  g.workers = c->cfg.workers;
+  g.eps = c->cfg.eps;
+  g.alpha = c->cfg.residual_scale;
+  g.beta = c->cfg.branch_scale;
+  g.inv_width = (float)(1.0 / c->cfg.width);
+  g.partials = c->partials;
+  g.padded = c->padded;
+  return g;
+}
+
+}  // namespace
+
+extern "C" {
+
+evg_status evg_blocknorm_init(evg_blocknorm** out, const evg_blocknorm_config* cfg, void* hip_stream) {
+  if (!out || !cfg) return fail(EVG_ERR_INVALID, "out and cfg must be non-NULL");
+  *out = nullptr;
+  if (cfg->workers < 1 || cfg->width < 1 || cfg->width > EVG_BLOCKNORM_MAX_WIDTH)
+    return fail(EVG_ERR_INVALID, "workers must be at least 1, width 1 .. %u", EVG_BLOCKNORM_MAX_WIDTH);
+  if ((uint64_t)cfg->workers * cfg->max_rows > 0x7FFFFFFFull || (uint64_t)cfg->workers * cfg->width > 0x7FFFFFFFull)
+    return fail(EVG_ERR_INVALID, "workers, max_rows: more than 2^31 rows or weights");
+  evg_status st;
+  if ((st = check_type(cfg->type, "type")) != EVG_OK) return st;
+  if (cfg->kind > EVG_NORM_LAYER) return fail(EVG_ERR_INVALID, "kind must be EVG_NORM_RMS or EVG_NORM_LAYER");
+  if (!(cfg->eps >= 0.f) || std::isinf(cfg->eps)) return fail(EVG_ERR_INVALID, "eps must be finite and not negative");
+  if (!std::isfinite(cfg->residual_scale) || !std::isfinite(cfg->branch_scale)) return fail(EVG_ERR_INVALID, "the scales must be finite");
+  evg_blocknorm* c = new (std::nothrow) evg_blocknorm();
+  if (!c) return fail(EVG_ERR_OOM, "host allocation failed");
+  c->cfg = *cfg;
+  c->stream = static_cast<hipStream_t>(hip_stream);
+  c->padded = (cfg->width + 63) / 64 * 64;
+  // Stripes of whole gate groups are at least half as long as those asked for, and a group's last one may be short (backward).
+  const uint64_t per = (kStripes + cfg->workers - 1) / cfg->workers;
+  c->max_stripes = 3 * (per < cfg->max_rows ? per : cfg->max_rows) + 2;
+  const hipError_t e = hipMalloc((void**)&c->partials, cfg->workers * c->max_stripes * 5 * c->padded * sizeof(float));
+  if (e != hipSuccess) {
+    delete c;
+    return fail(e == hipErrorOutOfMemory ? EVG_ERR_OOM : EVG_ERR_HIP, "workspace: %s", hipGetErrorString(e));
+  }
+  *out = c;
+  return EVG_OK;
+}
+
+evg_status evg_blocknorm_forward(evg_blocknorm* c, const evg_blocknorm_in* in, const evg_mat* residual_out, const evg_mat* normed) {
+  if (!c || !in) return fail(EVG_ERR_INVALID, "context and in must be non-NULL");
+  evg_status st = check_norm_in(c, in);
+  if (st != EVG_OK) return st;
+  const uint32_t W = c->cfg.workers, D = c->cfg.width, ty = c->cfg.type;
+  const bool has_out = residual_out && residual_out->p, has_normed = normed && normed->p;
+  if (has_normed != (in->pre.p != nullptr)) return fail(EVG_ERR_INVALID, "normed is given exactly if pre is");
+  if (!has_out && !has_normed) return fail(EVG_ERR_INVALID, "there is nothing to compute");
+  if (has_out && (st = check_mat(residual_out, W, in->rows, D, ty, true, "residual_out")) != EVG_OK) return st;
+  if (has_normed && (st = check_mat(normed, W, in->rows, D, ty, true, "normed")) != EVG_OK) return st;
+  const uint64_t gates = in->gate.p ? ((uint64_t)in->rows + in->gate_rows - 1) / in->gate_rows : 0;
+  const Span outs[] = {mat_span(residual_out, W, in->rows, D, ty, "residual_out"), mat_span(normed, W, in->rows, D, ty, "normed")};
+  const Span ins[] = {mat_span(&in->residual, W, in->rows, D, ty, "residual"), mat_span(&in->branch, W, in->rows, D, ty, "branch"),
+                      mat_span(&in->gate, W, gates, D, ty, "gate"), mat_span(&in->post, W, 1, D, ty, "post"),
+                      mat_span(&in->post_bias, W, 1, D, ty, "post_bias"), mat_span(&in->pre, W, 1, D, ty, "pre"),
+                      mat_span(&in->pre_bias, W, 1, D, ty, "pre_bias")};
+  if ((st = check_apart(outs, 2, ins, 7, 0, 0)) != EVG_OK) return st;
+  if (!in->rows) return EVG_OK;
+  NormArgs g = norm_args(c, in);
+  if (has_out) g.out = *residual_out;
+  if (has_normed) g.normed = *normed;
+  HIP_TRY(launch_typed(g, ty, c->cfg.kind, false, c->stream));
+  return EVG_OK;
+}
+
+evg_status evg_blocknorm_backward(evg_blocknorm* c, const evg_blocknorm_in* in, const evg_mat* d_residual, const evg_mat* d_normed,
+                                  const evg_blocknorm_grads* out) {
+  if (!c || !in || !out) return fail(EVG_ERR_INVALID, "context, in and out must be non-NULL");
+  evg_status st = check_norm_in(c, in);
+  if (st != EVG_OK) return st;
+  const uint32_t W = c->cfg.workers, D = c->cfg.width, ty = c->cfg.type;
+  const bool has_res = d_residual && d_residual->p, has_normed = d_normed && d_normed->p;
+  if (has_normed && !in->pre.p) return fail(EVG_ERR_INVALID, "d_normed is given without pre");
+  if (has_res && (st = check_mat(d_residual, W, in->rows, D, ty, false, "d_residual")) != EVG_OK) return st;
+  if (has_normed && (st = check_mat(d_normed, W, in->rows, D, ty, false, "d_normed")) != EVG_OK) return st;
+  const uint64_t gates = in->gate.p ? ((uint64_t)in->rows + in->gate_rows - 1) / in->gate_rows : 0;
+  const struct { const evg_mat *m, *of; uint64_t rows; const char* what; } grads[] = {
+      {&out->residual, &in->residual, in->rows, "the gradient of residual"}, {&out->branch, &in->branch, in->rows, "the gradient of branch"},
+      {&out->gate, &in->gate, gates, "the gradient of gate"}, {&out->post, &in->post, 1, "the gradient of post"},
+      {&out->post_bias, &in->post_bias, 1, "the gradient of post_bias"}, {&out->pre, &in->pre, 1, "the gradient of pre"},
+      {&out->pre_bias, &in->pre_bias, 1, "the gradient of pre_bias"}};
+  Span outs[7], ins[9];
+  int n = 0;
+  for (int i = 0; i < 7; ++i) {
+    ins[i] = mat_span(grads[i].of, W, grads[i].rows, D, ty, "an input");
+    if (!grads[i].m->p) continue;
+    if (!grads[i].of->p) return fail(EVG_ERR_INVALID, "%s is asked for, which is absent", grads[i].what);
+    if ((st = check_mat(grads[i].m, W, grads[i].rows, D, ty, true, grads[i].what)) != EVG_OK) return st;
+    outs[n++] = mat_span(grads[i].m, W, grads[i].rows, D, ty, grads[i].what);
+  }
+  ins[7] = mat_span(has_res ? d_residual : nullptr, W, in->rows, D, ty, "d_residual");
+  ins[8] = mat_span(has_normed ? d_normed : nullptr, W, in->rows, D, ty, "d_normed");
+  if ((st = check_apart(outs, n, ins, 9, out->residual.p ? 0 : -1, 7)) != EVG_OK) return st;
+  NormArgs g = norm_args(c, in);
+  if (has_res) g.d_out = *d_residual;
+  if (has_normed) g.d_normed = *d_normed;
+  g.d = *out;
+  if (in->rows) {
+    g.stripe_rows = stripe_rows(W, in->rows);
+    g.stripes = (in->rows + g.stripe_rows - 1) / g.stripe_rows;
+    if (out->gate.p && in->gate_rows <= g.stripe_rows) {
+      g.stripe_rows = g.stripe_rows / in->gate_rows * in->gate_rows;
+      g.stripes = (in->rows + g.stripe_rows - 1) / g.stripe_rows;
+    } else if (out->gate.p) {
+      const uint32_t group = in->gate_rows < in->rows ? in->gate_rows : in->rows;
+      g.group_stripes = (group + g.stripe_rows - 1) / g.stripe_rows;
+      g.stripe_rows = (group + g.group_stripes - 1) / g.group_stripes;
+      g.stripes = (uint32_t)gates * g.group_stripes;
+    }
+    if (g.stripes > c->max_stripes) return fail(EVG_ERR_STATE, "%u stripes of rows, room for %llu", g.stripes, (unsigned long long)c->max_stripes);
+  }
+  HIP_TRY(launch_typed(g, ty, c->cfg.kind, true, c->stream));
+  return EVG_OK;
+}
+
+evg_status evg_blocknorm_destroy(evg_blocknorm* c) {
+  if (!c) return EVG_OK;
+  hipError_t e = hipStreamSynchronize(c->stream);
+  if (c->partials) { const hipError_t f = hipFree(c->partials); if (e == hipSuccess) e = f; }
+  delete c;
+  HIP_TRY(e);
+  return EVG_OK;
+}
+
+}  // extern "C"

@@ -14,15 +14,16 @@
 #include <vector>
 
 #include "../../include/evg.h"
+#include "evg_host.h"
 #include "evg_internal.h"
 
 using namespace evg;
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-evg_status fail(evg_status s, const char* fmt, ...) {
+evg_status evg::fail(evg_status s, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -32,13 +33,7 @@ evg_status fail(evg_status s, const char* fmt, ...) {
   return s;
 }
 
-#define HIP_TRY(expr)                                                                   \
-  do {                                                                                  \
-    hipError_t e_ = (expr);                                                             \
-    if (e_ != hipSuccess)                                                               \
-      return fail(e_ == hipErrorOutOfMemory ? EVG_ERR_OOM : EVG_ERR_HIP, "%s: %s", #expr, \
-                  hipGetErrorString(e_));                                               \
-  } while (0)
+namespace {
 
 inline uint64_t pad_to(uint64_t v, uint64_t m) { return (v + m - 1) / m * m; }
 
@@ -193,11 +188,13 @@ evg_status check_layers(uint32_t L, const uint64_t* layer_numel) {
 
 bool finite_f(float v) { return std::isfinite(v); }
 
+}  // namespace
+
 // A kernel that is handed host memory, or an array shorter than the sizes say, faults
 // the GPU; so ask the runtime what `p` is.  The range test sees the whole allocation
 // `p` lies in (a sub-allocator's pool block counts as one), so it catches what runs
 // past that; where the runtime cannot name the range the test is skipped.
-evg_status check_device_array(const void* p, uint64_t bytes, const char* what) {
+evg_status evg::check_device_array(const void* p, uint64_t bytes, const char* what) {
   hipPointerAttribute_t at;
   hipError_t e = hipPointerGetAttributes(&at, p);
   if (e != hipSuccess || (at.type != hipMemoryTypeDevice && at.type != hipMemoryTypeManaged)) {
@@ -220,8 +217,6 @@ evg_status check_device_array(const void* p, uint64_t bytes, const char* what) {
                 (unsigned long long)bytes, (unsigned long long)(end - (uintptr_t)p));
   return EVG_OK;
 }
-
-}  // namespace
 
 extern "C" {
 

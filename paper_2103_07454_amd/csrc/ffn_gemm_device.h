@@ -1,0 +1,328 @@
+// The feed-forward block's matrix products on the matrix cores: one kernel for all types, orders of the operands and epilogues.
+//
+// C[m][n] = sum_k A(m, k) B(n, k).  An operand is K-contiguous (rows of k) or M/N-contiguous (rows of m or n).  A workgroup has a
+// tile of BM x BN; each step of 128 bytes of k (64 elements of 16 bits, 32 of 32) is staged through one of two buffers in LDS, while
+// the matrix cores work on the other.  A wavefront has WM x 64 of the tile in accumulators of 32 x 32.
+//
+// The operands of the matrix instruction are swapped (B's fragment first), so that a lane holds four neighbouring n of one m, which
+// leave as one store.
+//
+// LDS, in units of 16 bytes.  K-contiguous: row m has 8 units, unit c at m * 8 + (c ^ (m & 7)): the 8 lanes that read one unit each
+// of 8 neighbouring rows meet 8 different groups of banks.  M/N-contiguous: row k has BM / E units (E elements to a unit).  16-bit
+// fragments come by transposing reads: 16 lanes read 4 rows of 32 bytes and each gets 4 k of one m.  A read touches 16 rows k; units
+// are permuted in pairs by ((k & 3) | (k >> 3 & 1) << 2), so that 8 of them meet all banks.  32-bit fragments are read element by
+// element; rows that differ in bit 2 of k go to different halves of the banks.
+#pragma once
+#include <type_traits>
+
+#include "ffn_internal.h"
+#include "nn_device.h"
+#include "../../include/evg_nn.h"
+
+namespace evg {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> struct Frag { u32x4 v; };   // 16 bytes of k of one m or n
+
+__device__ __forceinline__ f32x16 mfma(const Frag<half_t>& a, const Frag<half_t>& b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a.v), __builtin_bit_cast(f16x8, b.v), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.v), __builtin_bit_cast(bf16x8, b.v), c, 0, 0, 0);
+}
+// The instruction takes 2 k, one from each half of the wavefront; four of them take the 8 that the fragments hold.
+__device__ __forceinline__ f32x16 mfma(const Frag<float>& a, const Frag<float>& b, f32x16 c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.v[i]), __uint_as_float(b.v[i]), c, 0, 0, 0);
+  return c;
+}
+
+// Activations and their slopes.  exp(-x) overflows to infinity for x below -88, and x / (1 + inf) is the limit, -0.
+__device__ __forceinline__ void activate(uint32_t kind, float x, float& a, float& slope) {
+  if (kind == EVG_ACT_SILU) {
+    const float s = 1.f / (1.f + expf(-x));
+    a = x * s;
+    slope = s * fmaf(x, 1.f - s, 1.f);
+  } else if (kind == EVG_ACT_GELU) {
+    const float cdf = 0.5f * erfcf(-0.70710678118654752f * x);
+    a = x * cdf;
+    slope = fmaf(x, 0.39894228040143268f * expf(-0.5f * x * x), cdf);
+  } else if (kind == EVG_ACT_GELU_TANH) {
+    // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
+    const float z2 = 1.5957691216057308f * fmaf(0.044715f * x, x * x, x), dz2 = 1.5957691216057308f * fmaf(0.134145f * x, x, 1.f);
+    const float s = 1.f / (1.f + expf(-z2));
+    a = x * s;
+    slope = s * fmaf(x * dz2, 1.f - s, 1.f);
+  } else {
+    a = x > 0.f ? x : (x != x ? x : 0.f);
+    slope = x > 0.f ? 1.f : (x != x ? x : 0.f);
+  }
+}
+
+constexpr uint32_t kOut = 0x80000000u;   // a byte offset beyond every buffer: such loads give 0
+
+template <typename T, int BD, bool KC>   // one operand's tile: BD rows or columns of the product, K-contiguous or not
+struct Tile {
+  static constexpr int E = 16 / sizeof(T), BK = 128 / sizeof(T);
+  static constexpr int kUnits = BD * 8;
+  static constexpr int kPerRow = KC ? 8 : BD / E;   // units of a row in LDS
+  // The unit that lies at a place, as (row, unit of the row).
+  static __device__ __forceinline__ int swizzle(int row) {
+    if constexpr (KC) return row & 7;
+    else if constexpr (sizeof(T) == 4) return (row >> 2 & 1) << 3;
+    else if constexpr (BD >= 128) return ((row & 3) | (row >> 3 & 1) << 2) << 1;
+    else return ((row >> 1 & 1) | (row >> 3 & 1) << 1) << 1;
+  }
+};
+
+// Fragment `ks` (0 .. 3: 32 bytes of k) of the 32 rows from d0 on.
+template <typename T, int BD, bool KC>
+__device__ __forceinline__ Frag<T> read_frag(const u32x4* s, int d0, int ks, int lane) {
+  using L = Tile<T, BD, KC>;
+  Frag<T> f;
+  if constexpr (KC) {
+    const int row = d0 + (lane & 31);
+    f.v = s[row * 8 + ((ks * 2 + (lane >> 5)) ^ (row & 7))];
+  } else if constexpr (sizeof(T) == 2) {
+    const int q = lane >> 4, i = lane & 15;
+    const int k = ks * 16 + (q >> 1) * 8 + (i >> 2);
+    const int unit = (d0 >> 3) + (q & 1) * 2 + ((i & 3) >> 1);
+    const char* p = (const char*)(s + k * L::kPerRow + (unit ^ L::swizzle(k))) + (i & 1) * 8;
+    const char* p2 = (const char*)(s + (k + 4) * L::kPerRow + (unit ^ L::swizzle(k + 4))) + (i & 1) * 8;
+    using P = __attribute__((address_space(3))) s16x4*;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p2);
+    struct { s16x4 a, b; } both{lo, hi};
+    f.v = __builtin_bit_cast(u32x4, both);
+  } else {
+    const int d = d0 + (lane & 31);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int k = (ks * 2 + (lane >> 5)) * 4 + j;
+      f.v[j] = ((const uint32_t*)(s + k * L::kPerRow + ((d >> 2) ^ L::swizzle(k))))[d & 3];
+    }
+  }
+  return f;
+}
+
+template <typename T, int OP, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
+__global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void k_ffn_gemm(GemmArgs g) {
+  constexpr bool AKC = OP != GEMM_WEIGHT, BKC = OP == GEMM_GATED || OP == GEMM_DOWN;
+  constexpr int WAVES = WAVES_M * WAVES_N, WM = BM / WAVES_M, TM = WM / 32;
+  static_assert(BN / WAVES_N == 64 && WM % 32 == 0, "a wavefront has 64 columns");
+  using LA = Tile<T, BM, AKC>;
+  using LB = Tile<T, BN, BKC>;
+  constexpr int E = LA::E, BK = LA::BK;
+  constexpr int NA = BM / 8 / WAVES, NB = BN / 8 / WAVES;   // wavefront loads of 64 units for each step
+  __shared__ u32x4 lds0[LA::kUnits + LB::kUnits], lds1[LA::kUnits + LB::kUnits];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Tiles in an order in which neighbours share operands: eight rows of tiles, column by column.  Workgroups go to the eight XCDs in
+  // turn; each gets a contiguous part of the order, so that what it shares lies in its own L2.
+  const uint32_t tiles = g.tiles_m * g.tiles_n;
+  uint32_t id = blockIdx.x;
+  {
+    const uint32_t all = gridDim.x, x = id & 7, each = all >> 3, more = all & 7;
+    id = x * each + min(x, more) + (id >> 3);
+  }
+  const uint32_t cell = id / tiles, part = cell % g.parts, w = cell / g.parts;
+  id %= tiles;
+  const uint32_t band = 8 * g.tiles_n, first = id / band * 8, rows = min(8u, g.tiles_m - first);
+  const uint32_t tm = first + id % band % rows, tn = id % band / rows;
+  const uint32_t m0 = tm * BM, n0 = tn * (OP == GEMM_GATED ? BN / 2 : BN);
+
+  // Each operand's first byte in memory that this tile reads, and its loads' rows and units.
+  const uint32_t phases = OP == GEMM_INPUT ? 2 : 1;
+  const uint32_t steps1 = (g.K + BK - 1) / BK, steps = steps1 * phases;
+  const int b_which = OP == GEMM_GATED ? wave & 1 : 0;   // 32 rows of gate's and 32 of up's in turn: of each wavefront's loads, and of each one's 64 columns
+
+  u32x4 held_a[ALIGNED ? 1 : NA], held_b[ALIGNED ? 1 : NB];
+
+  auto one = [&](auto layout, const GemmOperand& o, uint32_t lead, uint32_t dim, int j, uint32_t kt, u32x4* lds, u32x4* held, bool gated_rows) {
+    using L = decltype(layout);
+    constexpr bool KC = L::kPerRow == 8 && std::is_same_v<L, Tile<T, L::kUnits / 8, true>>;
+    const uint32_t k0 = kt * BK;
+    const int load = wave * (L::kUnits / 64 / WAVES) + j, place = load * 64 + lane;
+    const int row = place / L::kPerRow, unit = (place % L::kPerRow) ^ L::swizzle(row);
+    uint32_t d, k;    // first element of the unit
+    if constexpr (KC) { d = gated_rows ? (row >> 6) * 32 + (row & 31) : row; k = unit * E; }
+    else { d = unit * E; k = row; }
+    const bool ok = d + lead < dim && k + k0 < g.K;
+    const T* base = (const T*)o.p + (int64_t)w * o.worker + (KC ? (int64_t)lead * o.ld + k0 : (int64_t)k0 * o.ld + lead);
+    if constexpr (ALIGNED) {
+      // To the end of the last row.  Rows are whole units: the caller's by the rule for this variant, the library's own by their padding.
+      const uint64_t left = (KC ? (uint64_t)(dim - 1 - lead) * o.ld + ((g.K + E - 1) / E * E - k0) : (uint64_t)(g.K - 1 - k0) * o.ld + ((dim + E - 1) / E * E - lead)) * sizeof(T);
+      const uint32_t bytes = (uint32_t)min(left, (uint64_t)0x7FFFFFF0u);
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+      const uint32_t off = ok ? (KC ? d * (uint32_t)o.ld + k : k * (uint32_t)o.ld + d) * (uint32_t)sizeof(T) : kOut;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + load * 64), 16, (int)off, 0, 0, 0);
+    } else {
+      u32x4 v = {0, 0, 0, 0};
+      if (ok) {
+        const T* p = base + (KC ? (int64_t)d * o.ld + k : (int64_t)k * o.ld + d);
+        const uint32_t n = KC ? g.K - k0 - k : dim - lead - d;
+        if (n >= E) {
+          __builtin_memcpy(&v, __builtin_assume_aligned(p, sizeof(T)), 16);
+        } else {
+          T e[E];
+#pragma unroll
+          for (int i = 0; i < E; ++i) e[i] = i < (int)n ? p[i] : (T)0.f;
+          __builtin_memcpy(&v, e, 16);
+        }
+      }
+      held[j] = v;
+    }
+  };
+  auto fetch = [&](uint32_t step, u32x4* lds) {
+    const uint32_t phase = step >= steps1, kt = step - phase * steps1;
+    const GemmOperand& a = g.a[OP == GEMM_WEIGHT ? part : phase];
+    const GemmOperand& b = g.b[OP == GEMM_GATED ? b_which : OP == GEMM_WEIGHT ? 0 : phase];
+#pragma unroll
+    for (int j = 0; j < NA; ++j) one(LA{}, a, m0, g.M, j, kt, lds, held_a, false);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) one(LB{}, b, n0, g.N, j, kt, lds + LA::kUnits, held_b, OP == GEMM_GATED);
+  };
+  auto put = [&](u32x4* lds) {
+    if constexpr (!ALIGNED) {
+#pragma unroll
+      for (int j = 0; j < NA; ++j) lds[(wave * NA + j) * 64 + lane] = held_a[j];
+#pragma unroll
+      for (int j = 0; j < NB; ++j) lds[LA::kUnits + (wave * NB + j) * 64 + lane] = held_b[j];
+    }
+  };
+
+  f32x16 acc[TM][2];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  const int wm = wave / WAVES_N * WM, wn = wave % WAVES_N * 64;
+  auto multiply = [&](const u32x4* lds) {
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      Frag<T> a[TM], b[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) b[j] = read_frag<T, BN, BKC>(lds + LA::kUnits, wn + j * 32, ks, lane);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) a[i] = read_frag<T, BM, AKC>(lds, wm + i * 32, ks, lane);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = mfma(b[j], a[i], acc[i][j]);
+    }
+  };
+
+  if (steps) {   // none: the product is 0
+    fetch(0, lds0);
+    put(lds0);
+    __syncthreads();
+  }
+  for (uint32_t step = 0; step < steps; step += 2) {
+    if (step + 1 < steps) fetch(step + 1, lds1);
+    multiply(lds0);
+    if (step + 1 >= steps) break;
+    put(lds1);
+    __syncthreads();
+    if (step + 2 < steps) fetch(step + 2, lds0);
+    multiply(lds1);
+    if (step + 2 < steps) put(lds0);
+    __syncthreads();
+  }
+
+  // A lane has, of its row m, four times four neighbouring columns of each accumulator.
+  const GemmOperand& co = g.c[OP == GEMM_WEIGHT ? part : 0];
+  T* const c = (T*)co.p + (int64_t)w * co.worker;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const uint32_t m = m0 + wm + i * 32 + (lane & 31);
+    if (m >= g.M) continue;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (OP == GEMM_GATED) {
+        const uint32_t n = n0 + (wn >> 1) + 8 * q + 4 * (lane >> 5);
+        if (n >= g.pitch) continue;
+        float gate[4], up[4], h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool real = n + e < g.N;     // the columns up to `pitch` are 0
+          gate[e] = real ? acc[i][0][q * 4 + e] : 0.f;
+          up[e] = real ? acc[i][1][q * 4 + e] : 0.f;
+          float a, slope;
+          activate(g.activation, gate[e], a, slope);
+          h[e] = real ? a * up[e] : 0.f;
+        }
+        store_n<4>(c + (int64_t)m * co.ld + n, h);
+        if (g.proj) {
+          float* p = g.proj + w * g.proj_worker + (uint64_t)m * 2 * g.pitch + n;
+          *(f32x4*)p = f32x4{gate[0], gate[1], gate[2], gate[3]};
+          *(f32x4*)(p + g.pitch) = f32x4{up[0], up[1], up[2], up[3]};
+        }
+      } else if constexpr (OP == GEMM_GATED_BWD) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t n = n0 + wn + j * 32 + 8 * q + 4 * (lane >> 5);
+          if (n >= g.pitch) continue;
+          const float* p = g.proj + w * g.proj_worker + (uint64_t)m * 2 * g.pitch + n;
+          const f32x4 gate = *(const f32x4*)p, up = *(const f32x4*)(p + g.pitch);
+          float dg[4], du[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float a, slope;
+            activate(g.activation, gate[e], a, slope);
+            const bool real = n + e < g.N;
+            dg[e] = real ? acc[i][j][q * 4 + e] * up[e] * slope : 0.f;
+            du[e] = real ? acc[i][j][q * 4 + e] * a : 0.f;
+          }
+          store_n<4>(c + (int64_t)m * co.ld + n, dg);
+          store_n<4>(c + (int64_t)m * co.ld + g.pitch + n, du);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t n = n0 + wn + j * 32 + 8 * q + 4 * (lane >> 5);
+          if (n >= g.N) continue;
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = acc[i][j][q * 4 + e];
+          store_upto<4>(c + (int64_t)m * co.ld + n, (int)(g.N - n), v);
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int OP>
+hipError_t launch_op(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) {
+  constexpr uint32_t share = OP == GEMM_GATED ? 2 : 1;   // a tile's columns are gate's and up's
+  const uint32_t bm = tile == TILE_256 ? 256 : tile == TILE_128 ? 128 : 64, bn = (tile == TILE_256 ? 256 : 128) / share;
+  g.tiles_m = (g.M + bm - 1) / bm;
+  // padding columns are written too where there are any
+  const uint32_t n = OP == GEMM_GATED || OP == GEMM_GATED_BWD ? g.pitch : g.N;
+  g.tiles_n = (n + bn - 1) / bn;
+  const uint64_t grid = (uint64_t)g.tiles_m * g.tiles_n * g.workers * g.parts;
+  if (!grid) return hipSuccess;
+  if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  if (aligned) {
+    if constexpr (sizeof(T) == 2) {
+      if (tile == TILE_256) { k_ffn_gemm<T, OP, 256, 256, 2, 4, true><<<(uint32_t)grid, 512, 0, s>>>(g); return hipGetLastError(); }
+    }
+    if (tile == TILE_128) k_ffn_gemm<T, OP, 128, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
+    else k_ffn_gemm<T, OP, 64, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
+  } else {
+    if (tile == TILE_128) k_ffn_gemm<T, OP, 128, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
+    else k_ffn_gemm<T, OP, 64, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace evg

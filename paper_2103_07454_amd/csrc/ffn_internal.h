@@ -1,0 +1,39 @@
+// Launch descriptions of the feed-forward block's matrix products.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace evg {
+
+enum GemmOp : uint32_t {
+  GEMM_GATED = 0,     // h = act(A Bg^T) * (A Bu^T), both K-contiguous; writes h and, for a backward pass, both projections
+  GEMM_DOWN = 1,      // C = A B^T, both K-contiguous
+  GEMM_GATED_BWD = 2, // dh = A B, B N-contiguous; writes the gradients of both projections
+  GEMM_INPUT = 3,     // C = A0 B0 + A1 B1, B N-contiguous
+  GEMM_WEIGHT = 4,    // C = A^T B, A M-contiguous, B N-contiguous; two of them at once
+  GEMM_OPS = 5
+};
+
+struct GemmOperand {
+  const void* p;      // null: this part is left out
+  int64_t worker, ld; // elements between workers and between rows of what lies in memory
+};
+
+// C (M x N) from products over K; for each of `workers` and `parts`.
+struct GemmArgs {
+  GemmOperand a[2], b[2], c[2];   // phases of the product (GEMM_INPUT), gate and up (GEMM_GATED), or parts (GEMM_WEIGHT)
+  uint32_t M, N, K, workers, parts;
+  uint32_t tiles_m, tiles_n;
+  uint32_t activation;
+  // GEMM_GATED, GEMM_GATED_BWD: the projections in 32 bits, row t: gate's at 0, up's at `pitch`, and the gradients in the same places of c[0]
+  float* proj;
+  uint64_t proj_worker;
+  uint32_t pitch;                  // padded hidden width
+};
+
+// Tile shapes.
+enum GemmTile : uint32_t { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2 };
+
+template <typename T> hipError_t launch_gemm(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g, hipStream_t s);
+
+}  // namespace evg

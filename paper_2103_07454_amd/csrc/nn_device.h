@@ -1,0 +1,63 @@
+// Loads, stores and sums that the operators' kernels share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace evg {
+
+typedef _Float16 half_t;
+typedef __bf16 bf16_t;
+
+template <typename T> __device__ __forceinline__ float to_f(T v) { return (float)v; }
+// Rounds to the nearest, ties to even.
+template <typename T> __device__ __forceinline__ T from_f(float v) { return (T)v; }
+
+// N consecutive elements at any alignment that their type allows: global accesses of 16 bytes need none on gfx950.
+template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Pack { T v[N]; };
+
+template <int N, typename T>
+__device__ __forceinline__ void load_n(const T* p, float* v) {
+  const Pack<T, N> r = *reinterpret_cast<const Pack<T, N>*>(p);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = to_f(r.v[i]);
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void store_n(T* p, const float* v) {
+  Pack<T, N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.v[i] = from_f<T>(v[i]);
+  *reinterpret_cast<Pack<T, N>*>(p) = r;
+}
+
+// The first n of N elements (n may be <= 0 or >= N); the others are 0.
+template <int N, typename T>
+__device__ __forceinline__ void load_upto(const T* p, int n, float* v) {
+  if (n >= N) {
+    load_n<N>(p, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = i < n ? to_f(p[i]) : 0.f;
+  }
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void store_upto(T* p, int n, const float* v) {
+  if (n >= N) {
+    store_n<N>(p, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = from_f<T>(v[i]);
+  }
+}
+
+// The sum over a wavefront, in every lane; the order is fixed.
+template <typename F>
+__device__ __forceinline__ F wave_sum(F v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
+  return v;
+}
+
+}  // namespace evg
