@@ -48,7 +48,9 @@ GemmTile choose_tile(const GemmArgs& g, uint32_t n, uint32_t share, bool aligned
 
 hipError_t product(const evg_ffn* c, GemmOp op, bool aligned, GemmArgs& g) {
   g.workers = c->cfg.workers;
-  g.activation = c->cfg.activation;
+  const bool tanh_form = c->cfg.activation == EVG_ACT_GELU_TANH;   // 2 sqrt(2 / pi) (x + 0.044715 x^3)
+  g.activation = {tanh_form ? 1.5957691216057308f : 1.f, tanh_form ? 1.5957691216057308f * 0.044715f : 0.f, c->cfg.activation == EVG_ACT_RELU,
+                  c->cfg.activation == EVG_ACT_GELU};
   g.pitch = c->pitch;
   const bool padded = op == GEMM_GATED || op == GEMM_GATED_BWD;
   const GemmTile tile = choose_tile(g, padded ? g.pitch : g.N, op == GEMM_GATED ? 2 : 1, aligned, c->cfg.type);

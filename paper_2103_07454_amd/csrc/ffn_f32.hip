@@ -1,18 +1,11 @@
-// The feed-forward block's matrix products, float.
+// The feed-forward block's matrix products, 32 bits.
 #include "ffn_gemm_device.h"
 
 namespace evg {
 
 template <>
 hipError_t launch_gemm<float>(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g, hipStream_t s) {
-  switch (op) {
-    case GEMM_GATED: return launch_op<float, GEMM_GATED>(tile, aligned, g, s);
-    case GEMM_DOWN: return launch_op<float, GEMM_DOWN>(tile, aligned, g, s);
-    case GEMM_GATED_BWD: return launch_op<float, GEMM_GATED_BWD>(tile, aligned, g, s);
-    case GEMM_INPUT: return launch_op<float, GEMM_INPUT>(tile, aligned, g, s);
-    case GEMM_WEIGHT: return launch_op<float, GEMM_WEIGHT>(tile, aligned, g, s);
-    default: return hipErrorInvalidValue;
-  }
+  return launch_any<float>(op, tile, aligned, g, s);
 }
 
 }  // namespace evg

@@ -2,7 +2,7 @@
 //
 // C[m][n] = sum_k A(m, k) B(n, k).  An operand is K-contiguous (rows of k) or M/N-contiguous (rows of m or n).  A workgroup has a
 // tile of BM x BN; each step of 128 bytes of k (64 elements of 16 bits, 32 of 32) is staged through one of two buffers in LDS, while
-// the matrix cores work on the other.  A wavefront has WM x 64 of the tile in accumulators of 32 x 32.
+// the matrix cores work on the other.  A wavefront has WM x WN of the tile in accumulators of 32 x 32.
 //
 // The operands of the matrix instruction are swapped (B's fragment first), so that a lane holds four neighbouring n of one m, which
 // leave as one store.
@@ -44,25 +44,26 @@ __device__ __forceinline__ f32x16 mfma(const Frag<float>& a, const Frag<float>& 
   return c;
 }
 
-// Activations and their slopes.  exp(-x) overflows to infinity for x below -88, and x / (1 + inf) is the limit, -0.
-__device__ __forceinline__ void activate(uint32_t kind, float x, float& a, float& slope) {
-  if (kind == EVG_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-x));
-    a = x * s;
-    slope = s * fmaf(x, 1.f - s, 1.f);
-  } else if (kind == EVG_ACT_GELU) {
+// An activation a = x s(x) and its slope s + x s'(x).  SiLU and the tanh form of GELU are logistic functions of z = x (c0 + c1 x^2),
+// 0.5 (1 + tanh y) = 1 / (1 + exp(-2 y)), and ReLU is the step; GELU itself (ERF) has kernels of its own, as the error function is
+// long.  For 16-bit tensors exp and the quotient are the hardware's, a few units of 2^-23 off where s is not vanishing.
+template <bool ERF, bool FAST>
+__device__ __forceinline__ void activate(const Activation& f, float x, float& a, float& slope) {
+  if constexpr (ERF) {
     const float cdf = 0.5f * erfcf(-0.70710678118654752f * x);
     a = x * cdf;
-    slope = fmaf(x, 0.39894228040143268f * expf(-0.5f * x * x), cdf);
-  } else if (kind == EVG_ACT_GELU_TANH) {
-    // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
-    const float z2 = 1.5957691216057308f * fmaf(0.044715f * x, x * x, x), dz2 = 1.5957691216057308f * fmaf(0.134145f * x, x, 1.f);
-    const float s = 1.f / (1.f + expf(-z2));
-    a = x * s;
-    slope = s * fmaf(x * dz2, 1.f - s, 1.f);
+    slope = fmaf(x, 0.39894228040143268f * (FAST ? __expf(-0.5f * x * x) : expf(-0.5f * x * x)), cdf);
   } else {
-    a = x > 0.f ? x : (x != x ? x : 0.f);
-    slope = x > 0.f ? 1.f : (x != x ? x : 0.f);
+    const float z = x * fmaf(f.c1 * x, x, f.c0), dz = fmaf(3.f * f.c1 * x, x, f.c0);
+    const float e = 1.f + (FAST ? __expf(-z) : expf(-z));   // infinite for z below -88: s is 0 then
+    const float s = FAST ? __builtin_amdgcn_rcpf(e) : 1.f / e;
+    const float t = s * (1.f - s);
+    a = x * s;
+    slope = t > 0.f ? fmaf(x * dz, t, s) : s;               // far out x dz may be infinite
+    if (f.relu) {
+      a = x > 0.f ? x : x <= 0.f ? 0.f : x;
+      slope = x > 0.f ? 1.f : x <= 0.f ? 0.f : x;
+    }
   }
 }
 
@@ -82,23 +83,23 @@ struct Tile {
   }
 };
 
-// Fragment `ks` (0 .. 3: 32 bytes of k) of the 32 rows from d0 on.
+// Fragment `ks` (0 .. 3: 32 bytes of k) of the 32 rows from d0 on, of a tile `from` units into a buffer.  Addresses are one offset from
+// the buffer: the compiler follows them no further when it looks for loads into LDS that a read has to wait for.
 template <typename T, int BD, bool KC>
-__device__ __forceinline__ Frag<T> read_frag(const u32x4* s, int d0, int ks, int lane) {
+__device__ __forceinline__ Frag<T> read_frag(const u32x4* s, int from, int d0, int ks, int lane) {
   using L = Tile<T, BD, KC>;
   Frag<T> f;
   if constexpr (KC) {
     const int row = d0 + (lane & 31);
-    f.v = s[row * 8 + ((ks * 2 + (lane >> 5)) ^ (row & 7))];
+    f.v = s[from + row * 8 + ((ks * 2 + (lane >> 5)) ^ (row & 7))];
   } else if constexpr (sizeof(T) == 2) {
     const int q = lane >> 4, i = lane & 15;
     const int k = ks * 16 + (q >> 1) * 8 + (i >> 2);
     const int unit = (d0 >> 3) + (q & 1) * 2 + ((i & 3) >> 1);
-    const char* p = (const char*)(s + k * L::kPerRow + (unit ^ L::swizzle(k))) + (i & 1) * 8;
-    const char* p2 = (const char*)(s + (k + 4) * L::kPerRow + (unit ^ L::swizzle(k + 4))) + (i & 1) * 8;
+    const int byte = (from + k * L::kPerRow + (unit ^ L::swizzle(k))) * 16 + (i & 1) * 8;
     using P = __attribute__((address_space(3))) s16x4*;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p2);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)((const char*)s + byte));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)((const char*)s + (byte + 4 * L::kPerRow * 16)));   // 4 rows on, which are permuted alike
     struct { s16x4 a, b; } both{lo, hi};
     f.v = __builtin_bit_cast(u32x4, both);
   } else {
@@ -106,21 +107,100 @@ __device__ __forceinline__ Frag<T> read_frag(const u32x4* s, int d0, int ks, int
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int k = (ks * 2 + (lane >> 5)) * 4 + j;
-      f.v[j] = ((const uint32_t*)(s + k * L::kPerRow + ((d >> 2) ^ L::swizzle(k))))[d & 3];
+      f.v[j] = ((const uint32_t*)s)[(from + k * L::kPerRow + ((d >> 2) ^ L::swizzle(k))) * 4 + (d & 3)];
     }
   }
   return f;
 }
 
-template <typename T, int OP, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
+// One operand's way into LDS: what a thread loads of each step's tile, 16 bytes at a time.
+template <typename T, int BD, bool KC, int WAVES, bool ALIGNED, bool PAIRED>
+struct Loader {
+  using L = Tile<T, BD, KC>;
+  static constexpr int E = L::E, BK = L::BK, N = L::kUnits / 64 / WAVES;   // loads of a wavefront in a step
+  static constexpr int kApart = KC ? 8 : 64 / L::kPerRow;                  // rows between them
+  const char* base;      // the tile's first element at the next step
+  uint64_t left;         // bytes from there to the operand's last row's end
+  uint64_t stride;       // bytes from step to step
+  uint32_t off[N];       // of this lane's units
+  uint32_t k;            // of its first unit, within a step
+  uint32_t ld, d, room;  // elements between rows; the first unit's row or column of the tile, and how many the product has from the tile on
+
+  // PAIRED: rows of the tile are 32 of one matrix and 32 of another in turn, and this wavefront's are all of one.
+  __device__ __forceinline__ void start(const GemmOperand& o, uint32_t w, uint32_t lead, uint32_t dim, uint32_t K, int wave, int lane) {
+    ld = (uint32_t)o.ld;
+    base = (const char*)((const T*)o.p + (int64_t)w * o.worker + (KC ? (int64_t)lead * o.ld : (int64_t)lead));
+    // Rows are whole units where they are loaded as such: the caller's by the rule for that variant, the library's own by their padding.
+    const uint64_t last = KC ? (uint64_t)(dim - 1 - lead) * o.ld + (K + E - 1) / E * E : (uint64_t)(K - 1) * o.ld + ((dim + E - 1) / E * E - lead);
+    left = last * sizeof(T);
+    stride = (KC ? (uint64_t)BK : (uint64_t)BK * o.ld) * sizeof(T);
+    room = dim - lead;
+    const int place = wave * N * 64 + lane, row = place / L::kPerRow, unit = (place % L::kPerRow) ^ L::swizzle(row);
+    if constexpr (KC) { d = PAIRED ? (row >> 6) * 32 + (row & 31) : row; k = unit * E; }
+    else { d = unit * E; k = row; }
+    if constexpr (ALIGNED) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if constexpr (KC) {
+          off[j] = ((d + j * kApart) * ld + k) * (uint32_t)sizeof(T);         // rows beyond the last one lie beyond `left`
+        } else {
+          const int r = row + j * kApart, c = (place % L::kPerRow ^ L::swizzle(r)) * E;
+          off[j] = (uint32_t)c < room ? (r * ld + c) * (uint32_t)sizeof(T) : kOut;   // and so do rows k
+        }
+      }
+    }
+  }
+
+  // The step whose first k is K - k_left; zeros where that is none.
+  __device__ __forceinline__ void fetch(int k_left, u32x4* lds, u32x4* held, int wave, int lane) {
+    if constexpr (ALIGNED) {
+      const uint32_t bytes = (uint32_t)min(left, (uint64_t)0x7FFFFFF0u);
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
+      const uint32_t none = KC && (int)k >= k_left ? kOut : 0;   // rows k beyond the last one lie beyond `left`
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (wave * N + j) * 64), 16, (int)(off[j] | none), 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int place = (wave * N + j) * 64 + lane, row = place / L::kPerRow, unit = (place % L::kPerRow) ^ L::swizzle(row);
+        const uint32_t dj = KC ? d + j * kApart : unit * E, kj = KC ? k : row;
+        u32x4 v = {0, 0, 0, 0};
+        if (dj < room && (int)kj < k_left) {
+          const T* p = (const T*)base + (KC ? (int64_t)dj * ld + kj : (int64_t)kj * ld + dj);
+          const uint32_t n = KC ? k_left - kj : room - dj;
+          if (n >= E) {
+            __builtin_memcpy(&v, __builtin_assume_aligned(p, sizeof(T)), 16);
+          } else {
+            T e[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) e[i] = i < (int)n ? p[i] : (T)0.f;
+            __builtin_memcpy(&v, e, 16);
+          }
+        }
+        held[j] = v;
+      }
+    }
+    base += stride;
+    left -= min(left, stride);
+  }
+
+  __device__ __forceinline__ void put(u32x4* lds, const u32x4* held, int wave, int lane) const {
+    if constexpr (!ALIGNED) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) lds[(wave * N + j) * 64 + lane] = held[j];
+    }
+  }
+};
+
+template <typename T, int OP, bool ERF, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
 __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void k_ffn_gemm(GemmArgs g) {
   constexpr bool AKC = OP != GEMM_WEIGHT, BKC = OP == GEMM_GATED || OP == GEMM_DOWN;
-  constexpr int WAVES = WAVES_M * WAVES_N, WM = BM / WAVES_M, TM = WM / 32;
-  static_assert(BN / WAVES_N == 64 && WM % 32 == 0, "a wavefront has 64 columns");
+  constexpr int WAVES = WAVES_M * WAVES_N, WM = BM / WAVES_M, TM = WM / 32, WN = BN / WAVES_N, TN = WN / 32;
+  static_assert(WN % 64 == 0 && WM % 32 == 0, "a wavefront has pairs of accumulators side by side");
   using LA = Tile<T, BM, AKC>;
   using LB = Tile<T, BN, BKC>;
-  constexpr int E = LA::E, BK = LA::BK;
-  constexpr int NA = BM / 8 / WAVES, NB = BN / 8 / WAVES;   // wavefront loads of 64 units for each step
+  constexpr int BK = LA::BK;
   __shared__ u32x4 lds0[LA::kUnits + LB::kUnits], lds1[LA::kUnits + LB::kUnits];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -138,104 +218,74 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void k_ffn_gemm(GemmArgs g) 
   const uint32_t tm = first + id % band % rows, tn = id % band / rows;
   const uint32_t m0 = tm * BM, n0 = tn * (OP == GEMM_GATED ? BN / 2 : BN);
 
-  // Each operand's first byte in memory that this tile reads, and its loads' rows and units.
-  const uint32_t phases = OP == GEMM_INPUT ? 2 : 1;
-  const uint32_t steps1 = (g.K + BK - 1) / BK, steps = steps1 * phases;
-  const int b_which = OP == GEMM_GATED ? wave & 1 : 0;   // 32 rows of gate's and 32 of up's in turn: of each wavefront's loads, and of each one's 64 columns
-
-  u32x4 held_a[ALIGNED ? 1 : NA], held_b[ALIGNED ? 1 : NB];
-
-  auto one = [&](auto layout, const GemmOperand& o, uint32_t lead, uint32_t dim, int j, uint32_t kt, u32x4* lds, u32x4* held, bool gated_rows) {
-    using L = decltype(layout);
-    constexpr bool KC = L::kPerRow == 8 && std::is_same_v<L, Tile<T, L::kUnits / 8, true>>;
-    const uint32_t k0 = kt * BK;
-    const int load = wave * (L::kUnits / 64 / WAVES) + j, place = load * 64 + lane;
-    const int row = place / L::kPerRow, unit = (place % L::kPerRow) ^ L::swizzle(row);
-    uint32_t d, k;    // first element of the unit
-    if constexpr (KC) { d = gated_rows ? (row >> 6) * 32 + (row & 31) : row; k = unit * E; }
-    else { d = unit * E; k = row; }
-    const bool ok = d + lead < dim && k + k0 < g.K;
-    const T* base = (const T*)o.p + (int64_t)w * o.worker + (KC ? (int64_t)lead * o.ld + k0 : (int64_t)k0 * o.ld + lead);
-    if constexpr (ALIGNED) {
-      // To the end of the last row.  Rows are whole units: the caller's by the rule for this variant, the library's own by their padding.
-      const uint64_t left = (KC ? (uint64_t)(dim - 1 - lead) * o.ld + ((g.K + E - 1) / E * E - k0) : (uint64_t)(g.K - 1 - k0) * o.ld + ((dim + E - 1) / E * E - lead)) * sizeof(T);
-      const uint32_t bytes = (uint32_t)min(left, (uint64_t)0x7FFFFFF0u);
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
-      const uint32_t off = ok ? (KC ? d * (uint32_t)o.ld + k : k * (uint32_t)o.ld + d) * (uint32_t)sizeof(T) : kOut;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + load * 64), 16, (int)off, 0, 0, 0);
-    } else {
-      u32x4 v = {0, 0, 0, 0};
-      if (ok) {
-        const T* p = base + (KC ? (int64_t)d * o.ld + k : (int64_t)k * o.ld + d);
-        const uint32_t n = KC ? g.K - k0 - k : dim - lead - d;
-        if (n >= E) {
-          __builtin_memcpy(&v, __builtin_assume_aligned(p, sizeof(T)), 16);
-        } else {
-          T e[E];
-#pragma unroll
-          for (int i = 0; i < E; ++i) e[i] = i < (int)n ? p[i] : (T)0.f;
-          __builtin_memcpy(&v, e, 16);
-        }
-      }
-      held[j] = v;
+  Loader<T, BM, AKC, WAVES, ALIGNED, false> la;
+  Loader<T, BN, BKC, WAVES, ALIGNED, OP == GEMM_GATED> lb;
+  static_assert(OP != GEMM_GATED || decltype(lb)::N * 8 == 32, "a wavefront loads rows of one matrix only");
+  u32x4 held_a[ALIGNED ? 1 : decltype(la)::N], held_b[ALIGNED ? 1 : decltype(lb)::N];
+  const uint32_t steps1 = (g.K + BK - 1) / BK, steps = steps1 * (OP == GEMM_INPUT ? 2 : 1);
+  uint32_t fetched = 0;
+  int k_left = (int)g.K;
+  auto fetch = [&](u32x4* lds) {
+    if (OP == GEMM_INPUT && fetched == steps1) {   // the second of the two products
+      la.start(g.a[1], w, m0, g.M, g.K, wave, lane);
+      lb.start(g.b[1], w, n0, g.N, g.K, wave, lane);
+      k_left = (int)g.K;
     }
-  };
-  auto fetch = [&](uint32_t step, u32x4* lds) {
-    const uint32_t phase = step >= steps1, kt = step - phase * steps1;
-    const GemmOperand& a = g.a[OP == GEMM_WEIGHT ? part : phase];
-    const GemmOperand& b = g.b[OP == GEMM_GATED ? b_which : OP == GEMM_WEIGHT ? 0 : phase];
-#pragma unroll
-    for (int j = 0; j < NA; ++j) one(LA{}, a, m0, g.M, j, kt, lds, held_a, false);
-#pragma unroll
-    for (int j = 0; j < NB; ++j) one(LB{}, b, n0, g.N, j, kt, lds + LA::kUnits, held_b, OP == GEMM_GATED);
+    la.fetch(k_left, lds, held_a, wave, lane);
+    lb.fetch(k_left, lds + LA::kUnits, held_b, wave, lane);
+    k_left -= BK;
+    ++fetched;
   };
   auto put = [&](u32x4* lds) {
-    if constexpr (!ALIGNED) {
-#pragma unroll
-      for (int j = 0; j < NA; ++j) lds[(wave * NA + j) * 64 + lane] = held_a[j];
-#pragma unroll
-      for (int j = 0; j < NB; ++j) lds[LA::kUnits + (wave * NB + j) * 64 + lane] = held_b[j];
-    }
+    la.put(lds, held_a, wave, lane);
+    lb.put(lds + LA::kUnits, held_b, wave, lane);
   };
 
-  f32x16 acc[TM][2];
+  f32x16 acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  const int wm = wave / WAVES_N * WM, wn = wave % WAVES_N * 64;
+  const int wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
   auto multiply = [&](const u32x4* lds) {
+    Frag<T> a[2][TM], b[2][TN];
+    auto read = [&](int ks, int set) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) b[set][j] = read_frag<T, BN, BKC>(lds, LA::kUnits, wn + j * 32, ks, lane);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) a[set][i] = read_frag<T, BM, AKC>(lds, 0, wm + i * 32, ks, lane);
+    };
+    read(0, 0);
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
-      Frag<T> a[TM], b[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) b[j] = read_frag<T, BN, BKC>(lds + LA::kUnits, wn + j * 32, ks, lane);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) a[i] = read_frag<T, BM, AKC>(lds, wm + i * 32, ks, lane);
+      if (ks < 3) read(ks + 1, (ks + 1) & 1);
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = mfma(b[j], a[i], acc[i][j]);
+        for (int j = 0; j < TN; ++j) acc[i][j] = mfma(b[ks & 1][j], a[ks & 1][i], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
   if (steps) {   // none: the product is 0
-    fetch(0, lds0);
+    la.start(g.a[OP == GEMM_WEIGHT ? part : 0], w, m0, g.M, g.K, wave, lane);
+    lb.start(g.b[OP == GEMM_GATED ? wave & 1 : 0], w, n0, g.N, g.K, wave, lane);
+    fetch(lds0);
     put(lds0);
     __syncthreads();
   }
-  for (uint32_t step = 0; step < steps; step += 2) {
-    if (step + 1 < steps) fetch(step + 1, lds1);
+  for (uint32_t step = 0; step < steps; step += 2) {   // an odd last step is followed by one of zeros
+    fetch(lds1);
     multiply(lds0);
-    if (step + 1 >= steps) break;
     put(lds1);
     __syncthreads();
-    if (step + 2 < steps) fetch(step + 2, lds0);
+    const bool more = step + 2 < steps;
+    if (more) fetch(lds0);
     multiply(lds1);
-    if (step + 2 < steps) put(lds0);
+    if (more) put(lds0);
     __syncthreads();
   }
 
@@ -249,27 +299,30 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void k_ffn_gemm(GemmArgs g) 
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if constexpr (OP == GEMM_GATED) {
-        const uint32_t n = n0 + (wn >> 1) + 8 * q + 4 * (lane >> 5);
-        if (n >= g.pitch) continue;
-        float gate[4], up[4], h[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool real = n + e < g.N;     // the columns up to `pitch` are 0
-          gate[e] = real ? acc[i][0][q * 4 + e] : 0.f;
-          up[e] = real ? acc[i][1][q * 4 + e] : 0.f;
-          float a, slope;
-          activate(g.activation, gate[e], a, slope);
-          h[e] = real ? a * up[e] : 0.f;
-        }
-        store_n<4>(c + (int64_t)m * co.ld + n, h);
-        if (g.proj) {
-          float* p = g.proj + w * g.proj_worker + (uint64_t)m * 2 * g.pitch + n;
-          *(f32x4*)p = f32x4{gate[0], gate[1], gate[2], gate[3]};
-          *(f32x4*)(p + g.pitch) = f32x4{up[0], up[1], up[2], up[3]};
+        for (int j = 0; j < TN; j += 2) {
+          const uint32_t n = n0 + (wn >> 1) + j * 16 + 8 * q + 4 * (lane >> 5);
+          if (n >= g.pitch) continue;
+          float gate[4], up[4], h[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const bool real = n + e < g.N;     // the columns up to `pitch` are 0
+            gate[e] = real ? acc[i][j][q * 4 + e] : 0.f;
+            up[e] = real ? acc[i][j + 1][q * 4 + e] : 0.f;
+            float a, slope;
+            activate<ERF, sizeof(T) == 2>(g.activation, gate[e], a, slope);
+            h[e] = real ? a * up[e] : 0.f;
+          }
+          store_n<4>(c + (int64_t)m * co.ld + n, h);
+          if (g.proj) {
+            float* p = g.proj + w * g.proj_worker + (uint64_t)m * 2 * g.pitch + n;
+            *(f32x4*)p = f32x4{gate[0], gate[1], gate[2], gate[3]};
+            *(f32x4*)(p + g.pitch) = f32x4{up[0], up[1], up[2], up[3]};
+          }
         }
       } else if constexpr (OP == GEMM_GATED_BWD) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < TN; ++j) {
           const uint32_t n = n0 + wn + j * 32 + 8 * q + 4 * (lane >> 5);
           if (n >= g.pitch) continue;
           const float* p = g.proj + w * g.proj_worker + (uint64_t)m * 2 * g.pitch + n;
@@ -278,7 +331,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void k_ffn_gemm(GemmArgs g) 
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float a, slope;
-            activate(g.activation, gate[e], a, slope);
+            activate<ERF, sizeof(T) == 2>(g.activation, gate[e], a, slope);
             const bool real = n + e < g.N;
             dg[e] = real ? acc[i][j][q * 4 + e] * up[e] * slope : 0.f;
             du[e] = real ? acc[i][j][q * 4 + e] * a : 0.f;
@@ -288,7 +341,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void k_ffn_gemm(GemmArgs g) 
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < TN; ++j) {
           const uint32_t n = n0 + wn + j * 32 + 8 * q + 4 * (lane >> 5);
           if (n >= g.N) continue;
           float v[4];
@@ -301,7 +354,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void k_ffn_gemm(GemmArgs g) 
   }
 }
 
-template <typename T, int OP>
+template <typename T, int OP, bool ERF>
 hipError_t launch_op(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) {
   constexpr uint32_t share = OP == GEMM_GATED ? 2 : 1;   // a tile's columns are gate's and up's
   const uint32_t bm = tile == TILE_256 ? 256 : tile == TILE_128 ? 128 : 64, bn = (tile == TILE_256 ? 256 : 128) / share;
@@ -314,15 +367,28 @@ hipError_t launch_op(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) {
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
   if (aligned) {
     if constexpr (sizeof(T) == 2) {
-      if (tile == TILE_256) { k_ffn_gemm<T, OP, 256, 256, 2, 4, true><<<(uint32_t)grid, 512, 0, s>>>(g); return hipGetLastError(); }
+      if (tile == TILE_256) { k_ffn_gemm<T, OP, ERF, 256, 256, 2, 4, true><<<(uint32_t)grid, 512, 0, s>>>(g); return hipGetLastError(); }
     }
-    if (tile == TILE_128) k_ffn_gemm<T, OP, 128, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
-    else k_ffn_gemm<T, OP, 64, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
+    if (tile == TILE_128) k_ffn_gemm<T, OP, ERF, 128, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
+    else k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
   } else {
-    if (tile == TILE_128) k_ffn_gemm<T, OP, 128, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
-    else k_ffn_gemm<T, OP, 64, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
+    if (tile == TILE_128) k_ffn_gemm<T, OP, ERF, 128, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
+    else k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
   }
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_any(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g, hipStream_t s) {
+  const bool erf = g.activation.erf;
+  switch (op) {
+    case GEMM_GATED: return erf ? launch_op<T, GEMM_GATED, true>(tile, aligned, g, s) : launch_op<T, GEMM_GATED, false>(tile, aligned, g, s);
+    case GEMM_GATED_BWD: return erf ? launch_op<T, GEMM_GATED_BWD, true>(tile, aligned, g, s) : launch_op<T, GEMM_GATED_BWD, false>(tile, aligned, g, s);
+    case GEMM_DOWN: return launch_op<T, GEMM_DOWN, false>(tile, aligned, g, s);
+    case GEMM_INPUT: return launch_op<T, GEMM_INPUT, false>(tile, aligned, g, s);
+    case GEMM_WEIGHT: return launch_op<T, GEMM_WEIGHT, false>(tile, aligned, g, s);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace evg

@@ -14,6 +14,12 @@ enum GemmOp : uint32_t {
   GEMM_OPS = 5
 };
 
+// a = x s(x): s the logistic function of x (c0 + c1 x^2), the step, or (erf) the normal distribution.
+struct Activation {
+  float c0, c1;
+  uint32_t relu, erf;
+};
+
 struct GemmOperand {
   const void* p;      // null: this part is left out
   int64_t worker, ld; // elements between workers and between rows of what lies in memory
@@ -24,7 +30,7 @@ struct GemmArgs {
   GemmOperand a[2], b[2], c[2];   // phases of the product (GEMM_INPUT), gate and up (GEMM_GATED), or parts (GEMM_WEIGHT)
   uint32_t M, N, K, workers, parts;
   uint32_t tiles_m, tiles_n;
-  uint32_t activation;
+  Activation activation;
   // GEMM_GATED, GEMM_GATED_BWD: the projections in 32 bits, row t: gate's at 0, up's at `pitch`, and the gradients in the same places of c[0]
   float* proj;
   uint64_t proj_worker;
