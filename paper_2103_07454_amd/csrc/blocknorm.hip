@@ -65,12 +65,27 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float (*red)[2][TPR
 
 template <int NV> struct Row { float v[NV * kV]; };
 
+// Elements beyond the width are 0.  Every lane loads, those that have no whole 8 elements from the row's start, so that no branch
+// stands between one tensor's loads and the next one's; only a width that is no multiple of 8 has a lane read some elements singly.
 template <int NV, int TPR, typename T>
 __device__ __forceinline__ void load_row(const T* p, int width, int lane, Row<NV>& r) {
+  if (width >= kV) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int c = (k * TPR + lane) * kV;
-    load_upto<kV>(p + c, width - c, r.v + k * kV);
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * TPR + lane) * kV;
+      const bool whole = c + kV <= width;
+      load_n<kV>(p + (whole ? c : 0), r.v + k * kV);
+#pragma unroll
+      for (int i = 0; i < kV; ++i) r.v[k * kV + i] = whole ? r.v[k * kV + i] : 0.f;
+    }
+  }
+  if (width % kV) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * TPR + lane) * kV;
+      if (c < width && c + kV > width) load_upto<kV>(p + c, width - c, r.v + k * kV);
+      else if (width < kV) load_upto<kV>(p, 0, r.v + k * kV);
+    }
   }
 }
 

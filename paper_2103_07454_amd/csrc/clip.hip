@@ -16,6 +16,8 @@ namespace evg {
 namespace {
 
 constexpr int kClipThreads = 256;
+// Up to so many sums, each workgroup that writes adds up its worker's for itself (a load or two for each thread); more are added by a launch between.
+constexpr uint32_t kOwnSums = 512;
 
 // A run of elements of a worker's slice without padding in it.
 struct ClipChunk { uint32_t off, len; };   // off: a multiple of 4
@@ -25,8 +27,7 @@ struct ClipTables {
   uint32_t nchunks, P;
   uint64_t pitch;        // elements of a worker's slice
   double* partials;      // [P][nchunks]
-  uint32_t* arrived;     // [P], 0 between launches
-  float* factor;         // [P]
+  float* factor;         // [P], where a launch of its own finds them
 };
 
 struct ClipCall {
@@ -35,65 +36,90 @@ struct ClipCall {
   float* norm;           // [P] or null
 };
 
-// One workgroup sums the squares of a chunk; a worker's last one to arrive adds the chunks' sums, in their order, and leaves the factor.
+// The sum of a workgroup's values, in every thread; the order is fixed.
+__device__ __forceinline__ double group_sum(double v, double* part) {
+  v = wave_sum(v);
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
+  __syncthreads();
+  v = part[0];
+#pragma unroll
+  for (int i = 1; i < kClipThreads / 64; ++i) v += part[i];
+  return v;
+}
+
+// One workgroup sums the squares of a chunk.  Squares of 32 bits are exact in 64.
 template <typename T>
-__global__ __launch_bounds__(kClipThreads) void k_clip_norm(ClipTables t, ClipCall call, const T* __restrict__ grad) {
-  constexpr int E = 16 / sizeof(T);
+__global__ __launch_bounds__(kClipThreads) void k_clip_squares(ClipTables t, const T* __restrict__ grad) {
+  constexpr int E = 16 / sizeof(T), U = 8;
   __shared__ double part[kClipThreads / 64];
-  __shared__ bool last;
   const uint32_t r = blockIdx.x / t.nchunks, c = blockIdx.x % t.nchunks;
   const ClipChunk d = t.chunks[c];
   const T* g = grad + (uint64_t)r * t.pitch + d.off;
-  double sum = 0.0;
-#pragma unroll 4
-  for (uint32_t j = threadIdx.x * E; j < d.len; j += kClipThreads * E) {
+  double sum[2] = {0.0, 0.0};
+  uint32_t j = threadIdx.x * E;
+  for (; j + (U - 1) * kClipThreads * E + E <= d.len; j += U * kClipThreads * E) {   // U loads under way at once
+    float v[U][E];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_n<E>(g + j + u * kClipThreads * E, v[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < E; ++i) sum[i & 1] = fma((double)v[u][i], (double)v[u][i], sum[i & 1]);
+  }
+  for (; j < d.len; j += kClipThreads * E) {
     float v[E];
     load_upto<E>(g + j, (int)(d.len - j), v);
 #pragma unroll
-    for (int i = 0; i < E; ++i) sum = fma((double)v[i], (double)v[i], sum);
+    for (int i = 0; i < E; ++i) sum[i & 1] = fma((double)v[i], (double)v[i], sum[i & 1]);
   }
-  const int wave = threadIdx.x / 64;
-  sum = wave_sum(sum);
-  if (threadIdx.x % 64 == 0) part[wave] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    sum = part[0];
-    for (int i = 1; i < kClipThreads / 64; ++i) sum += part[i];
-    __hip_atomic_store(&t.partials[(uint64_t)r * t.nchunks + c], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __hip_atomic_fetch_add(&t.arrived[r], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == t.nchunks - 1;
-  }
-  __syncthreads();
-  if (!last) return;
-  sum = 0.0;
-  for (uint32_t i = threadIdx.x; i < t.nchunks; i += kClipThreads)
-    sum += __hip_atomic_load(&t.partials[(uint64_t)r * t.nchunks + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  sum = wave_sum(sum);
-  if (threadIdx.x % 64 == 0) part[wave] = sum;
-  __syncthreads();
-  if (threadIdx.x) return;
-  sum = part[0];
-  for (int i = 1; i < kClipThreads / 64; ++i) sum += part[i];
+  const double all = group_sum(sum[0] + sum[1], part);
+  if (threadIdx.x == 0) t.partials[(uint64_t)r * t.nchunks + c] = all;
+}
+
+// Worker r's norm and factor from its chunks' sums, in their order.
+__device__ __forceinline__ float clip_factor(const ClipTables& t, const ClipCall& call, uint32_t r, double* part, float* norm_out) {
+  double sum = 0.0;
+#pragma unroll 4
+  for (uint32_t i = threadIdx.x; i < t.nchunks; i += kClipThreads) sum += t.partials[(uint64_t)r * t.nchunks + i];
+  sum = group_sum(sum, part);
   const float norm = (float)(sqrt(sum) * fabs((double)call.scale));
   const float keep = call.max_norm / (norm + call.eps);
   float factor = call.scale * (keep > 1.f ? 1.f : keep);   // a NaN stays one
   if (call.zero_nonfinite && !(norm <= 3.402823466e38f)) factor = 0.f;
-  t.factor[r] = factor;
-  if (call.norm) call.norm[r] = norm;
-  t.arrived[r] = 0;
+  if (norm_out && threadIdx.x == 0) norm_out[r] = norm;
+  return factor;
 }
 
-template <typename T, typename U>
+__global__ __launch_bounds__(kClipThreads) void k_clip_factor(ClipTables t, ClipCall call) {
+  __shared__ double part[kClipThreads / 64];
+  const float f = clip_factor(t, call, blockIdx.x, part, call.norm);
+  if (threadIdx.x == 0) t.factor[blockIdx.x] = f;
+}
+
+template <typename T, typename U, bool OWN>
 __global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipTables t, ClipCall call, const T* __restrict__ grad, U* __restrict__ out, bool in_place) {
-  constexpr int E = 16 / sizeof(U);
+  constexpr int E = 16 / sizeof(U), N = 8;
+  __shared__ double part[OWN ? kClipThreads / 64 : 1];
   const uint32_t r = blockIdx.x / t.nchunks, c = blockIdx.x % t.nchunks;
-  const float f = t.factor[r];
+  const float f = OWN ? clip_factor(t, call, r, part, c == 0 ? call.norm : nullptr) : t.factor[r];
   if (in_place && f == 1.f) return;
   const bool zero = call.zero_nonfinite && f == 0.f;   // also where an element is not finite
   const ClipChunk d = t.chunks[c];
   const T* g = grad + (uint64_t)r * t.pitch + d.off;
   U* o = out + (uint64_t)r * t.pitch + d.off;
-#pragma unroll 4
-  for (uint32_t j = threadIdx.x * E; j < d.len; j += kClipThreads * E) {
+  uint32_t j = threadIdx.x * E;
+  for (; j + (N - 1) * kClipThreads * E + E <= d.len; j += N * kClipThreads * E) {
+    float v[N][E];
+#pragma unroll
+    for (int u = 0; u < N; ++u) load_n<E>(g + j + u * kClipThreads * E, v[u]);
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[u][i] = zero ? 0.f : v[u][i] * f;
+      store_n<E>(o + j + u * kClipThreads * E, v[u]);
+    }
+  }
+  for (; j < d.len; j += kClipThreads * E) {
     float v[E];
     load_upto<E>(g + j, (int)(d.len - j), v);
 #pragma unroll
@@ -105,8 +131,13 @@ __global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipTables t, ClipC
 template <typename T, typename U>
 hipError_t launch_clip(const ClipTables& t, const ClipCall& call, const void* grad, void* out, hipStream_t s) {
   const uint32_t grid = t.P * t.nchunks;
-  k_clip_norm<T><<<grid, kClipThreads, 0, s>>>(t, call, (const T*)grad);
-  k_clip_scale<T, U><<<grid, kClipThreads, 0, s>>>(t, call, (const T*)grad, (U*)out, grad == out);
+  k_clip_squares<T><<<grid, kClipThreads, 0, s>>>(t, (const T*)grad);
+  if (t.nchunks <= kOwnSums) {
+    k_clip_scale<T, U, true><<<grid, kClipThreads, 0, s>>>(t, call, (const T*)grad, (U*)out, grad == out);
+  } else {
+    k_clip_factor<<<t.P, kClipThreads, 0, s>>>(t, call);
+    k_clip_scale<T, U, false><<<grid, kClipThreads, 0, s>>>(t, call, (const T*)grad, (U*)out, grad == out);
+  }
   return hipGetLastError();
 }
 
@@ -156,9 +187,8 @@ evg_status evg_clip_init(evg_clip** out, const evg_clip_config* cfg, void* hip_s
     c->t.nchunks = (uint32_t)chunks.size();
     c->t.P = cfg->P;
     c->t.pitch = pitch;
-    const size_t partials = (size_t)cfg->P * chunks.size() * 8, descs = chunks.size() * sizeof(ClipChunk), words = ((size_t)cfg->P * 4 + 7) / 8 * 8;
-    hipError_t e = hipMalloc(&c->owned, partials + descs + 2 * words);
-    if (e == hipSuccess) e = hipMemsetAsync(c->owned, 0, partials + descs + 2 * words, c->stream);
+    const size_t partials = (size_t)cfg->P * chunks.size() * 8, descs = chunks.size() * sizeof(ClipChunk);
+    hipError_t e = hipMalloc(&c->owned, partials + descs + (size_t)cfg->P * 4);
     char* p = (char*)c->owned;
     if (e == hipSuccess) e = hipMemcpyAsync(p + partials, chunks.data(), descs, hipMemcpyHostToDevice, c->stream);
     if (e == hipSuccess) e = hipStreamSynchronize(c->stream);
@@ -169,8 +199,7 @@ evg_status evg_clip_init(evg_clip** out, const evg_clip_config* cfg, void* hip_s
     }
     c->t.partials = (double*)p;
     c->t.chunks = (const ClipChunk*)(p + partials);
-    c->t.arrived = (uint32_t*)(p + partials + descs);
-    c->t.factor = (float*)(p + partials + descs + words);
+    c->t.factor = (float*)(p + partials + descs);
     *out = c;
   } catch (const std::exception&) {
     return fail(EVG_ERR_OOM, "host allocation failed");

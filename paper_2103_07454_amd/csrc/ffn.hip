@@ -28,6 +28,9 @@ struct evg_ffn {
 
 namespace {
 
+// Rows of the projections that are kept: whole accumulators of 32.
+uint64_t proj_rows(uint32_t rows) { return ((uint64_t)rows + 31) / 32 * 32; }
+
 // Can a product read it by 16-byte units?  Addresses, strides and rows are whole units, and a tile's rows lie within 31 bits.
 bool whole_units(const GemmOperand& o, uint64_t cols, uint32_t bytes) {
   const uint64_t e = 16 / bytes;
@@ -119,7 +122,7 @@ evg_status evg_ffn_init(evg_ffn** out, const evg_ffn_config* cfg, void* hip_stre
 
 uint64_t evg_ffn_saved_bytes(const evg_ffn* c, uint32_t rows) {
   if (!c) return 0;
-  return (uint64_t)c->cfg.workers * rows * c->pitch * (2 * sizeof(float) + type_bytes(c->cfg.type));
+  return (uint64_t)c->cfg.workers * c->pitch * (proj_rows(rows) * 2 * sizeof(float) + (uint64_t)rows * type_bytes(c->cfg.type));
 }
 
 evg_status evg_ffn_forward(evg_ffn* c, uint32_t rows, const evg_mat* x, const evg_mat* w_gate, const evg_mat* w_up,
@@ -137,7 +140,7 @@ evg_status evg_ffn_forward(evg_ffn* c, uint32_t rows, const evg_mat* x, const ev
   if ((st = check_apart(outs, 2, ins, 4)) != EVG_OK) return st;
   if (!rows) return EVG_OK;
   const uint32_t e = type_bytes(s.type);
-  const uint64_t proj = (uint64_t)s.W * rows * 2 * c->pitch;
+  const uint64_t proj = (uint64_t)s.W * proj_rows(rows) * 2 * c->pitch;
   const GemmOperand h{saved ? (char*)saved + proj * sizeof(float) : c->hidden, (int64_t)rows * c->pitch, (int64_t)c->pitch};
 
   GemmArgs g{};
@@ -147,7 +150,7 @@ evg_status evg_ffn_forward(evg_ffn* c, uint32_t rows, const evg_mat* x, const ev
   g.c[0] = h;
   g.M = rows, g.N = s.F, g.K = s.D, g.parts = 1;
   g.proj = (float*)saved;
-  g.proj_worker = (uint64_t)rows * 2 * c->pitch;
+  g.proj_worker = proj_rows(rows) * 2 * c->pitch;
   HIP_TRY(product(c, GEMM_GATED, whole_units(g.a[0], s.D, e) && whole_units(g.b[0], s.D, e) && whole_units(g.b[1], s.D, e), g));
 
   g = GemmArgs{};
@@ -183,7 +186,7 @@ evg_status evg_ffn_backward(evg_ffn* c, uint32_t rows, const evg_mat* dy, const 
                        mat_span(dw_up, s.W, s.F, s.D, s.type, "dw_up"), mat_span(dw_down, s.W, s.D, s.F, s.type, "dw_down")};
   if ((st = check_apart(outs, 4, ins, 6)) != EVG_OK) return st;
   const uint32_t e = type_bytes(s.type);
-  const uint64_t proj = (uint64_t)s.W * rows * 2 * c->pitch;
+  const uint64_t proj = (uint64_t)s.W * proj_rows(rows) * 2 * c->pitch;
   const int64_t two = 2 * (int64_t)c->pitch;
   const GemmOperand h{(const char*)saved + proj * sizeof(float), (int64_t)rows * c->pitch, (int64_t)c->pitch};
   const GemmOperand dg{c->grads, (int64_t)rows * two, two}, du{(const char*)c->grads + (uint64_t)c->pitch * e, (int64_t)rows * two, two};
@@ -195,7 +198,7 @@ evg_status evg_ffn_backward(evg_ffn* c, uint32_t rows, const evg_mat* dy, const 
     g.c[0] = dg;
     g.M = rows, g.N = s.F, g.K = s.D, g.parts = 1;
     g.proj = (float*)saved;
-    g.proj_worker = (uint64_t)rows * two;
+    g.proj_worker = proj_rows(rows) * 2 * c->pitch;
     HIP_TRY(product(c, GEMM_GATED_BWD, whole_units(g.a[0], s.D, e) && whole_units(g.b[0], s.F, e), g));
   }
   if (rows && has[0]) {

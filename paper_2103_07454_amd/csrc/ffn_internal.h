@@ -31,7 +31,7 @@ struct GemmArgs {
   uint32_t M, N, K, workers, parts;
   uint32_t tiles_m, tiles_n;
   Activation activation;
-  // GEMM_GATED, GEMM_GATED_BWD: the projections in 32 bits, row t: gate's at 0, up's at `pitch`, and the gradients in the same places of c[0]
+  // GEMM_GATED, GEMM_GATED_BWD: the projections in 32 bits, in the accumulators' order; the gradients are rows of c[0], gate's at 0, up's at `pitch`
   float* proj;
   uint64_t proj_worker;
   uint32_t pitch;                  // padded hidden width
