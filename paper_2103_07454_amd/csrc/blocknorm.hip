@@ -9,13 +9,14 @@
 //     d_pre = sum dn ur,  d_pre_bias = sum dn,  d_post = sum da ub,  d_post_bias = sum da     over a worker's rows
 // The backward pass makes both norms anew from residual and branch: nothing has to be kept, and r' is not read in rounded form.
 //
-// Both passes are bound by memory.  A row stays in the registers of 64 to 1024 threads, at most 16 elements of each tensor in a
+// Both passes are bound by memory.  A row stays in the registers of 64 to 1024 threads, 8 or 16 elements of each tensor in a
 // thread, so that each tensor is read once; the sums over a row go through the wavefront and one exchange in LDS.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
 #include <exception>
 #include <new>
+#include <type_traits>
 
 #include "nn_device.h"
 #include "nn_host.h"
@@ -48,8 +49,8 @@ __device__ __forceinline__ T* at(const evg_mat& m, uint32_t w, uint64_t row) {
 // The sums of two values over the threads that share a row.  `red` alternates between two sets, so one barrier is enough.
 template <int TPR>
 __device__ __forceinline__ void row_sum2(float& a, float& b, float (*red)[2][TPR / 64], int& turn) {
-  a = wave_sum(a);
-  b = wave_sum(b);
+  a = wave_sum_uniform(a);
+  b = wave_sum_uniform(b);
   if constexpr (TPR > 64) {
     float(&set)[2][TPR / 64] = red[turn];
     turn ^= 1;
@@ -120,22 +121,6 @@ __device__ __forceinline__ float make_unit(Row<NV>& x, const NormArgs& g, int la
   return inv;
 }
 
-// d becomes the gradient of the row whose unit row is u, d that of u on entry.
-template <int NV, int TPR, bool LAYER, typename R>
-__device__ __forceinline__ void unit_gradient(Row<NV>& d, const Row<NV>& u, float inv, const NormArgs& g, R red, int& turn) {
-  float s = 0.f, m = 0.f;
-#pragma unroll
-  for (int i = 0; i < NV * kV; ++i) {
-    s = fmaf(d.v[i], u.v[i], s);
-    if (LAYER) m += d.v[i];
-  }
-  row_sum2<TPR>(s, m, red, turn);
-  s *= g.inv_width;
-  m = LAYER ? m * g.inv_width : 0.f;
-#pragma unroll
-  for (int i = 0; i < NV * kV; ++i) d.v[i] = (d.v[i] - m - u.v[i] * s) * inv;
-}
-
 template <typename T, int NV, int TPR, bool LAYER>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_blocknorm_forward(NormArgs g) {
   constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;   // rows of a workgroup
@@ -190,9 +175,79 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_blocknorm_forward(Nor
   if (real) store_row<NV, TPR>(at<T>(g.normed, w, t), width, lane, r);
 }
 
-// One stripe of a worker's rows: the rows' gradients, and the stripe's share of the weights' and the gate's.
-template <typename T, int NV, int TPR, bool LAYER>
+// A thread's part of a row as it lies in memory, in whole registers (two 16-bit elements to each).
+template <typename T, int NV> struct Raw { uint32_t w[NV][kV * sizeof(T) / 4]; };
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Words { uint32_t w[kV * sizeof(T) / 4]; };
+
+template <typename T>
+__device__ __forceinline__ float element(const uint32_t* w, int i) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+  else if constexpr (std::is_same_v<T, bf16_t>) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  else return (float)__builtin_bit_cast(half_t, (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu));
+}
+
+// WHOLE: the width is a multiple of 8, so a lane has 8 elements or none.
+template <bool WHOLE, int NV, int TPR, typename T>
+__device__ __forceinline__ void load_raw(const T* p, int width, int lane, Raw<T, NV>& r) {
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (k * TPR + lane) * kV;
+    if (WHOLE || width >= kV) {
+      const Words<T> x = *reinterpret_cast<const Words<T>*>(p + (c + kV <= width ? c : 0));
+#pragma unroll
+      for (int i = 0; i < (int)(kV * sizeof(T) / 4); ++i) r.w[k][i] = x.w[i];
+    }
+    if (!WHOLE && width % kV && c < width && c + kV > width) {
+      T e[kV];
+#pragma unroll
+      for (int i = 0; i < kV; ++i) e[i] = c + i < width ? p[c + i] : (T)0.f;
+      __builtin_memcpy(r.w[k], e, sizeof e);
+    }
+  }
+}
+
+// As values; those beyond the width are 0.  The empty statement keeps the compiler from making them long before they are needed, which
+// would take twice the registers.
+template <int NV, int TPR, typename T>
+__device__ __forceinline__ void unpack(Raw<T, NV>& r, int width, int lane, Row<NV>& x) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int i = 0; i < kV / 2; ++i) asm volatile("" : "+v"(r.w[k][i]));
+  }
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int i = 0; i < kV; ++i) x.v[k * kV + i] = (k * TPR + lane) * kV < width ? element<T>(r.w[k], i) : 0.f;
+}
+
+template <bool WHOLE, int NV, int TPR, typename T>
+__device__ __forceinline__ void put_row(T* p, int width, int lane, const Row<NV>& r) {
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (k * TPR + lane) * kV;
+    if (WHOLE) {
+      if (c < width) store_n<kV>(p + c, r.v + k * kV);
+    } else {
+      store_upto<kV>(p + c, width - c, r.v + k * kV);
+    }
+  }
+}
+
+// A tensor's rows in their order.
+template <typename T> struct Lines {
+  T* p;
+  int64_t row;
+  __device__ __forceinline__ Lines(const evg_mat& m, uint32_t w, uint32_t t) : p(m.p ? at<T>(m, w, t) : nullptr), row(m.row) {}
+  __device__ __forceinline__ void next() { p += row; }
+};
+
+// One stripe of a worker's rows: the rows' gradients, and the stripe's share of the weights' and the gate's.  GATED, POST: whether
+// there is a gate and a norm after the block; -1: as the arguments say (widths that are no multiple of 8).
+template <typename T, int NV, int TPR, bool LAYER, int GATED, int POST>
 __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
+  constexpr bool WHOLE = GATED >= 0;
   __shared__ float red[2][2][TPR / 64];
   int turn = 0;
   const int lane = threadIdx.x;
@@ -208,96 +263,154 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
     t1 = min(g.in.rows, t0 + g.stripe_rows);
   }
   constexpr int N = NV * kV;
+  const bool branch = g.in.branch.p, pre = g.d_normed.p, direct = g.d_out.p;
+  const bool gated = GATED >= 0 ? GATED : g.in.gate.p != nullptr, post = POST >= 0 ? POST : g.in.post.p != nullptr;
+  const bool post_bias = LAYER && g.in.post_bias.p;
+  Raw<T, NV> w_post, w_postbias, w_pre;
+  if (post) load_raw<WHOLE, NV, TPR>(at<const T>(g.in.post, w, 0), width, lane, w_post);
+  if (post_bias) load_raw<WHOLE, NV, TPR>(at<const T>(g.in.post_bias, w, 0), width, lane, w_postbias);
+  if (pre) load_raw<WHOLE, NV, TPR>(at<const T>(g.in.pre, w, 0), width, lane, w_pre);
   Row<NV> s_pre, s_prebias, s_post, s_postbias, s_gate;
 #pragma unroll
   for (int i = 0; i < N; ++i) s_pre.v[i] = s_prebias.v[i] = s_post.v[i] = s_postbias.v[i] = s_gate.v[i] = 0.f;
+
+  Lines<const T> l_r(g.in.residual, w, t0), l_b(g.in.branch, w, t0), l_dn(g.d_normed, w, t0), l_do(g.d_out, w, t0);
+  Lines<T> o_r(g.d.residual, w, t0), o_b(g.d.branch, w, t0);
+  uint32_t gate_row = gated ? t0 / g.in.gate_rows : 0, until = gated ? (uint32_t)min((uint64_t)g.in.rows, (uint64_t)(gate_row + 1) * g.in.gate_rows) : 0;
+  const float alpha = g.alpha, beta = g.beta, inv_width = g.inv_width;
   for (uint32_t t = t0; t < t1; ++t) {
-    Row<NV> r, b, gate, k, d;
-    load_row<NV, TPR>(at<const T>(g.in.residual, w, t), width, lane, r);
-    float inv_b = 1.f, inv_r = 1.f;
-    Row<NV> after;
-    if (g.in.branch.p) {
-      load_row<NV, TPR>(at<const T>(g.in.branch, w, t), width, lane, b);
-      if (g.in.gate.p) load_row<NV, TPR>(at<const T>(g.in.gate, w, t / g.in.gate_rows), width, lane, gate);
-      if (g.in.post.p) {
-        inv_b = make_unit<NV, TPR, LAYER>(b, g, lane, red, turn);
-        load_row<NV, TPR>(at<const T>(g.in.post, w, 0), width, lane, k);
+    Raw<T, NV> c_r, c_b, c_gate, c_dn, c_do;
+    load_raw<WHOLE, NV, TPR>(l_r.p, width, lane, c_r);
+    if (branch) load_raw<WHOLE, NV, TPR>(l_b.p, width, lane, c_b);
+    if (gated) load_raw<WHOLE, NV, TPR>(at<const T>(g.in.gate, w, gate_row), width, lane, c_gate);
+    if (pre) load_raw<WHOLE, NV, TPR>(l_dn.p, width, lane, c_dn);
+    if (direct) load_raw<WHOLE, NV, TPR>(l_do.p, width, lane, c_do);
+    l_r.next(), l_b.next(), l_dn.next(), l_do.next();
+    Row<NV> r, b, k, d;
+    float inv_b = 1.f;
+    // after the block: the unit row stays in b, and is scaled where it is needed
+    auto after = [&](Row<NV>& a) {
+      a = b;
+      if (post) {
+        unpack<NV, TPR>(w_post, width, lane, a);
 #pragma unroll
-        for (int i = 0; i < N; ++i) after.v[i] = b.v[i] * k.v[i];
-        if (LAYER && g.in.post_bias.p) {
-          load_row<NV, TPR>(at<const T>(g.in.post_bias, w, 0), width, lane, k);
+        for (int i = 0; i < N; ++i) a.v[i] *= b.v[i];
+        if (post_bias) {
+          Row<NV> e;
+          unpack<NV, TPR>(w_postbias, width, lane, e);
 #pragma unroll
-          for (int i = 0; i < N; ++i) after.v[i] += k.v[i];
+          for (int i = 0; i < N; ++i) a.v[i] += e.v[i];
         }
-      } else {
-        after = b;
       }
+    };
+    if (branch) {
+      unpack<NV, TPR>(c_b, width, lane, b);
+      if (post) inv_b = make_unit<NV, TPR, LAYER>(b, g, lane, red, turn);
+      Row<NV> a;
+      after(a);
+      if (gated) {
+        unpack<NV, TPR>(c_gate, width, lane, k);
 #pragma unroll
-      for (int i = 0; i < N; ++i) r.v[i] = fmaf(g.alpha, r.v[i], g.beta * (g.in.gate.p ? gate.v[i] * after.v[i] : after.v[i]));
+        for (int i = 0; i < N; ++i) a.v[i] *= k.v[i];
+      }
+      unpack<NV, TPR>(c_r, width, lane, r);
+#pragma unroll
+      for (int i = 0; i < N; ++i) r.v[i] = fmaf(alpha, r.v[i], beta * a.v[i]);
     } else {
+      unpack<NV, TPR>(c_r, width, lane, r);
 #pragma unroll
-      for (int i = 0; i < N; ++i) r.v[i] *= g.alpha;
+      for (int i = 0; i < N; ++i) r.v[i] *= alpha;
     }
-    if (g.d_normed.p) {
-      inv_r = make_unit<NV, TPR, LAYER>(r, g, lane, red, turn);
-      load_row<NV, TPR>(at<const T>(g.d_normed, w, t), width, lane, d);
-      load_row<NV, TPR>(at<const T>(g.in.pre, w, 0), width, lane, k);
+    if (pre) {
+      // with q = dn pre:  (q - mean(q) - r mean(q r) / s^2) / s of the centred row r, whose two sums go together
+      unpack<NV, TPR>(c_dn, width, lane, d);
+      unpack<NV, TPR>(w_pre, width, lane, k);
+      float mean_q = 0.f;
+      if constexpr (LAYER) {
+        float sr = 0.f, sq = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) { sr += r.v[i]; sq = fmaf(d.v[i], k.v[i], sq); }
+        row_sum2<TPR>(sr, sq, red, turn);
+        const float mean = sr * inv_width;
+        mean_q = sq * inv_width;
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.v[i] = ((i / kV) * TPR + lane) * kV + i % kV < width ? r.v[i] - mean : 0.f;
+      }
+      float ss = 0.f, qr = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) { ss = fmaf(r.v[i], r.v[i], ss); qr = fmaf(d.v[i] * k.v[i], r.v[i], qr); }
+      row_sum2<TPR>(ss, qr, red, turn);
+      const float inv = 1.f / sqrtf(ss * inv_width + g.eps);
+      const float c = qr * inv_width * inv;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        s_pre.v[i] = fmaf(d.v[i], r.v[i], s_pre.v[i]);
+        const float u = r.v[i] * inv;
+        s_pre.v[i] = fmaf(d.v[i], u, s_pre.v[i]);
         if (LAYER) s_prebias.v[i] += d.v[i];
-        d.v[i] *= k.v[i];
+        d.v[i] = (d.v[i] * k.v[i] - mean_q - u * c) * inv;
       }
-      unit_gradient<NV, TPR, LAYER>(d, r, inv_r, g, red, turn);
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) d.v[i] = 0.f;
     }
-    if (g.d_out.p) {
-      load_row<NV, TPR>(at<const T>(g.d_out, w, t), width, lane, k);
+    if (direct) {
+      unpack<NV, TPR>(c_do, width, lane, k);
 #pragma unroll
       for (int i = 0; i < N; ++i) d.v[i] += k.v[i];
     }
-    if (g.d.residual.p) {
+    if (o_r.p) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) k.v[i] = g.alpha * d.v[i];
-      store_row<NV, TPR>(at<T>(g.d.residual, w, t), width, lane, k);
+      for (int i = 0; i < N; ++i) k.v[i] = alpha * d.v[i];
+      put_row<WHOLE, NV, TPR>(o_r.p, width, lane, k);
+      o_r.next();
     }
-    if (!g.in.branch.p) continue;
-    if (g.in.gate.p) {
+    if (!branch) continue;
 #pragma unroll
-      for (int i = 0; i < N; ++i) s_gate.v[i] = fmaf(g.beta * d.v[i], after.v[i], s_gate.v[i]);
-      const bool ends = !g.group_stripes && (t + 1 == g.in.rows || (t + 1) % g.in.gate_rows == 0);
-      if (ends) {
-        if (g.d.gate.p) store_row<NV, TPR>(at<T>(g.d.gate, w, t / g.in.gate_rows), width, lane, s_gate);
+    for (int i = 0; i < N; ++i) d.v[i] *= beta;
+    if (gated) {
+      after(k);
+#pragma unroll
+      for (int i = 0; i < N; ++i) s_gate.v[i] = fmaf(d.v[i], k.v[i], s_gate.v[i]);
+      unpack<NV, TPR>(c_gate, width, lane, k);
+#pragma unroll
+      for (int i = 0; i < N; ++i) d.v[i] *= k.v[i];
+      if (t + 1 == until && !g.group_stripes) {
+        if (g.d.gate.p) put_row<WHOLE, NV, TPR>(at<T>(g.d.gate, w, gate_row), width, lane, s_gate);
 #pragma unroll
         for (int i = 0; i < N; ++i) s_gate.v[i] = 0.f;
+        ++gate_row;
+        until = (uint32_t)min((uint64_t)g.in.rows, (uint64_t)until + g.in.gate_rows);
       }
-#pragma unroll
-      for (int i = 0; i < N; ++i) d.v[i] = g.beta * d.v[i] * gate.v[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) d.v[i] *= g.beta;
     }
-    if (g.in.post.p) {
-      load_row<NV, TPR>(at<const T>(g.in.post, w, 0), width, lane, k);
+    if (post) {
+      unpack<NV, TPR>(w_post, width, lane, k);
+      float pb = 0.f, sp = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         s_post.v[i] = fmaf(d.v[i], b.v[i], s_post.v[i]);
         if (LAYER) s_postbias.v[i] += d.v[i];
         d.v[i] *= k.v[i];
+        pb = fmaf(d.v[i], b.v[i], pb);
+        if (LAYER) sp += d.v[i];
       }
-      unit_gradient<NV, TPR, LAYER>(d, b, inv_b, g, red, turn);
+      row_sum2<TPR>(pb, sp, red, turn);
+      pb *= inv_width;
+      sp *= inv_width;
+#pragma unroll
+      for (int i = 0; i < N; ++i) d.v[i] = (d.v[i] - sp - b.v[i] * pb) * inv_b;
     }
-    if (g.d.branch.p) store_row<NV, TPR>(at<T>(g.d.branch, w, t), width, lane, d);
+    if (o_b.p) {
+      put_row<WHOLE, NV, TPR>(o_b.p, width, lane, d);
+      o_b.next();
+    }
   }
   float* p = g.partials + ((uint64_t)w * g.stripes + stripe) * 5 * g.padded;
-  const int padded = (int)g.padded;
-  if (g.d.pre.p) store_row<NV, TPR>(p, padded, lane, s_pre);
-  if (LAYER && g.d.pre_bias.p) store_row<NV, TPR>(p + padded, padded, lane, s_prebias);
-  if (g.d.post.p) store_row<NV, TPR>(p + 2 * padded, padded, lane, s_post);
-  if (LAYER && g.d.post_bias.p) store_row<NV, TPR>(p + 3 * padded, padded, lane, s_postbias);
-  if (g.d.gate.p && g.group_stripes) store_row<NV, TPR>(p + 4 * padded, padded, lane, s_gate);
+  const int padded = (int)g.padded;   // a multiple of 64
+  if (g.d.pre.p) put_row<true, NV, TPR>(p, padded, lane, s_pre);
+  if (LAYER && g.d.pre_bias.p) put_row<true, NV, TPR>(p + padded, padded, lane, s_prebias);
+  if (g.d.post.p) put_row<true, NV, TPR>(p + 2 * padded, padded, lane, s_post);
+  if (LAYER && g.d.post_bias.p) put_row<true, NV, TPR>(p + 3 * padded, padded, lane, s_postbias);
+  if (g.d.gate.p && g.group_stripes) put_row<true, NV, TPR>(p + 4 * padded, padded, lane, s_gate);
 }
 
 // Adds the stripes' shares, in their order: 64 columns to a workgroup, each of its wavefronts has every 16th stripe.
@@ -326,31 +439,48 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_blocknorm_join(NormArgs g, 
 }
 
 template <typename T, int NV, int TPR, bool LAYER>
-hipError_t launch_sized(const NormArgs& g, bool backward, hipStream_t s) {
-  if (!backward) {
-    constexpr int rows = TPR < 256 ? 256 / TPR : 1;
-    const uint64_t all = (uint64_t)g.workers * g.in.rows;
-    k_blocknorm_forward<T, NV, TPR, LAYER><<<(uint32_t)((all + rows - 1) / rows), TPR * rows, 0, s>>>(g);
-  } else if (g.stripes) {
-    k_blocknorm_backward<T, NV, TPR, LAYER><<<g.workers * g.stripes, TPR, 0, s>>>(g);
-  }
+hipError_t forward_sized(const NormArgs& g, hipStream_t s) {
+  constexpr int rows = TPR < 256 ? 256 / TPR : 1;
+  const uint64_t all = (uint64_t)g.workers * g.in.rows;
+  k_blocknorm_forward<T, NV, TPR, LAYER><<<(uint32_t)((all + rows - 1) / rows), TPR * rows, 0, s>>>(g);
   return hipGetLastError();
 }
 
 template <typename T, bool LAYER>
-hipError_t launch_kind(const NormArgs& g, bool backward, hipStream_t s) {
-  if (g.width <= 512) return launch_sized<T, 1, 64, LAYER>(g, backward, s);
-  if (g.width <= 1024) return launch_sized<T, 2, 64, LAYER>(g, backward, s);
-  if (g.width <= 2048) return launch_sized<T, 2, 128, LAYER>(g, backward, s);
-  if (g.width <= 4096) return launch_sized<T, 2, 256, LAYER>(g, backward, s);
-  if (g.width <= 8192) return launch_sized<T, 2, 512, LAYER>(g, backward, s);
-  return launch_sized<T, 2, 1024, LAYER>(g, backward, s);
+hipError_t launch_forward(const NormArgs& g, hipStream_t s) {
+  if (g.width <= 512) return forward_sized<T, 1, 64, LAYER>(g, s);
+  if (g.width <= 1024) return forward_sized<T, 2, 64, LAYER>(g, s);
+  if (g.width <= 2048) return forward_sized<T, 2, 128, LAYER>(g, s);
+  if (g.width <= 4096) return forward_sized<T, 2, 256, LAYER>(g, s);
+  if (g.width <= 8192) return forward_sized<T, 2, 512, LAYER>(g, s);
+  return forward_sized<T, 2, 1024, LAYER>(g, s);
+}
+
+template <typename T, bool LAYER, int GATED, int POST>
+hipError_t backward_sized(const NormArgs& g, hipStream_t s) {
+  const uint32_t grid = g.workers * g.stripes;
+  if (!grid) return hipSuccess;
+  if (g.width <= 512) k_blocknorm_backward<T, 1, 64, LAYER, GATED, POST><<<grid, 64, 0, s>>>(g);
+  else if (g.width <= 1024) k_blocknorm_backward<T, 1, 128, LAYER, GATED, POST><<<grid, 128, 0, s>>>(g);
+  else if (g.width <= 2048) k_blocknorm_backward<T, 1, 256, LAYER, GATED, POST><<<grid, 256, 0, s>>>(g);
+  else if (g.width <= 4096) k_blocknorm_backward<T, 1, 512, LAYER, GATED, POST><<<grid, 512, 0, s>>>(g);
+  else if (g.width <= 8192) k_blocknorm_backward<T, 1, 1024, LAYER, GATED, POST><<<grid, 1024, 0, s>>>(g);
+  else k_blocknorm_backward<T, 2, 1024, LAYER, GATED, POST><<<grid, 1024, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+template <typename T, bool LAYER>
+hipError_t launch_backward(const NormArgs& g, hipStream_t s) {
+  if (g.width % kV) return backward_sized<T, LAYER, -1, -1>(g, s);
+  if (g.in.gate.p) return g.in.post.p ? backward_sized<T, LAYER, 1, 1>(g, s) : backward_sized<T, LAYER, 1, 0>(g, s);
+  return g.in.post.p ? backward_sized<T, LAYER, 0, 1>(g, s) : backward_sized<T, LAYER, 0, 0>(g, s);
 }
 
 template <typename T>
 hipError_t launch_blocknorm(const NormArgs& g, uint32_t kind, bool backward, hipStream_t s) {
-  hipError_t e = kind == EVG_NORM_LAYER ? launch_kind<T, true>(g, backward, s) : launch_kind<T, false>(g, backward, s);
-  if (e != hipSuccess || !backward) return e;
+  if (!backward) return kind == EVG_NORM_LAYER ? launch_forward<T, true>(g, s) : launch_forward<T, false>(g, s);
+  const hipError_t e = kind == EVG_NORM_LAYER ? launch_backward<T, true>(g, s) : launch_backward<T, false>(g, s);
+  if (e != hipSuccess) return e;
   const uint32_t groups = g.d.gate.p && g.group_stripes ? g.stripes / g.group_stripes : 0;
   if (!g.d.pre.p && !g.d.pre_bias.p && !g.d.post.p && !g.d.post_bias.p && !groups) return hipSuccess;
   k_blocknorm_join<T><<<(g.width + 63) / 64 * g.workers * (4 + groups), kJoinWaves * 64, 0, s>>>(g, groups);

@@ -60,4 +60,20 @@ __device__ __forceinline__ F wave_sum(F v) {
   return v;
 }
 
+// The same of 32-bit values without the LDS permutes, whose latency a row's dependent sums would add up: the lanes of 16 by data-parallel
+// moves, then rows of 16 into the next and halves into the last lane, from where it is uniform.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum_uniform(float v) {
+  v += moved<0xB1, 0xf>(v);    // lanes 1 0 3 2
+  v += moved<0x4E, 0xf>(v);    // lanes 2 3 0 1
+  v += moved<0x141, 0xf>(v);   // mirrored within 8
+  v += moved<0x140, 0xf>(v);   // mirrored within 16
+  v += moved<0x142, 0xa>(v);   // row 0's into row 1, row 2's into row 3
+  v += moved<0x143, 0xc>(v);   // the lower half's into the upper one
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
 }  // namespace evg
