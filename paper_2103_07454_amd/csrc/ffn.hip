@@ -42,7 +42,8 @@ GemmOperand operand(const evg_mat& m, uint32_t workers, uint64_t rows, uint64_t 
 }
 
 // The largest tile of which there are enough to occupy the chip.
-GemmTile choose_tile(const GemmArgs& g, uint32_t n, uint32_t share, bool aligned, uint32_t type) {
+GemmTile choose_tile(GemmOp op, const GemmArgs& g, uint32_t n, uint32_t share, bool aligned, uint32_t type) {
+  if ((op == GEMM_GATED || op == GEMM_DOWN) && g.M <= kMostRows) return TILE_ROWS;
   auto count = [&](uint64_t bm, uint64_t bn) { return ((g.M + bm - 1) / bm) * ((n + bn / share - 1) / (bn / share)) * g.workers * g.parts; };
   if (aligned && type != EVG_F32 && count(256, 256) >= 200) return TILE_256;
   if (count(128, 128) >= 256) return TILE_128;
@@ -56,7 +57,7 @@ hipError_t product(const evg_ffn* c, GemmOp op, bool aligned, GemmArgs& g) {
                   c->cfg.activation == EVG_ACT_GELU};
   g.pitch = c->pitch;
   const bool padded = op == GEMM_GATED || op == GEMM_GATED_BWD;
-  const GemmTile tile = choose_tile(g, padded ? g.pitch : g.N, op == GEMM_GATED ? 2 : 1, aligned, c->cfg.type);
+  const GemmTile tile = choose_tile(op, g, padded ? g.pitch : g.N, op == GEMM_GATED ? 2 : 1, aligned, c->cfg.type);
   if (c->cfg.type == EVG_F32) return launch_gemm<float>(op, tile, aligned, g, c->stream);
   if (c->cfg.type == EVG_F16) return launch_gemm<half_t>(op, tile, aligned, g, c->stream);
   return launch_gemm<bf16_t>(op, tile, aligned, g, c->stream);

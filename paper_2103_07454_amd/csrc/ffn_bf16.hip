@@ -1,5 +1,5 @@
 // The feed-forward block's matrix products, bf16.
-#include "ffn_gemm_device.h"
+#include "ffn_rows_device.h"
 
 namespace evg {
 

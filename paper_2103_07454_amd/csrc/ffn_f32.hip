@@ -1,5 +1,5 @@
 // The feed-forward block's matrix products, 32 bits.
-#include "ffn_gemm_device.h"
+#include "ffn_rows_device.h"
 
 namespace evg {
 

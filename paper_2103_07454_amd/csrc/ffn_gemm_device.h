@@ -385,17 +385,4 @@ hipError_t launch_op(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t launch_any(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g, hipStream_t s) {
-  const bool erf = g.activation.erf;
-  switch (op) {
-    case GEMM_GATED: return erf ? launch_op<T, GEMM_GATED, true>(tile, aligned, g, s) : launch_op<T, GEMM_GATED, false>(tile, aligned, g, s);
-    case GEMM_GATED_BWD: return erf ? launch_op<T, GEMM_GATED_BWD, true>(tile, aligned, g, s) : launch_op<T, GEMM_GATED_BWD, false>(tile, aligned, g, s);
-    case GEMM_DOWN: return launch_op<T, GEMM_DOWN, false>(tile, aligned, g, s);
-    case GEMM_INPUT: return launch_op<T, GEMM_INPUT, false>(tile, aligned, g, s);
-    case GEMM_WEIGHT: return launch_op<T, GEMM_WEIGHT, false>(tile, aligned, g, s);
-    default: return hipErrorInvalidValue;
-  }
-}
-
 }  // namespace evg

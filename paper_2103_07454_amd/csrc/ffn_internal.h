@@ -38,7 +38,8 @@ struct GemmArgs {
 };
 
 // Tile shapes.
-enum GemmTile : uint32_t { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2 };
+enum GemmTile : uint32_t { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_ROWS = 3 };   // TILE_ROWS: GEMM_GATED and GEMM_DOWN of at most kMostRows tokens
+constexpr uint32_t kMostRows = 64;
 
 template <typename T> hipError_t launch_gemm(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g, hipStream_t s);
 

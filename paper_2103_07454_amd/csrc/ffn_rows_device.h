@@ -1,0 +1,184 @@
+// The forward products for few tokens: every weight is read once, straight into the matrix cores' fragments.
+//
+// A workgroup has 16 columns (of gate and of up) and all tokens, up to 16 G; its wavefronts share out k, 128 bytes of each weight row in
+// turn, and their sums meet in LDS in a fixed order.  Nothing goes through LDS on the way in: no weight is used twice, and the tokens come
+// from the L2.  Bound by memory: what counts is how many loads are under way, so each wavefront asks for up to four steps at once.
+#pragma once
+#include "ffn_gemm_device.h"
+
+namespace evg {
+
+__device__ __forceinline__ f32x4 mfma16(const Frag<half_t>& a, const Frag<half_t>& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a.v), __builtin_bit_cast(f16x8, b.v), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.v), __builtin_bit_cast(bf16x8, b.v), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(const Frag<float>& a, const Frag<float>& b, f32x4 c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.v[i]), __uint_as_float(b.v[i]), c, 0, 0, 0);
+  return c;
+}
+
+template <typename T, int OP, bool ERF, int G, int kRowWaves>
+__global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
+  constexpr int E = 16 / sizeof(T), STEP = 128 / sizeof(T), B = OP == GEMM_GATED ? 2 : 1;
+  constexpr int AHEAD = G == 1 ? 4 : 2;
+  __shared__ f32x4 sums[kRowWaves][B * G][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t groups = g.tiles_n, w = blockIdx.x / groups, n0 = blockIdx.x % groups * 16;
+  const int row = lane & 15, quarter = lane >> 4;
+  // A fragment's lane has 16 bytes of one row.  Rows that there are not read the last one's, and what comes of them is not stored.
+  const T* wp[B];
+#pragma unroll
+  for (int b = 0; b < B; ++b) wp[b] = (const T*)g.b[b].p + (int64_t)w * g.b[b].worker + (int64_t)min(n0 + row, g.N - 1) * g.b[b].ld + quarter * E;
+  const T* xp[G];
+#pragma unroll
+  for (int i = 0; i < G; ++i) xp[i] = (const T*)g.a[0].p + (int64_t)w * g.a[0].worker + (int64_t)min(i * 16u + row, g.M - 1) * g.a[0].ld + quarter * E;
+  f32x4 acc[B][G];
+#pragma unroll
+  for (int b = 0; b < B; ++b)
+#pragma unroll
+    for (int i = 0; i < G; ++i) acc[b][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  auto load = [](const T* p) {
+    Frag<T> f;
+    __builtin_memcpy(&f.v, __builtin_assume_aligned(p, sizeof(T)), 16);
+    return f;
+  };
+  const uint32_t whole = g.K / STEP;   // steps
+  auto run = [&](uint32_t step, auto count) {   // `count` steps of this wavefront from `step` on
+    constexpr int C = decltype(count)::value;
+    Frag<T> fw[C][2][B], fx[C][2][G];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const uint32_t k = (step + c * kRowWaves) * STEP;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int b = 0; b < B; ++b) fw[c][half][b] = load(wp[b] + k + half * (STEP / 2));
+#pragma unroll
+        for (int i = 0; i < G; ++i) fx[c][half][i] = load(xp[i] + k + half * (STEP / 2));
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);   // all of them are asked for before the first is used
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+          for (int i = 0; i < G; ++i) acc[b][i] = mfma16(fw[c][half][b], fx[c][half][i], acc[b][i]);
+  };
+  uint32_t step = wave;
+  for (; step + (AHEAD - 1) * kRowWaves < whole; step += AHEAD * kRowWaves) run(step, std::integral_constant<int, AHEAD>{});
+  if (AHEAD > 2 && step + kRowWaves < whole) {
+    run(step, std::integral_constant<int, 2>{});
+    step += 2 * kRowWaves;
+  }
+  if (step < whole) {
+    run(step, std::integral_constant<int, 1>{});
+    step += kRowWaves;
+  }
+  if (step == whole && g.K % STEP) {   // what is left of k: 16 bytes that reach beyond it are read element by element
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const uint32_t k = whole * STEP + half * (STEP / 2);
+      const int left = (int)(g.K - k) - quarter * E;
+      auto some = [&](const T* p) {
+        Frag<T> f;
+        f.v = u32x4{0, 0, 0, 0};
+        if (left >= E) return load(p + k);
+        if (left > 0) {
+          T e[E];
+#pragma unroll
+          for (int j = 0; j < E; ++j) e[j] = j < left ? p[k + j] : (T)0.f;
+          __builtin_memcpy(&f.v, e, 16);
+        }
+        return f;
+      };
+      Frag<T> fw[B];
+#pragma unroll
+      for (int b = 0; b < B; ++b) fw[b] = some(wp[b]);
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        const Frag<T> fx = some(xp[i]);
+#pragma unroll
+        for (int b = 0; b < B; ++b) acc[b][i] = mfma16(fw[b], fx, acc[b][i]);
+      }
+    }
+  }
+
+#pragma unroll
+  for (int b = 0; b < B; ++b)
+#pragma unroll
+    for (int i = 0; i < G; ++i) sums[wave][b * G + i][lane] = acc[b][i];
+  __syncthreads();
+  if (wave >= G) return;
+  f32x4 v[B];
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+    v[b] = sums[0][b * G + wave][lane];
+#pragma unroll
+    for (int s = 1; s < kRowWaves; ++s) v[b] += sums[s][b * G + wave][lane];
+  }
+  // A lane has four neighbouring columns of one token.
+  const uint32_t m = wave * 16 + row, n = n0 + quarter * 4;
+  if (m >= g.M) return;
+  T* const c = (T*)g.c[0].p + (int64_t)w * g.c[0].worker + (int64_t)m * g.c[0].ld + n;
+  if constexpr (OP == GEMM_GATED) {
+    float gate[4], up[4], h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool real = n + e < g.N;   // the columns up to `pitch` are 0
+      gate[e] = real ? v[0][e] : 0.f;
+      up[e] = real ? v[1][e] : 0.f;
+      float a, slope;
+      activate<ERF, sizeof(T) == 2>(g.activation, gate[e], a, slope);
+      h[e] = real ? a * up[e] : 0.f;
+    }
+    store_n<4>(c, h);
+    if (g.proj) {
+      float* p = proj_at(g, w, m, n, (int)(n >> 3 & 3), (int)((m & 31) + (n >> 2 & 1) * 32));
+      *(f32x4*)p = f32x4{gate[0], gate[1], gate[2], gate[3]};
+      *(f32x4*)(p + 1024) = f32x4{up[0], up[1], up[2], up[3]};
+    }
+  } else {
+    const float y[4] = {v[0][0], v[0][1], v[0][2], v[0][3]};
+    store_upto<4>(c, (int)g.N - (int)n, y);
+  }
+}
+
+template <typename T, int OP, bool ERF>
+hipError_t launch_rows(GemmArgs g, hipStream_t s) {
+  g.tiles_n = ((OP == GEMM_GATED ? g.pitch : g.N) + 15) / 16;
+  const uint64_t grid = (uint64_t)g.tiles_n * g.workers;
+  if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  constexpr int waves = OP == GEMM_GATED ? 8 : 16;   // 16 columns of gate and of up, or of one product: as many loads
+  if (g.M <= 16) k_ffn_rows<T, OP, ERF, 1, waves><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
+  else if (g.M <= 32) k_ffn_rows<T, OP, ERF, 2, waves><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
+  else k_ffn_rows<T, OP, ERF, 4, waves><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_any(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g, hipStream_t s) {
+  const bool erf = g.activation.erf;
+  if (tile == TILE_ROWS) {
+    if (g.M > kMostRows || !g.M) return hipErrorInvalidValue;
+    if (op == GEMM_DOWN) return launch_rows<T, GEMM_DOWN, false>(g, s);
+    if (op != GEMM_GATED) return hipErrorInvalidValue;
+    return erf ? launch_rows<T, GEMM_GATED, true>(g, s) : launch_rows<T, GEMM_GATED, false>(g, s);
+  }
+  switch (op) {
+    case GEMM_GATED: return erf ? launch_op<T, GEMM_GATED, true>(tile, aligned, g, s) : launch_op<T, GEMM_GATED, false>(tile, aligned, g, s);
+    case GEMM_GATED_BWD: return erf ? launch_op<T, GEMM_GATED_BWD, true>(tile, aligned, g, s) : launch_op<T, GEMM_GATED_BWD, false>(tile, aligned, g, s);
+    case GEMM_DOWN: return launch_op<T, GEMM_DOWN, false>(tile, aligned, g, s);
+    case GEMM_INPUT: return launch_op<T, GEMM_INPUT, false>(tile, aligned, g, s);
+    case GEMM_WEIGHT: return launch_op<T, GEMM_WEIGHT, false>(tile, aligned, g, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace evg

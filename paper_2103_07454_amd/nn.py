@@ -12,6 +12,7 @@ that a call allocates belong to the operator's stream.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
@@ -60,6 +61,14 @@ class FFNConfig(C.Structure):
                 ("type", C.c_uint32), ("activation", C.c_uint32), ("train", C.c_uint32)]
 
 
+# Arguments that are structures go as packed bytes, which costs a call less than filling ctypes structures: evg_mat,
+# evg_blocknorm_in and evg_blocknorm_grads.
+_MAT = struct.Struct("3q").pack
+_IN = struct.Struct("2I21q").pack
+_GRADS = struct.Struct("21q").pack
+assert struct.calcsize("3q") == C.sizeof(Mat) and struct.calcsize("2I21q") == C.sizeof(BlockNormIn)
+_ABSENT = (0, 0, 0)
+
 _lib = None
 
 
@@ -67,12 +76,12 @@ def lib():
     global _lib
     if _lib is None:
         l = evg.lib()
-        vp, mp, u32 = C.c_void_p, C.POINTER(Mat), C.c_uint32
+        vp, mp, u32 = C.c_void_p, C.c_void_p, C.c_uint32
         l.evg_clip_init.argtypes = [C.POINTER(vp), C.POINTER(ClipConfig), vp]
         l.evg_clip_run.argtypes = [vp, vp, vp, C.c_float, C.c_float, vp]
         l.evg_blocknorm_init.argtypes = [C.POINTER(vp), C.POINTER(BlockNormConfig), vp]
-        l.evg_blocknorm_forward.argtypes = [vp, C.POINTER(BlockNormIn), mp, mp]
-        l.evg_blocknorm_backward.argtypes = [vp, C.POINTER(BlockNormIn), mp, mp, C.POINTER(BlockNormGrads)]
+        l.evg_blocknorm_forward.argtypes = [vp, mp, mp, mp]
+        l.evg_blocknorm_backward.argtypes = [vp, mp, mp, mp, mp]
         l.evg_ffn_init.argtypes = [C.POINTER(vp), C.POINTER(FFNConfig), vp]
         l.evg_ffn_saved_bytes.argtypes = [vp, u32]
         l.evg_ffn_saved_bytes.restype = C.c_uint64
@@ -101,29 +110,35 @@ class _Operator:
             raise ValueError("device must be a GPU")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self._raw = self.stream.cuda_stream
         self._h = C.c_void_p()
 
     def _make(self, init, cfg):
         with torch.cuda.device(self.device):
-            evg._check(init(C.byref(self._h), C.byref(cfg), C.c_void_p(self.stream.cuda_stream)))
+            evg._check(init(C.byref(self._h), C.byref(cfg), C.c_void_p(self._raw)))
 
-    def _empty(self, *shape, dtype=None):
-        if torch.cuda.current_stream(self.device) == self.stream:
+    def _empty(self, shape, dtype=None):
+        """Memory of the operator's stream."""
+        if torch._C._cuda_getCurrentRawStream(self._index) == self._raw:
             return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
 
-    def _mat(self, t, shape, what):
-        """A tensor of the given shape, [workers, rows, columns] or [workers, columns], as the library takes it."""
-        if t.dtype != self.dtype or t.device != self.device:
+    def _at(self, t, shape, what):
+        """Address and strides of a tensor of the given shape, [workers, rows, columns] or [workers, columns]."""
+        if t.dtype is not self.dtype or t.get_device() != self._index:
             raise ValueError(f"{what} must be {self.dtype} on {self.device}, is {t.dtype} on {t.device}")
         if t.shape != shape:
             raise ValueError(f"{what} must have the shape {tuple(shape)}, has {tuple(t.shape)}")
         stride = t.stride()
         if stride[-1] != 1 and shape[-1] > 1:
             raise ValueError(f"{what}: the last axis must have stride 1")
-        return Mat(t.data_ptr() or _NOTHING, stride[0], stride[1] if len(stride) == 3 else 0)
+        return t.data_ptr() or _NOTHING, stride[0], stride[1] if len(stride) == 3 else 0
+
+    def _mat(self, t, shape, what):
+        return _MAT(*self._at(t, shape, what))
 
     def _rows(self, t, width, what):
         if t.dim() != 3 or t.shape[0] != self.workers or t.shape[2] != width:
@@ -168,12 +183,12 @@ class GradClip(_Operator):
         """``(out, norm)``: the clipped arena and each worker's norm.  ``out`` may be ``grad`` itself."""
         shape = (self.workers, self.pitch)
         if out is None:
-            out = self._empty(*shape, dtype=self.out_dtype)
+            out = self._empty(shape, self.out_dtype)
         if norm is None:
-            norm = self._empty(self.workers, dtype=torch.float32)
+            norm = self._empty(self.workers, torch.float32)
         for t, dtype, size, what in ((grad, self.dtype, shape, "grad"), (out, self.out_dtype, shape, "out"),
                                      (norm, torch.float32, shape[:1], "norm")):
-            if t.dtype != dtype or t.device != self.device or t.shape != size or not t.is_contiguous():
+            if t.dtype is not dtype or t.get_device() != self._index or t.shape != size or not t.is_contiguous():
                 raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {size} on {self.device}")
         evg._check(lib().evg_clip_run(self._h, grad.data_ptr(), out.data_ptr(), max_norm, scale, norm.data_ptr()))
         return out, norm
@@ -197,35 +212,35 @@ class BlockNorm(_Operator):
         self._make(lib().evg_blocknorm_init, BlockNormConfig(self.workers, self.width, self.max_rows, _TYPES[dtype], kind, eps,
                                                              residual_scale, branch_scale))
 
-    def _shapes(self, rows):
-        vector = (self.workers, self.width)
-        token = (self.workers, rows, self.width)
-        gate = (self.workers, -(-rows // self.gate_rows) if self.gate_rows else 0, self.width)
-        return dict(residual=token, branch=token, gate=gate, post=vector, post_bias=vector, pre=vector, pre_bias=vector)
-
-    def _in(self, given):
-        rows = self._rows(given["residual"], self.width, "residual")
-        if given["gate"] is not None and not self.gate_rows:
-            raise ValueError("a gate is given, but the operator was made without gate_rows")
-        shapes = self._shapes(rows)
-        arg = BlockNormIn(rows, self.gate_rows)
-        for name, t in given.items():
-            if t is not None:
-                setattr(arg, name, self._mat(t, shapes[name], name))
-        return arg, shapes
+    def _in(self, residual, branch, gate, post, post_bias, pre, pre_bias):
+        """The shapes of tokens, the gate and weights, and the inputs as the library takes them."""
+        rows = self._rows(residual, self.width, "residual")
+        token, vector, gates = residual.shape, (self.workers, self.width), None
+        at = self._at
+        if gate is not None:
+            if not self.gate_rows:
+                raise ValueError("a gate is given, but the operator was made without gate_rows")
+            gates = (self.workers, -(-rows // self.gate_rows), self.width)
+        return token, gates, vector, _IN(
+            rows, self.gate_rows, *at(residual, token, "residual"),
+            *(_ABSENT if branch is None else at(branch, token, "branch")),
+            *(_ABSENT if gate is None else at(gate, gates, "gate")),
+            *(_ABSENT if post is None else at(post, vector, "post")),
+            *(_ABSENT if post_bias is None else at(post_bias, vector, "post_bias")),
+            *(_ABSENT if pre is None else at(pre, vector, "pre")),
+            *(_ABSENT if pre_bias is None else at(pre_bias, vector, "pre_bias")))
 
     def forward(self, residual, branch=None, *, gate=None, post=None, post_bias=None, pre=None, pre_bias=None,
                 residual_out=None, normed=None):
         """``(residual', normed)``; ``normed`` is None without ``pre``.  ``residual_out`` may be ``residual`` itself."""
-        arg, shapes = self._in(dict(residual=residual, branch=branch, gate=gate, post=post, post_bias=post_bias, pre=pre,
-                                    pre_bias=pre_bias))
+        token, _, _, arg = self._in(residual, branch, gate, post, post_bias, pre, pre_bias)
         same = branch is None and self._keeps and residual_out is None    # residual' is the residual
         if not same and residual_out is None:
-            residual_out = self._empty(*shapes["residual"])
+            residual_out = self._empty(token)
         if normed is None and pre is not None:
-            normed = self._empty(*shapes["residual"])
-        out = None if same else self._mat(residual_out, shapes["residual"], "residual_out")
-        n = None if normed is None else self._mat(normed, shapes["residual"], "normed")
+            normed = self._empty(token)
+        out = None if same else self._mat(residual_out, token, "residual_out")
+        n = None if normed is None else self._mat(normed, token, "normed")
         if out is not None or n is not None:
             evg._check(lib().evg_blocknorm_forward(self._h, arg, out, n))
         return residual if same else residual_out, normed
@@ -235,19 +250,21 @@ class BlockNorm(_Operator):
         """The gradients ``d_<name>`` of every tensor given, from those of ``residual'`` and ``normed`` (either may be None).
 
         ``out``: a dict of tensors to write some of them to."""
-        given = dict(residual=residual, branch=branch, gate=gate, post=post, post_bias=post_bias, pre=pre, pre_bias=pre_bias)
-        arg, shapes = self._in(given)
-        grads, result = BlockNormGrads(), {}
-        for name, t in given.items():
-            if t is not None:
-                d = (out or {}).get("d_" + name)
-                if d is None:
-                    d = self._empty(*shapes[name])
-                result["d_" + name] = d
-                setattr(grads, name, self._mat(d, shapes[name], "d_" + name))
-        r = None if d_residual is None else self._mat(d_residual, shapes["residual"], "d_residual")
-        n = None if d_normed is None else self._mat(d_normed, shapes["residual"], "d_normed")
-        evg._check(lib().evg_blocknorm_backward(self._h, arg, r, n, grads))
+        token, gates, vector, arg = self._in(residual, branch, gate, post, post_bias, pre, pre_bias)
+        grads, result = [], {}
+        for name, t, shape in (("d_residual", residual, token), ("d_branch", branch, token), ("d_gate", gate, gates), ("d_post", post, vector),
+                               ("d_post_bias", post_bias, vector), ("d_pre", pre, vector), ("d_pre_bias", pre_bias, vector)):
+            if t is None:
+                grads += _ABSENT
+                continue
+            d = out.get(name) if out else None
+            if d is None:
+                d = self._empty(shape)
+            result[name] = d
+            grads += self._at(d, shape, name)
+        r = None if d_residual is None else self._mat(d_residual, token, "d_residual")
+        n = None if d_normed is None else self._mat(d_normed, token, "d_normed")
+        evg._check(lib().evg_blocknorm_backward(self._h, arg, r, n, _GRADS(*grads)))
         return result
 
 
@@ -275,8 +292,8 @@ class GatedFFN(_Operator):
         """``y``; with ``save``, ``(y, saved)``, the latter for ``backward``."""
         rows = self._rows(x, self.width, "x")
         if out is None:
-            out = self._empty(*x.shape)
-        saved = self._empty(lib().evg_ffn_saved_bytes(self._h, rows), dtype=torch.uint8) if save else None
+            out = self._empty(x.shape)
+        saved = self._empty(lib().evg_ffn_saved_bytes(self._h, rows), torch.uint8) if save else None
         evg._check(lib().evg_ffn_forward(self._h, rows, self._mat(x, x.shape, "x"), *self._weights(w_gate, w_up, w_down),
                                          self._mat(out, x.shape, "out"), saved.data_ptr() if save else None))
         return (out, saved) if save else out
@@ -290,8 +307,8 @@ class GatedFFN(_Operator):
             raise ValueError(f"saved must be the {need} bytes that forward(save=True) returned")
         weights = self._weights(w_gate, w_up, w_down)
         if dx is None and input_gradient:
-            dx = self._empty(*x.shape)
-        grads = [self._empty(*w.shape) if d is None else d for d, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down))]
+            dx = self._empty(x.shape)
+        grads = [self._empty(w.shape) if d is None else d for d, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down))]
         evg._check(lib().evg_ffn_backward(
             self._h, rows, self._mat(dy, x.shape, "dy"), self._mat(x, x.shape, "x"), *weights, saved.data_ptr() or None,
             None if dx is None else self._mat(dx, x.shape, "dx"),

@@ -87,7 +87,7 @@ def test_ffn_refuses(nn, change):
 
 def test_null_handles(nn):
     l = nn.lib()
-    m, i, g = nn.Mat(), nn.BlockNormIn(), nn.BlockNormGrads()
+    m, i, g = C.byref(nn.Mat()), C.byref(nn.BlockNormIn()), C.byref(nn.BlockNormGrads())
     assert l.evg_clip_run(None, None, None, 1.0, 1.0, None) == 1
     assert l.evg_blocknorm_forward(None, i, m, m) == 1 and l.evg_blocknorm_backward(None, i, m, m, g) == 1
     assert l.evg_ffn_forward(None, 1, m, m, m, m, m, None) == 1
