@@ -24,7 +24,49 @@ struct evg_ffn {
   uint32_t pitch = 0;      // hidden, padded to 64: columns beyond `hidden` are 0
   void* hidden = nullptr;  // h where nothing is saved: [workers][max_rows][pitch]
   void* grads = nullptr;   // dg and du: [workers][max_rows][2][pitch]
+  // Where a width is no whole number of 16-byte units: room for copies with rows that are (null: not needed).
+  uint32_t width_pitch = 0;
+  void *x = nullptr, *dy = nullptr, *w_gate = nullptr, *w_up = nullptr, *w_down = nullptr;
 };
+
+namespace evg {
+namespace {
+
+// One thread copies 16 bytes.  Reads need no alignment beyond their elements'.
+template <typename T>
+__global__ __launch_bounds__(256) void k_ffn_pack(PackArgs a) {
+  constexpr int E = 16 / sizeof(T);
+  const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= a.units) return;
+  uint32_t k = 0;
+  while (k + 1 < a.count && id >= a.one[k + 1].first) ++k;
+  const PackOne& o = a.one[k];
+  const uint32_t per = (o.cols + E - 1) / E, unit = (uint32_t)((id - o.first) % per);
+  const uint64_t line = (id - o.first) / per, w = line / o.rows, row = line % o.rows;
+  const T* from = (const T*)o.from.p + (int64_t)w * o.from.worker + (int64_t)row * o.from.ld + unit * E;
+  Pack<T, E> v;
+  const int n = (int)(o.cols - unit * E);
+  if (n >= E) {
+    v = *reinterpret_cast<const Pack<T, E>*>(from);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) v.v[i] = i < n ? from[i] : (T)0.f;
+  }
+  *reinterpret_cast<uint4*>((T*)o.to + line * o.pitch + unit * E) = __builtin_bit_cast(uint4, v);
+}
+
+}  // namespace
+
+hipError_t launch_pack(uint32_t type, const PackArgs& a, hipStream_t s) {
+  if (!a.units) return hipSuccess;
+  const uint64_t grid = (a.units + 255) / 256;
+  if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  if (type == EVG_F32) k_ffn_pack<float><<<(uint32_t)grid, 256, 0, s>>>(a);
+  else k_ffn_pack<half_t><<<(uint32_t)grid, 256, 0, s>>>(a);   // bits
+  return hipGetLastError();
+}
+
+}  // namespace evg
 
 namespace {
 
@@ -41,13 +83,34 @@ GemmOperand operand(const evg_mat& m, uint32_t workers, uint64_t rows, uint64_t 
   return {m.p, workers > 1 ? m.worker : 0, rows > 1 ? m.row : (int64_t)cols};
 }
 
-// The largest tile of which there are enough to occupy the chip.
-GemmTile choose_tile(GemmOp op, const GemmArgs& g, uint32_t n, uint32_t share, bool aligned, uint32_t type) {
+// The tile with the least time by a model of what was measured (warm, normal values, us; a step is 128 bytes of k of a tile):
+//   16 bits  256 x 256  one a CU, 1.29 a step, and 2.1 with all CUs busy, when the chip's power binds
+//            128 x 128  two a CU, 0.84 or 1.04 a step; 1.17 times the energy for the same product
+//             64 x 128  three a CU, 0.72 (two) or 1.0 a step; 1.5 times the energy
+//             32 x  64  k shared out to four wavefronts, one a CU: 0.7 for four steps, and 3.5 for their sums
+//   32 bits  the products bind a CU: 1.06 a step of 64 x 128, 1.1 for four of 32 x 64
+// Measured, bf16, 256 / 128 / 64:  8192 tokens 2048 x 8192 in all 2263 / 2882 / 3550;  1024 tokens 2048 x 8192, gated 65 / 71 / 84, down 165 / 95 / 92;
+// 2048 tokens 2048 x 2048, gated 51 / 39 / 52;  64 / 32 x 64:  512 tokens 1024 x 2816, down 26 / 12, input 54 / 21;  8 x 250 tokens 512 x 1344 (f16),
+// down 14 / 20;  f32, 1024 tokens 1024 x 4096, down 136 / 78, gated 136 / 191.
+// The gated backward product ends with as much reading and writing as products: tiles of 64 overlap it (1024 tokens 2048 x 8192 82 / 64 / 57) unless 256
+// x 256 fill the chip (8192 tokens 448 / 631 / 504).
+GemmTile choose_tile(GemmOp op, const GemmArgs& g, uint32_t n, bool aligned, uint32_t type) {
+  const bool wide = type == EVG_F32;
   if ((op == GEMM_GATED || op == GEMM_DOWN) && g.M <= kMostRows) return TILE_ROWS;
-  auto count = [&](uint64_t bm, uint64_t bn) { return ((g.M + bm - 1) / bm) * ((n + bn / share - 1) / (bn / share)) * g.workers * g.parts; };
-  if (aligned && type != EVG_F32 && count(256, 256) >= 200) return TILE_256;
-  if (count(128, 128) >= 256) return TILE_128;
-  return TILE_64;
+  const uint32_t share = op == GEMM_GATED ? 2 : 1;
+  auto count = [&](uint64_t bm, uint64_t bn) { return (double)(((g.M + bm - 1) / bm) * ((n + bn / share - 1) / (bn / share)) * g.workers * g.parts); };
+  const double c64 = count(64, 128), small = count(32, 64), steps = (double)(((uint64_t)g.K * (wide ? 4 : 2) + 127) / 128 * (op == GEMM_INPUT ? 2 : 1));
+  const double small_rounds = ceil(small / 256), t_small = wide ? small_rounds * (steps / 4 * 1.1 + 3.5) + 2 : 1.15 * small_rounds * (steps / 4 * 0.7 + 3.5) + 2;
+  auto rest = [](double c, double slots) { return c - floor(c / slots) * slots; };
+  const double r64 = rest(c64, 768);
+  const double t64 = wide ? steps * 1.06 * ceil(c64 / 256) + 1 : steps * fmax(floor(c64 / 768) + (r64 == 0 ? 0 : r64 <= 512 ? 0.72 : 1.0), 1.4 * 0.00103 * c64) + 1;
+  if (t_small < t64 && steps >= 4) return op != GEMM_GATED && small <= 64 ? TILE_SMALL_NARROW : TILE_SMALL;
+  if (wide || !aligned) return TILE_64;
+  const double c128 = count(128, 128), c256 = count(256, 256), r128 = rest(c128, 512);
+  if (op == GEMM_GATED_BWD) return c256 >= 256 ? TILE_256 : TILE_64;
+  const double t128 = steps * fmax(floor(c128 / 512) * 1.04 + (r128 == 0 ? 0 : r128 <= 256 ? 0.84 : 1.04), 1.17 * 0.00206 * c128) + 1;
+  const double t256 = steps * fmax(ceil(c256 / 256) * 1.29, 0.0082 * c256) + 1;
+  return t256 <= t128 && t256 <= t64 ? TILE_256 : t128 <= t64 ? TILE_128 : TILE_64;
 }
 
 hipError_t product(const evg_ffn* c, GemmOp op, bool aligned, GemmArgs& g) {
@@ -57,11 +120,33 @@ hipError_t product(const evg_ffn* c, GemmOp op, bool aligned, GemmArgs& g) {
                   c->cfg.activation == EVG_ACT_GELU};
   g.pitch = c->pitch;
   const bool padded = op == GEMM_GATED || op == GEMM_GATED_BWD;
-  const GemmTile tile = choose_tile(op, g, padded ? g.pitch : g.N, op == GEMM_GATED ? 2 : 1, aligned, c->cfg.type);
+  const GemmTile tile = choose_tile(op, g, padded ? g.pitch : g.N, aligned, c->cfg.type);
   if (c->cfg.type == EVG_F32) return launch_gemm<float>(op, tile, aligned, g, c->stream);
   if (c->cfg.type == EVG_F16) return launch_gemm<half_t>(op, tile, aligned, g, c->stream);
   return launch_gemm<bf16_t>(op, tile, aligned, g, c->stream);
 }
+
+// Collects the operands that need whole-unit copies.
+struct Packer {
+  const evg_ffn* c;
+  PackArgs a{};
+  explicit Packer(const evg_ffn* ctx) : c(ctx) { a.workers = ctx->cfg.workers; }
+  // The operand, or its copy to be: products read the latter by whole units.
+  GemmOperand take(const GemmOperand& o, void* room, uint32_t rows, uint32_t cols, uint32_t pitch) {
+    if (!room || whole_units(o, cols, type_bytes(c->cfg.type))) return o;
+    const uint32_t e = 16 / type_bytes(c->cfg.type);
+    a.one[a.count++] = {o, room, rows, cols, pitch, a.units};
+    a.units += (uint64_t)a.workers * rows * ((cols + e - 1) / e);
+    return {room, (int64_t)rows * pitch, (int64_t)pitch};
+  }
+  // Of an operand after take: by whole units?
+  bool whole(const GemmOperand& o, uint32_t cols) const {
+    for (uint32_t i = 0; i < a.count; ++i)
+      if (a.one[i].to == o.p) return true;
+    return whole_units(o, cols, type_bytes(c->cfg.type));
+  }
+  hipError_t launch() const { return launch_pack(c->cfg.type, a, c->stream); }
+};
 
 // What every call is handed: x, dy and y are rows x D, w_gate and w_up F x D, w_down D x F.
 struct Shape { uint32_t W, rows, D, F, type; };
@@ -96,7 +181,7 @@ evg_status evg_ffn_init(evg_ffn** out, const evg_ffn_config* cfg, void* hip_stre
   *out = nullptr;
   if (cfg->workers < 1 || cfg->workers > 65535) return fail(EVG_ERR_INVALID, "workers must be 1 .. 65535");
   if (cfg->width < 1 || cfg->width > (1u << 20) || cfg->hidden < 1 || cfg->hidden > (1u << 20)) return fail(EVG_ERR_INVALID, "width and hidden must be 1 .. 2^20");
-  if (cfg->max_rows > 0x7FFFFF00u) return fail(EVG_ERR_INVALID, "max_rows is out of range");
+  if (cfg->max_rows > 0x7FFF0000u) return fail(EVG_ERR_INVALID, "max_rows is out of range");
   evg_status st;
   if ((st = check_type(cfg->type, "type")) != EVG_OK) return st;
   if (cfg->activation > EVG_ACT_RELU) return fail(EVG_ERR_INVALID, "activation must be one of EVG_ACT_*");
@@ -110,10 +195,20 @@ evg_status evg_ffn_init(evg_ffn** out, const evg_ffn_config* cfg, void* hip_stre
     delete c;
     return fail(EVG_ERR_INVALID, "workers, max_rows and hidden together are out of range");
   }
-  hipError_t e = hipMalloc(&c->hidden, one ? one : 16);
-  if (e == hipSuccess && cfg->train) e = hipMalloc(&c->grads, one ? 2 * one : 16);
+  const uint32_t bytes = type_bytes(cfg->type), unit = 16 / bytes;
+  c->width_pitch = (cfg->width + 63) / 64 * 64;
+  const uint64_t tokens = (uint64_t)cfg->workers * cfg->max_rows * c->width_pitch * bytes, up = (uint64_t)cfg->workers * cfg->hidden * c->width_pitch * bytes,
+                 down = (uint64_t)cfg->workers * cfg->width * c->pitch * bytes;
+  const bool odd_width = cfg->width % unit, odd_hidden = cfg->hidden % unit, copies = cfg->max_rows > kMostRows;
+  struct { void** p; uint64_t bytes; bool need; } rooms[] = {
+      {&c->hidden, one, true}, {&c->grads, 2 * one, cfg->train != 0}, {&c->x, tokens, copies && odd_width}, {&c->dy, tokens, copies && odd_width && cfg->train},
+      {&c->w_gate, up, copies && odd_width}, {&c->w_up, up, copies && odd_width}, {&c->w_down, down, copies && odd_hidden}};
+  hipError_t e = hipSuccess;
+  for (auto& r : rooms)
+    if (r.need && e == hipSuccess) e = hipMalloc(r.p, r.bytes ? r.bytes : 16);
   if (e != hipSuccess) {
-    if (c->hidden) (void)hipFree(c->hidden);
+    for (auto& r : rooms)
+      if (*r.p) (void)hipFree(*r.p);
     delete c;
     return fail(e == hipErrorOutOfMemory ? EVG_ERR_OOM : EVG_ERR_HIP, "workspace: %s", hipGetErrorString(e));
   }
@@ -140,26 +235,33 @@ evg_status evg_ffn_forward(evg_ffn* c, uint32_t rows, const evg_mat* x, const ev
   const Span outs[] = {mat_span(y, s.W, rows, s.D, s.type, "y"), saved_span(c, saved, rows)};
   if ((st = check_apart(outs, 2, ins, 4)) != EVG_OK) return st;
   if (!rows) return EVG_OK;
-  const uint32_t e = type_bytes(s.type);
   const uint64_t proj = (uint64_t)s.W * proj_rows(rows) * 2 * c->pitch;
   const GemmOperand h{saved ? (char*)saved + proj * sizeof(float) : c->hidden, (int64_t)rows * c->pitch, (int64_t)c->pitch};
 
+  // Few tokens are multiplied straight from the tensors, whatever their alignment.
+  const bool copies = rows > kMostRows;
+  Packer p(c);
+  const GemmOperand X = p.take(operand(*x, s.W, rows, s.D), copies ? c->x : nullptr, rows, s.D, c->width_pitch);
+  const GemmOperand WG = p.take(operand(*w_gate, s.W, s.F, s.D), copies ? c->w_gate : nullptr, s.F, s.D, c->width_pitch);
+  const GemmOperand WU = p.take(operand(*w_up, s.W, s.F, s.D), copies ? c->w_up : nullptr, s.F, s.D, c->width_pitch);
+  const GemmOperand WD = p.take(operand(*w_down, s.W, s.D, s.F), copies ? c->w_down : nullptr, s.D, s.F, c->pitch);
+  HIP_TRY(p.launch());
   GemmArgs g{};
-  g.a[0] = operand(*x, s.W, rows, s.D);
-  g.b[0] = operand(*w_gate, s.W, s.F, s.D);
-  g.b[1] = operand(*w_up, s.W, s.F, s.D);
+  g.a[0] = X;
+  g.b[0] = WG;
+  g.b[1] = WU;
   g.c[0] = h;
   g.M = rows, g.N = s.F, g.K = s.D, g.parts = 1;
   g.proj = (float*)saved;
   g.proj_worker = proj_rows(rows) * 2 * c->pitch;
-  HIP_TRY(product(c, GEMM_GATED, whole_units(g.a[0], s.D, e) && whole_units(g.b[0], s.D, e) && whole_units(g.b[1], s.D, e), g));
+  HIP_TRY(product(c, GEMM_GATED, p.whole(X, s.D) && p.whole(WG, s.D) && p.whole(WU, s.D), g));
 
   g = GemmArgs{};
   g.a[0] = h;
-  g.b[0] = operand(*w_down, s.W, s.D, s.F);
+  g.b[0] = WD;
   g.c[0] = operand(*y, s.W, rows, s.D);
   g.M = rows, g.N = s.D, g.K = s.F, g.parts = 1;
-  HIP_TRY(product(c, GEMM_DOWN, whole_units(g.b[0], s.F, e), g));
+  HIP_TRY(product(c, GEMM_DOWN, p.whole(WD, s.F), g));
   return EVG_OK;
 }
 
@@ -191,24 +293,35 @@ evg_status evg_ffn_backward(evg_ffn* c, uint32_t rows, const evg_mat* dy, const 
   const int64_t two = 2 * (int64_t)c->pitch;
   const GemmOperand h{(const char*)saved + proj * sizeof(float), (int64_t)rows * c->pitch, (int64_t)c->pitch};
   const GemmOperand dg{c->grads, (int64_t)rows * two, two}, du{(const char*)c->grads + (uint64_t)c->pitch * e, (int64_t)rows * two, two};
-  const GemmOperand X = operand(*x, s.W, rows, s.D), DY = operand(*dy, s.W, rows, s.D);
+  // Few tokens: copies of the weights would cost more than reading them element by element where they are cut.
+  const bool copies = rows > kMostRows, up = has[0] || has[1] || has[2];
+  Packer p(c);
+  auto take = [&](bool need, const GemmOperand& o, void* room, uint32_t r, uint32_t cols, uint32_t pitch) { return p.take(o, need && copies ? room : nullptr, r, cols, pitch); };
+  const GemmOperand X = take(has[1] || has[2], operand(*x, s.W, rows, s.D), c->x, rows, s.D, c->width_pitch);
+  const GemmOperand DY = take(true, operand(*dy, s.W, rows, s.D), c->dy, rows, s.D, c->width_pitch);
+  const GemmOperand WD = take(up, operand(*w_down, s.W, s.D, s.F), c->w_down, s.D, s.F, c->pitch);
+  HIP_TRY(p.launch());
   GemmArgs g{};
-  if (rows && (has[0] || has[1] || has[2])) {
+  if (rows && up) {
     g.a[0] = DY;
-    g.b[0] = operand(*w_down, s.W, s.D, s.F);
+    g.b[0] = WD;
     g.c[0] = dg;
     g.M = rows, g.N = s.F, g.K = s.D, g.parts = 1;
     g.proj = (float*)saved;
     g.proj_worker = proj_rows(rows) * 2 * c->pitch;
-    HIP_TRY(product(c, GEMM_GATED_BWD, whole_units(g.a[0], s.D, e) && whole_units(g.b[0], s.F, e), g));
+    HIP_TRY(product(c, GEMM_GATED_BWD, p.whole(DY, s.D) && p.whole(WD, s.F), g));
   }
   if (rows && has[0]) {
+    Packer pw(c);
+    const GemmOperand WG = pw.take(operand(*w_gate, s.W, s.F, s.D), copies ? c->w_gate : nullptr, s.F, s.D, c->width_pitch);
+    const GemmOperand WU = pw.take(operand(*w_up, s.W, s.F, s.D), copies ? c->w_up : nullptr, s.F, s.D, c->width_pitch);
+    HIP_TRY(pw.launch());
     g = GemmArgs{};
     g.a[0] = dg, g.a[1] = du;
-    g.b[0] = operand(*w_gate, s.W, s.F, s.D), g.b[1] = operand(*w_up, s.W, s.F, s.D);
+    g.b[0] = WG, g.b[1] = WU;
     g.c[0] = operand(*dx, s.W, rows, s.D);
     g.M = rows, g.N = s.D, g.K = s.F, g.parts = 1;
-    HIP_TRY(product(c, GEMM_INPUT, whole_units(g.b[0], s.D, e) && whole_units(g.b[1], s.D, e), g));
+    HIP_TRY(product(c, GEMM_INPUT, pw.whole(WG, s.D) && pw.whole(WU, s.D), g));
   }
   if (has[1] || has[2]) {
     g = GemmArgs{};
@@ -217,7 +330,7 @@ evg_status evg_ffn_backward(evg_ffn* c, uint32_t rows, const evg_mat* dy, const 
     if (has[2]) { g.a[n] = du; g.c[n++] = operand(*dw_up, s.W, s.F, s.D); }
     g.b[0] = X;
     g.M = s.F, g.N = s.D, g.K = rows, g.parts = n;
-    HIP_TRY(product(c, GEMM_WEIGHT, whole_units(X, s.D, e), g));
+    HIP_TRY(product(c, GEMM_WEIGHT, p.whole(X, s.D), g));
   }
   if (has[3]) {
     g = GemmArgs{};
@@ -225,7 +338,7 @@ evg_status evg_ffn_backward(evg_ffn* c, uint32_t rows, const evg_mat* dy, const 
     g.b[0] = h;
     g.c[0] = operand(*dw_down, s.W, s.D, s.F);
     g.M = s.D, g.N = s.F, g.K = rows, g.parts = 1;
-    HIP_TRY(product(c, GEMM_WEIGHT, whole_units(DY, s.D, e), g));
+    HIP_TRY(product(c, GEMM_WEIGHT, p.whole(DY, s.D), g));
   }
   return EVG_OK;
 }
@@ -233,7 +346,7 @@ evg_status evg_ffn_backward(evg_ffn* c, uint32_t rows, const evg_mat* dy, const 
 evg_status evg_ffn_destroy(evg_ffn* c) {
   if (!c) return EVG_OK;
   hipError_t e = hipStreamSynchronize(c->stream);
-  for (void* p : {c->hidden, c->grads})
+  for (void* p : {c->hidden, c->grads, c->x, c->dy, c->w_gate, c->w_up, c->w_down})
     if (p) { const hipError_t f = hipFree(p); if (e == hipSuccess) e = f; }
   delete c;
   HIP_TRY(e);

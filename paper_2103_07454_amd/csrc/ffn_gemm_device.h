@@ -77,9 +77,10 @@ struct Tile {
   // The unit that lies at a place, as (row, unit of the row).
   static __device__ __forceinline__ int swizzle(int row) {
     if constexpr (KC) return row & 7;
-    else if constexpr (sizeof(T) == 4) return (row >> 2 & 1) << 3;
+    else if constexpr (sizeof(T) == 4) return BD >= 64 ? (row >> 2 & 1) << 3 : 0;
     else if constexpr (BD >= 128) return ((row & 3) | (row >> 3 & 1) << 2) << 1;
-    else return ((row >> 1 & 1) | (row >> 3 & 1) << 1) << 1;
+    else if constexpr (BD == 64) return ((row >> 1 & 1) | (row >> 3 & 1) << 1) << 1;
+    else return (row >> 3 & 1) << 1;
   }
 };
 
@@ -132,9 +133,10 @@ struct Loader {
     base = (const char*)((const T*)o.p + (int64_t)w * o.worker + (KC ? (int64_t)lead * o.ld : (int64_t)lead));
     // Rows are whole units where they are loaded as such: the caller's by the rule for that variant, the library's own by their padding.
     const uint64_t last = KC ? (uint64_t)(dim - 1 - lead) * o.ld + (K + E - 1) / E * E : (uint64_t)(K - 1) * o.ld + ((dim + E - 1) / E * E - lead);
-    left = last * sizeof(T);
+    // A tile may lie wholly in the padding behind the last column: it loads nothing.
+    room = lead < dim ? dim - lead : 0;
+    left = room ? last * sizeof(T) : 0;
     stride = (KC ? (uint64_t)BK : (uint64_t)BK * o.ld) * sizeof(T);
-    room = dim - lead;
     const int place = wave * N * 64 + lane, row = place / L::kPerRow, unit = (place % L::kPerRow) ^ L::swizzle(row);
     if constexpr (KC) { d = PAIRED ? (row >> 6) * 32 + (row & 31) : row; k = unit * E; }
     else { d = unit * E; k = row; }
@@ -183,6 +185,11 @@ struct Loader {
     }
     base += stride;
     left -= min(left, stride);
+  }
+
+  __device__ __forceinline__ void skip(uint32_t steps) {
+    base += steps * stride;
+    left -= min(left, steps * stride);
   }
 
   __device__ __forceinline__ void put(u32x4* lds, const u32x4* held, int wave, int lane) const {
@@ -460,16 +467,13 @@ hipError_t launch_op(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) {
   const uint64_t grid = (uint64_t)g.tiles_m * g.tiles_n * g.workers * g.parts;
   if (!grid) return hipSuccess;
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
-  if (aligned) {
-    if constexpr (sizeof(T) == 2) {
-      if (tile == TILE_256) { k_ffn_gemm<T, OP, ERF, 256, 256, 2, 4, true><<<(uint32_t)grid, 512, 0, s>>>(g); return hipGetLastError(); }
-    }
-    if (tile == TILE_128) k_ffn_gemm<T, OP, ERF, 128, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
-    else k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
-  } else {
-    if (tile == TILE_128) k_ffn_gemm<T, OP, ERF, 128, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
-    else k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
+  if constexpr (sizeof(T) == 2) {
+    if (aligned && tile == TILE_256) { k_ffn_gemm<T, OP, ERF, 256, 256, 2, 4, true><<<(uint32_t)grid, 512, 0, s>>>(g); return hipGetLastError(); }
+    if (aligned && tile == TILE_128) { k_ffn_gemm<T, OP, ERF, 128, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g); return hipGetLastError(); }
   }
+  if (tile != TILE_64) return hipErrorInvalidValue;
+  if (aligned) k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
+  else k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
   return hipGetLastError();
 }
 

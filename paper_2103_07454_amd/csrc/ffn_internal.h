@@ -37,9 +37,24 @@ struct GemmArgs {
   uint32_t pitch;                  // padded hidden width
 };
 
-// Tile shapes.
-enum GemmTile : uint32_t { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_ROWS = 3 };   // TILE_ROWS: GEMM_GATED and GEMM_DOWN of at most kMostRows tokens
+// Tiles: 256 x 256 and 128 x 128 (aligned operands of 16 bits), 64 x 128; few tokens (GEMM_GATED and GEMM_DOWN of at most kMostRows); 32 x 64
+// and 32 x 32 with k shared out among the wavefronts.
+enum GemmTile : uint32_t { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_ROWS = 3, TILE_SMALL = 4, TILE_SMALL_NARROW = 5 };
 constexpr uint32_t kMostRows = 64;
+
+// Copies of operands whose rows are no whole 16-byte units, with rows of `pitch` elements that are: zeros up to the next unit.
+struct PackOne {
+  GemmOperand from;
+  void* to;            // [workers][rows][pitch]
+  uint32_t rows, cols, pitch;
+  uint64_t first;      // units of the operands ahead of it
+};
+struct PackArgs {
+  PackOne one[4];
+  uint32_t count, workers;
+  uint64_t units;
+};
+hipError_t launch_pack(uint32_t type, const PackArgs& a, hipStream_t s);
 
 template <typename T> hipError_t launch_gemm(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g, hipStream_t s);
 

@@ -4,7 +4,7 @@
 // turn, and their sums meet in LDS in a fixed order.  Nothing goes through LDS on the way in: no weight is used twice, and the tokens come
 // from the L2.  Bound by memory: what counts is how many loads are under way, so each wavefront asks for up to four steps at once.
 #pragma once
-#include "ffn_gemm_device.h"
+#include "ffn_small_device.h"
 
 namespace evg {
 
@@ -170,6 +170,17 @@ hipError_t launch_any(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g,
     if (op == GEMM_DOWN) return launch_rows<T, GEMM_DOWN, false>(g, s);
     if (op != GEMM_GATED) return hipErrorInvalidValue;
     return erf ? launch_rows<T, GEMM_GATED, true>(g, s) : launch_rows<T, GEMM_GATED, false>(g, s);
+  }
+  if (tile == TILE_SMALL || tile == TILE_SMALL_NARROW) {
+    const bool narrow = tile == TILE_SMALL_NARROW;
+    switch (op) {
+      case GEMM_GATED: return erf ? launch_small<T, GEMM_GATED, true>(narrow, aligned, g, s) : launch_small<T, GEMM_GATED, false>(narrow, aligned, g, s);
+      case GEMM_GATED_BWD: return erf ? launch_small<T, GEMM_GATED_BWD, true>(narrow, aligned, g, s) : launch_small<T, GEMM_GATED_BWD, false>(narrow, aligned, g, s);
+      case GEMM_DOWN: return launch_small<T, GEMM_DOWN, false>(narrow, aligned, g, s);
+      case GEMM_INPUT: return launch_small<T, GEMM_INPUT, false>(narrow, aligned, g, s);
+      case GEMM_WEIGHT: return launch_small<T, GEMM_WEIGHT, false>(narrow, aligned, g, s);
+      default: return hipErrorInvalidValue;
+    }
   }
   switch (op) {
     case GEMM_GATED: return erf ? launch_op<T, GEMM_GATED, true>(tile, aligned, g, s) : launch_op<T, GEMM_GATED, false>(tile, aligned, g, s);

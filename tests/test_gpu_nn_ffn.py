@@ -49,7 +49,9 @@ def train(nn, t, dtype, kind, **kw):
 NAMES = ("y", "dx", "dw_gate", "dw_up", "dw_down")
 # one token, lengths around the tiles' 64, 128 and 256, widths and hidden widths around a unit's 8, a step's 64 and a tile's edge
 SIZES = [(1, 1, 64, 64), (1, 1, 1, 1), (1, 2, 8, 8), (2, 3, 7, 5), (1, 63, 64, 65), (1, 64, 72, 128), (1, 65, 120, 136), (3, 129, 96, 63),
-         (1, 257, 200, 257), (2, 16, 264, 520), (1, 17, 130, 66), (1, 40, 512, 72), (5, 33, 40, 24)]
+         (1, 257, 200, 257), (2, 16, 264, 520), (1, 17, 130, 66), (1, 40, 512, 72), (5, 33, 40, 24),
+         # long sums over few tiles, odd widths of more tokens than go straight from the tensors, padding of more than a small tile
+         (1, 70, 1000, 96), (2, 70, 65, 33), (1, 300, 130, 263), (1, 90, 520, 1032), (2, 100, 7, 1030), (4, 100, 784, 203)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=SHORT.get)
@@ -69,10 +71,11 @@ def test_activations(nn, dtype, kind):
     check(kind, dtype, t, got, NAMES)
 
 
-@pytest.mark.parametrize("dtype", TYPES, ids=SHORT.get)
-def test_large_tiles(nn, dtype):
-    """Sizes at which the largest tiles are chosen for every product, with edges inside them."""
-    t = tensors(1, 2100, 2056, 2312, dtype, seed=2)
+@pytest.mark.parametrize("dtype,size", [(d, (1, 2100, 2056, 2312)) for d in TYPES] + [(d, s) for d in TYPES[:2] for s in ((1, 2600, 2560, 2600), (1, 3208, 3200, 3210))],
+                         ids=lambda v: SHORT.get(v, str(v)) if isinstance(v, torch.dtype) else str(v))
+def test_large_tiles(nn, dtype, size):
+    """Sizes at which the larger tiles are chosen, for every product, with edges inside them."""
+    t = tensors(*size, dtype, seed=2)
     _, got = train(nn, t, dtype, "silu")
     check("silu", dtype, t, got, NAMES, device="cuda")
 
