@@ -30,6 +30,25 @@ __device__ __forceinline__ void store_n(T* p, const float* v) {
   *reinterpret_cast<Pack<T, N>*>(p) = r;
 }
 
+// Non-temporal: what is not read again soon should not push out what is.
+template <int N, typename T>
+__device__ __forceinline__ void load_n_once(const T* p, float* v) {
+  typedef uint32_t words __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T))));
+  const words w = __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
+  const Pack<T, N> r = __builtin_bit_cast(Pack<T, N>, w);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = to_f(r.v[i]);
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void store_n_once(T* p, const float* v) {
+  typedef uint32_t words __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T))));
+  Pack<T, N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.v[i] = from_f<T>(v[i]);
+  __builtin_nontemporal_store(__builtin_bit_cast(words, r), reinterpret_cast<words*>(p));
+}
+
 // The first n of N elements (n may be <= 0 or >= N); the others are 0.
 template <int N, typename T>
 __device__ __forceinline__ void load_upto(const T* p, int n, float* v) {
