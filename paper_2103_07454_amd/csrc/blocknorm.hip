@@ -177,7 +177,6 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_blocknorm_forward(Nor
 
 // A thread's part of a row as it lies in memory, in whole registers (two 16-bit elements to each).
 template <typename T, int NV> struct Raw { uint32_t w[NV][kV * sizeof(T) / 4]; };
-template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Words { uint32_t w[kV * sizeof(T) / 4]; };
 
 template <typename T>
 __device__ __forceinline__ float element(const uint32_t* w, int i) {
@@ -186,16 +185,18 @@ __device__ __forceinline__ float element(const uint32_t* w, int i) {
   else return (float)__builtin_bit_cast(half_t, (uint16_t)(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu));
 }
 
-// WHOLE: the width is a multiple of 8, so a lane has 8 elements or none.
-template <bool WHOLE, int NV, int TPR, typename T>
+// WHOLE: the width is a multiple of 8, so a lane has 8 elements or none.  ONCE: they go past the caches.
+template <bool WHOLE, int NV, int TPR, bool ONCE = false, typename T>
 __device__ __forceinline__ void load_raw(const T* p, int width, int lane, Raw<T, NV>& r) {
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * TPR + lane) * kV;
     if (WHOLE || width >= kV) {
-      const Words<T> x = *reinterpret_cast<const Words<T>*>(p + (c + kV <= width ? c : 0));
+      typedef uint32_t words __attribute__((ext_vector_type(kV * sizeof(T) / 4), aligned(sizeof(T))));
+      const words* from = reinterpret_cast<const words*>(p + (c + kV <= width ? c : 0));
+      const words x = ONCE ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
-      for (int i = 0; i < (int)(kV * sizeof(T) / 4); ++i) r.w[k][i] = x.w[i];
+      for (int i = 0; i < (int)(kV * sizeof(T) / 4); ++i) r.w[k][i] = x[i];
     }
     if (!WHOLE && width % kV && c < width && c + kV > width) {
       T e[kV];
@@ -222,13 +223,13 @@ __device__ __forceinline__ void unpack(Raw<T, NV>& r, int width, int lane, Row<N
     for (int i = 0; i < kV; ++i) x.v[k * kV + i] = (k * TPR + lane) * kV < width ? element<T>(r.w[k], i) : 0.f;
 }
 
-template <bool WHOLE, int NV, int TPR, typename T>
+template <bool WHOLE, int NV, int TPR, bool ONCE = false, typename T>
 __device__ __forceinline__ void put_row(T* p, int width, int lane, const Row<NV>& r) {
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * TPR + lane) * kV;
     if (WHOLE) {
-      if (c < width) store_n<kV>(p + c, r.v + k * kV);
+      if (c < width) { if (ONCE) store_n_once<kV>(p + c, r.v + k * kV); else store_n<kV>(p + c, r.v + k * kV); }
     } else {
       store_upto<kV>(p + c, width - c, r.v + k * kV);
     }
@@ -278,14 +279,24 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
   Lines<T> o_r(g.d.residual, w, t0), o_b(g.d.branch, w, t0);
   uint32_t gate_row = gated ? t0 / g.in.gate_rows : 0, until = gated ? (uint32_t)min((uint64_t)g.in.rows, (uint64_t)(gate_row + 1) * g.in.gate_rows) : 0;
   const float alpha = g.alpha, beta = g.beta, inv_width = g.inv_width;
+  // The next row's residual and branch, which its first sums need, are on their way while a row is finished (16 bits: there are registers for them).
+  constexpr bool AHEAD = sizeof(T) == 2 && NV == 1;
+  Raw<T, NV> n_r, n_b;
+  auto ask = [&]() {
+    load_raw<WHOLE, NV, TPR, true>(l_r.p, width, lane, n_r);
+    if (branch) load_raw<WHOLE, NV, TPR, true>(l_b.p, width, lane, n_b);
+    l_r.next(), l_b.next();
+  };
+  if (AHEAD && t0 < t1) ask();
   for (uint32_t t = t0; t < t1; ++t) {
     Raw<T, NV> c_r, c_b, c_gate, c_dn, c_do;
-    load_raw<WHOLE, NV, TPR>(l_r.p, width, lane, c_r);
-    if (branch) load_raw<WHOLE, NV, TPR>(l_b.p, width, lane, c_b);
+    if (!AHEAD) ask();
+    c_r = n_r, c_b = n_b;
     if (gated) load_raw<WHOLE, NV, TPR>(at<const T>(g.in.gate, w, gate_row), width, lane, c_gate);
-    if (pre) load_raw<WHOLE, NV, TPR>(l_dn.p, width, lane, c_dn);
-    if (direct) load_raw<WHOLE, NV, TPR>(l_do.p, width, lane, c_do);
-    l_r.next(), l_b.next(), l_dn.next(), l_do.next();
+    if (pre) load_raw<WHOLE, NV, TPR, true>(l_dn.p, width, lane, c_dn);
+    if (direct) load_raw<WHOLE, NV, TPR, true>(l_do.p, width, lane, c_do);
+    if (AHEAD && t + 1 < t1) ask();
+    l_dn.next(), l_do.next();
     Row<NV> r, b, k, d;
     float inv_b = 1.f;
     // after the block: the unit row stays in b, and is scaled where it is needed
@@ -361,7 +372,7 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
     if (o_r.p) {
 #pragma unroll
       for (int i = 0; i < N; ++i) k.v[i] = alpha * d.v[i];
-      put_row<WHOLE, NV, TPR>(o_r.p, width, lane, k);
+      put_row<WHOLE, NV, TPR, true>(o_r.p, width, lane, k);
       o_r.next();
     }
     if (!branch) continue;
@@ -400,7 +411,7 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
       for (int i = 0; i < N; ++i) d.v[i] = (d.v[i] - sp - b.v[i] * pb) * inv_b;
     }
     if (o_b.p) {
-      put_row<WHOLE, NV, TPR>(o_b.p, width, lane, d);
+      put_row<WHOLE, NV, TPR, true>(o_b.p, width, lane, d);
       o_b.next();
     }
   }
