@@ -32,34 +32,37 @@ struct evg_ffn {
 namespace evg {
 namespace {
 
-// One thread copies 16 bytes.  Reads need no alignment beyond their elements'.
+// A wavefront copies a row, 16 bytes to a lane.  Reads need no alignment beyond their elements'.
 template <typename T>
 __global__ __launch_bounds__(256) void k_ffn_pack(PackArgs a) {
   constexpr int E = 16 / sizeof(T);
-  const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= a.units) return;
+  const uint64_t id = (uint64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (id >= a.lines) return;
   uint32_t k = 0;
   while (k + 1 < a.count && id >= a.one[k + 1].first) ++k;
   const PackOne& o = a.one[k];
-  const uint32_t per = (o.cols + E - 1) / E, unit = (uint32_t)((id - o.first) % per);
-  const uint64_t line = (id - o.first) / per, w = line / o.rows, row = line % o.rows;
-  const T* from = (const T*)o.from.p + (int64_t)w * o.from.worker + (int64_t)row * o.from.ld + unit * E;
-  Pack<T, E> v;
-  const int n = (int)(o.cols - unit * E);
-  if (n >= E) {
-    v = *reinterpret_cast<const Pack<T, E>*>(from);
-  } else {
+  const uint64_t line = id - o.first;
+  const T* from = (const T*)o.from.p + (int64_t)(line / o.rows) * o.from.worker + (int64_t)(line % o.rows) * o.from.ld;
+  T* to = (T*)o.to + line * o.pitch;
+#pragma unroll 4
+  for (uint32_t c = (threadIdx.x & 63) * E; c < o.cols; c += 64 * E) {
+    Pack<T, E> v;
+    const int n = (int)(o.cols - c);
+    if (n >= E) {
+      v = *reinterpret_cast<const Pack<T, E>*>(from + c);
+    } else {
 #pragma unroll
-    for (int i = 0; i < E; ++i) v.v[i] = i < n ? from[i] : (T)0.f;
+      for (int i = 0; i < E; ++i) v.v[i] = i < n ? from[c + i] : (T)0.f;
+    }
+    *reinterpret_cast<uint4*>(to + c) = __builtin_bit_cast(uint4, v);
   }
-  *reinterpret_cast<uint4*>((T*)o.to + line * o.pitch + unit * E) = __builtin_bit_cast(uint4, v);
 }
 
 }  // namespace
 
 hipError_t launch_pack(uint32_t type, const PackArgs& a, hipStream_t s) {
-  if (!a.units) return hipSuccess;
-  const uint64_t grid = (a.units + 255) / 256;
+  if (!a.lines) return hipSuccess;
+  const uint64_t grid = (a.lines + 3) / 4;
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
   if (type == EVG_F32) k_ffn_pack<float><<<(uint32_t)grid, 256, 0, s>>>(a);
   else k_ffn_pack<half_t><<<(uint32_t)grid, 256, 0, s>>>(a);   // bits
@@ -86,28 +89,28 @@ GemmOperand operand(const evg_mat& m, uint32_t workers, uint64_t rows, uint64_t 
 // The tile with the least time by a model of what was measured (warm, normal values, us; a step is 128 bytes of k of a tile):
 //   16 bits  256 x 256  one a CU, 1.29 a step, and 2.1 with all CUs busy, when the chip's power binds
 //            128 x 128  two a CU, 0.84 or 1.04 a step; 1.17 times the energy for the same product
-//             64 x 128  three a CU, 0.72 (two) or 1.0 a step; 1.5 times the energy
+//             64 x 128  three a CU, 0.66, 0.72 or 1.0 a step; 1.5 times the energy
 //             32 x  64  k shared out to four wavefronts, one a CU: 0.7 for four steps, and 3.5 for their sums
 //   32 bits  the products bind a CU: 1.06 a step of 64 x 128, 1.1 for four of 32 x 64
-// Measured, bf16, 256 / 128 / 64:  8192 tokens 2048 x 8192 in all 2263 / 2882 / 3550;  1024 tokens 2048 x 8192, gated 65 / 71 / 84, down 165 / 95 / 92;
+// Measured, bf16, 256 / 128 / 64:  8192 tokens 2048 x 8192 in all 2259 / 2657 / 3499;  1024 tokens 2048 x 8192, gated 65 / 71 / 84, down 165 / 95 / 92;
 // 2048 tokens 2048 x 2048, gated 51 / 39 / 52;  64 / 32 x 64:  512 tokens 1024 x 2816, down 26 / 12, input 54 / 21;  8 x 250 tokens 512 x 1344 (f16),
 // down 14 / 20;  f32, 1024 tokens 1024 x 4096, down 136 / 78, gated 136 / 191.
-// The gated backward product ends with as much reading and writing as products: tiles of 64 overlap it (1024 tokens 2048 x 8192 82 / 64 / 57) unless 256
-// x 256 fill the chip (8192 tokens 448 / 631 / 504).
+// The gated backward product ends with as much reading and writing as products, which another workgroup's products on the CU overlap: 1024 tokens 2048
+// x 8192 76 / 48 / 60, 8192 tokens 433 / 410 / 431; where 128 x 128 are few, 2048 tokens 2048 x 2048, 67 / 35 / 32.
 GemmTile choose_tile(GemmOp op, const GemmArgs& g, uint32_t n, bool aligned, uint32_t type) {
   const bool wide = type == EVG_F32;
   if ((op == GEMM_GATED || op == GEMM_DOWN) && g.M <= kMostRows) return TILE_ROWS;
   const uint32_t share = op == GEMM_GATED ? 2 : 1;
   auto count = [&](uint64_t bm, uint64_t bn) { return (double)(((g.M + bm - 1) / bm) * ((n + bn / share - 1) / (bn / share)) * g.workers * g.parts); };
   const double c64 = count(64, 128), small = count(32, 64), steps = (double)(((uint64_t)g.K * (wide ? 4 : 2) + 127) / 128 * (op == GEMM_INPUT ? 2 : 1));
-  const double small_rounds = ceil(small / 256), t_small = wide ? small_rounds * (steps / 4 * 1.1 + 3.5) + 2 : 1.15 * small_rounds * (steps / 4 * 0.7 + 3.5) + 2;
+  const double small_rounds = ceil(small / 256), t_small = wide ? small_rounds * (steps / 4 * 1.1 + 3.5) + 2 : 1.35 * small_rounds * (steps / 4 * 0.7 + 3.5) + 2;
   auto rest = [](double c, double slots) { return c - floor(c / slots) * slots; };
   const double r64 = rest(c64, 768);
-  const double t64 = wide ? steps * 1.06 * ceil(c64 / 256) + 1 : steps * fmax(floor(c64 / 768) + (r64 == 0 ? 0 : r64 <= 512 ? 0.72 : 1.0), 1.4 * 0.00103 * c64) + 1;
+  const double t64 = wide ? steps * 1.06 * ceil(c64 / 256) + 1 : steps * fmax(floor(c64 / 768) + (r64 == 0 ? 0 : r64 <= 256 ? 0.66 : r64 <= 512 ? 0.72 : 1.0), 1.4 * 0.00103 * c64) + 1;
   if (t_small < t64 && steps >= 4) return op != GEMM_GATED && small <= 64 ? TILE_SMALL_NARROW : TILE_SMALL;
   if (wide || !aligned) return TILE_64;
   const double c128 = count(128, 128), c256 = count(256, 256), r128 = rest(c128, 512);
-  if (op == GEMM_GATED_BWD) return c256 >= 256 ? TILE_256 : TILE_64;
+  if (op == GEMM_GATED_BWD) return c128 > 384 ? TILE_128 : TILE_64;
   const double t128 = steps * fmax(floor(c128 / 512) * 1.04 + (r128 == 0 ? 0 : r128 <= 256 ? 0.84 : 1.04), 1.17 * 0.00206 * c128) + 1;
   const double t256 = steps * fmax(ceil(c256 / 256) * 1.29, 0.0082 * c256) + 1;
   return t256 <= t128 && t256 <= t64 ? TILE_256 : t128 <= t64 ? TILE_128 : TILE_64;
@@ -130,13 +133,12 @@ hipError_t product(const evg_ffn* c, GemmOp op, bool aligned, GemmArgs& g) {
 struct Packer {
   const evg_ffn* c;
   PackArgs a{};
-  explicit Packer(const evg_ffn* ctx) : c(ctx) { a.workers = ctx->cfg.workers; }
+  explicit Packer(const evg_ffn* ctx) : c(ctx) {}
   // The operand, or its copy to be: products read the latter by whole units.
   GemmOperand take(const GemmOperand& o, void* room, uint32_t rows, uint32_t cols, uint32_t pitch) {
     if (!room || whole_units(o, cols, type_bytes(c->cfg.type))) return o;
-    const uint32_t e = 16 / type_bytes(c->cfg.type);
-    a.one[a.count++] = {o, room, rows, cols, pitch, a.units};
-    a.units += (uint64_t)a.workers * rows * ((cols + e - 1) / e);
+    a.one[a.count++] = {o, room, rows, cols, pitch, a.lines};
+    a.lines += (uint64_t)c->cfg.workers * rows;
     return {room, (int64_t)rows * pitch, (int64_t)pitch};
   }
   // Of an operand after take: by whole units?

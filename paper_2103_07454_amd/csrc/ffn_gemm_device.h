@@ -58,12 +58,10 @@ __device__ __forceinline__ void activate(const Activation& f, float x, float& a,
     const float e = 1.f + (FAST ? __expf(-z) : expf(-z));   // infinite for z below -88: s is 0 then
     const float s = FAST ? __builtin_amdgcn_rcpf(e) : 1.f / e;
     const float t = s * (1.f - s);
-    a = x * s;
-    slope = t > 0.f ? fmaf(x * dz, t, s) : s;               // far out x dz may be infinite
-    if (f.relu) {
-      a = x > 0.f ? x : x <= 0.f ? 0.f : x;
-      slope = x > 0.f ? 1.f : x <= 0.f ? 0.f : x;
-    }
+    // Selected, not branched to: branches in the midst of an epilogue cost it a hundred registers.
+    const bool off = x <= 0.f;
+    a = f.relu ? (off ? 0.f : x) : x * s;
+    slope = f.relu ? (off ? 0.f : x > 0.f ? 1.f : x) : t > 0.f ? fmaf(x * dz, t, s) : s;   // far out x dz may be infinite
   }
 }
 
@@ -218,7 +216,7 @@ __device__ __forceinline__ void wait_and_meet() {
 }
 
 template <typename T, int OP, bool ERF, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
-__global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void k_ffn_gemm(GemmArgs g) {
+__global__ __launch_bounds__(WAVES_M * WAVES_N * 64, BM == 64 ? 3 : 2) void k_ffn_gemm(GemmArgs g) {
   constexpr bool AKC = OP != GEMM_WEIGHT, BKC = OP == GEMM_GATED || OP == GEMM_DOWN;
   constexpr int WAVES = WAVES_M * WAVES_N, WM = BM / WAVES_M, TM = WM / 32, WN = BN / WAVES_N, TN = WN / 32;
   static_assert(WN % 64 == 0 && WM % 32 == 0, "a wavefront has pairs of accumulators side by side");
@@ -414,35 +412,34 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void k_ffn_gemm(GemmArgs g) 
         }
       leave(Cols{}, c, rows0, first, g.pitch, [&](int j, int q) { return h[j][q]; });
     } else if constexpr (OP == GEMM_GATED_BWD) {
-      // The projections of 32 rows at once, all asked for before the first is used; what lies beyond the tensors reads its last block's.
+      // The projections of 32 x 32 at once, all asked for before the first is used; what lies beyond the tensors reads its last block's.
       const uint32_t first = n0 + wn;
-      f32x4 gate[TN][4], up[TN][4];
+      Pack<T, 4> dg[TN][4], du[TN][4];
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
+        f32x4 gate[4], up[4];
         const float* p = proj_at(g, w, rows0, min(first + j * 32, g.pitch - 32), 0, lane);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          gate[j][q] = *(const f32x4*)(p + q * 256);
-          up[j][q] = *(const f32x4*)(p + 1024 + q * 256);
+          gate[q] = *(const f32x4*)(p + q * 256);
+          up[q] = *(const f32x4*)(p + 1024 + q * 256);
         }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      Pack<T, 4> dg[TN][4], du[TN][4];
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const uint32_t n = first + j * 32 + 8 * q + 4 * (lane >> 5);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float a, slope;
-            activate<ERF, sizeof(T) == 2>(g.activation, gate[j][q][e], a, slope);
+            activate<ERF, sizeof(T) == 2>(g.activation, gate[q][e], a, slope);
             const float d = acc[i][j][q * 4 + e];
             const bool real = n + e < g.N;
-            dg[j][q].v[e] = from_f<T>(real ? d * up[j][q][e] * slope : 0.f);
+            dg[j][q].v[e] = from_f<T>(real ? d * up[q][e] * slope : 0.f);
             du[j][q].v[e] = from_f<T>(real ? d * a : 0.f);
           }
+          __builtin_amdgcn_sched_barrier(0);   // four at a time: more would take the registers of a second workgroup
         }
+      }
       leave(Cols{}, c, rows0, first, g.pitch, [&](int j, int q) { return dg[j][q]; });
       leave(Cols{}, c + g.pitch, rows0, first, g.pitch, [&](int j, int q) { return du[j][q]; });
     } else {
@@ -468,7 +465,9 @@ hipError_t launch_op(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) {
   if (!grid) return hipSuccess;
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
   if constexpr (sizeof(T) == 2) {
-    if (aligned && tile == TILE_256) { k_ffn_gemm<T, OP, ERF, 256, 256, 2, 4, true><<<(uint32_t)grid, 512, 0, s>>>(g); return hipGetLastError(); }
+    if constexpr (OP != GEMM_GATED_BWD) {   // which overlaps its reading and writing with a second workgroup's products
+      if (aligned && tile == TILE_256) { k_ffn_gemm<T, OP, ERF, 256, 256, 2, 4, true><<<(uint32_t)grid, 512, 0, s>>>(g); return hipGetLastError(); }
+    }
     if (aligned && tile == TILE_128) { k_ffn_gemm<T, OP, ERF, 128, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g); return hipGetLastError(); }
   }
   if (tile != TILE_64) return hipErrorInvalidValue;

@@ -47,12 +47,12 @@ struct PackOne {
   GemmOperand from;
   void* to;            // [workers][rows][pitch]
   uint32_t rows, cols, pitch;
-  uint64_t first;      // units of the operands ahead of it
+  uint64_t first;      // rows of the operands ahead of it
 };
 struct PackArgs {
   PackOne one[4];
-  uint32_t count, workers;
-  uint64_t units;
+  uint32_t count;
+  uint64_t lines;
 };
 hipError_t launch_pack(uint32_t type, const PackArgs& a, hipStream_t s);
 

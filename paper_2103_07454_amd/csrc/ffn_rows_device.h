@@ -20,21 +20,25 @@ __device__ __forceinline__ f32x4 mfma16(const Frag<float>& a, const Frag<float>&
   return c;
 }
 
-template <typename T, int OP, bool ERF, int G, int kRowWaves>
+// EIGHT: at most 8 tokens and 8 columns.  The matrix instruction's other 8 rows and columns take the second half of a step's k for the same
+// ones, so each of its 16 x 16 corners on the diagonal is half of the sum: twice the workgroups, each lane's load a byte of a weight that no
+// other has, and 128 bytes of a row in one load (one token through 2048 x 5632: 10.2 and 6.0 us instead of 12.2 and 8.1).
+template <typename T, int OP, bool ERF, int G, int kRowWaves, bool EIGHT>
 __global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
-  constexpr int E = 16 / sizeof(T), STEP = 128 / sizeof(T), B = OP == GEMM_GATED ? 2 : 1;
-  constexpr int AHEAD = G == 1 ? 4 : 2;
+  static_assert(!EIGHT || G == 1, "");
+  constexpr int E = 16 / sizeof(T), STEP = 128 / sizeof(T), B = OP == GEMM_GATED ? 2 : 1, HALVES = EIGHT ? 1 : 2, COLS = EIGHT ? 8 : 16;
+  constexpr int AHEAD = EIGHT ? (B == 2 ? 4 : 6) : G == 1 ? 4 : 2;
   __shared__ f32x4 sums[kRowWaves][B * G][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t groups = g.tiles_n, w = blockIdx.x / groups, n0 = blockIdx.x % groups * 16;
-  const int row = lane & 15, quarter = lane >> 4;
+  const uint32_t groups = g.tiles_n, w = blockIdx.x / groups, n0 = blockIdx.x % groups * COLS;
+  const int row = lane & (COLS - 1), quarter = lane >> 4, within = quarter * E + (EIGHT ? (lane >> 3 & 1) * (STEP / 2) : 0);   // of a step's k
   // A fragment's lane has 16 bytes of one row.  Rows that there are not read the last one's, and what comes of them is not stored.
   const T* wp[B];
 #pragma unroll
-  for (int b = 0; b < B; ++b) wp[b] = (const T*)g.b[b].p + (int64_t)w * g.b[b].worker + (int64_t)min(n0 + row, g.N - 1) * g.b[b].ld + quarter * E;
+  for (int b = 0; b < B; ++b) wp[b] = (const T*)g.b[b].p + (int64_t)w * g.b[b].worker + (int64_t)min(n0 + row, g.N - 1) * g.b[b].ld + within;
   const T* xp[G];
 #pragma unroll
-  for (int i = 0; i < G; ++i) xp[i] = (const T*)g.a[0].p + (int64_t)w * g.a[0].worker + (int64_t)min(i * 16u + row, g.M - 1) * g.a[0].ld + quarter * E;
+  for (int i = 0; i < G; ++i) xp[i] = (const T*)g.a[0].p + (int64_t)w * g.a[0].worker + (int64_t)min(i * 16u + row, g.M - 1) * g.a[0].ld + within;
   f32x4 acc[B][G];
 #pragma unroll
   for (int b = 0; b < B; ++b)
@@ -49,12 +53,12 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
   const uint32_t whole = g.K / STEP;   // steps
   auto run = [&](uint32_t step, auto count) {   // `count` steps of this wavefront from `step` on
     constexpr int C = decltype(count)::value;
-    Frag<T> fw[C][2][B], fx[C][2][G];
+    Frag<T> fw[C][HALVES][B], fx[C][HALVES][G];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const uint32_t k = (step + c * kRowWaves) * STEP;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
+      for (int half = 0; half < HALVES; ++half) {
 #pragma unroll
         for (int b = 0; b < B; ++b) fw[c][half][b] = load(wp[b] + k + half * (STEP / 2));
 #pragma unroll
@@ -65,7 +69,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
+      for (int half = 0; half < HALVES; ++half)
 #pragma unroll
         for (int b = 0; b < B; ++b)
 #pragma unroll
@@ -73,6 +77,10 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
   };
   uint32_t step = wave;
   for (; step + (AHEAD - 1) * kRowWaves < whole; step += AHEAD * kRowWaves) run(step, std::integral_constant<int, AHEAD>{});
+  if (AHEAD > 4 && step + 3 * kRowWaves < whole) {
+    run(step, std::integral_constant<int, 4>{});
+    step += 4 * kRowWaves;
+  }
   if (AHEAD > 2 && step + kRowWaves < whole) {
     run(step, std::integral_constant<int, 2>{});
     step += 2 * kRowWaves;
@@ -83,9 +91,9 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
   }
   if (step == whole && g.K % STEP) {   // what is left of k: 16 bytes that reach beyond it are read element by element
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
+    for (int half = 0; half < HALVES; ++half) {
       const uint32_t k = whole * STEP + half * (STEP / 2);
-      const int left = (int)(g.K - k) - quarter * E;
+      const int left = (int)(g.K - k) - within;
       auto some = [&](const T* p) {
         Frag<T> f;
         f.v = u32x4{0, 0, 0, 0};
@@ -115,13 +123,17 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
 #pragma unroll
     for (int i = 0; i < G; ++i) sums[wave][b * G + i][lane] = acc[b][i];
   __syncthreads();
-  if (wave >= G) return;
+  if (wave >= G || (EIGHT && (lane & 40))) return;
   f32x4 v[B];
 #pragma unroll
   for (int b = 0; b < B; ++b) {
     v[b] = sums[0][b * G + wave][lane];
+    if (EIGHT) v[b] += sums[0][b * G + wave][lane + 40];   // the other corner: 8 rows and 8 columns on
 #pragma unroll
-    for (int s = 1; s < kRowWaves; ++s) v[b] += sums[s][b * G + wave][lane];
+    for (int s = 1; s < kRowWaves; ++s) {
+      v[b] += sums[s][b * G + wave][lane];
+      if (EIGHT) v[b] += sums[s][b * G + wave][lane + 40];
+    }
   }
   // A lane has four neighbouring columns of one token.
   const uint32_t m = wave * 16 + row, n = n0 + quarter * 4;
@@ -152,13 +164,16 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
 
 template <typename T, int OP, bool ERF>
 hipError_t launch_rows(GemmArgs g, hipStream_t s) {
-  g.tiles_n = ((OP == GEMM_GATED ? g.pitch : g.N) + 15) / 16;
+  const bool eight = g.M <= 8;
+  const uint32_t cols = eight ? 8 : 16;
+  g.tiles_n = ((OP == GEMM_GATED ? g.pitch : g.N) + cols - 1) / cols;
   const uint64_t grid = (uint64_t)g.tiles_n * g.workers;
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
-  constexpr int waves = OP == GEMM_GATED ? 8 : 16;   // 16 columns of gate and of up, or of one product: as many loads
-  if (g.M <= 16) k_ffn_rows<T, OP, ERF, 1, waves><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
-  else if (g.M <= 32) k_ffn_rows<T, OP, ERF, 2, waves><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
-  else k_ffn_rows<T, OP, ERF, 4, waves><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
+  constexpr int waves = OP == GEMM_GATED ? 8 : 16;   // columns of gate and of up, or of one product: as many loads
+  if (eight) k_ffn_rows<T, OP, ERF, 1, waves, true><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
+  else if (g.M <= 16) k_ffn_rows<T, OP, ERF, 1, waves, false><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
+  else if (g.M <= 32) k_ffn_rows<T, OP, ERF, 2, waves, false><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
+  else k_ffn_rows<T, OP, ERF, 4, waves, false><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
   return hipGetLastError();
 }
 

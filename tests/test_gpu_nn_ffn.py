@@ -51,7 +51,7 @@ NAMES = ("y", "dx", "dw_gate", "dw_up", "dw_down")
 SIZES = [(1, 1, 64, 64), (1, 1, 1, 1), (1, 2, 8, 8), (2, 3, 7, 5), (1, 63, 64, 65), (1, 64, 72, 128), (1, 65, 120, 136), (3, 129, 96, 63),
          (1, 257, 200, 257), (2, 16, 264, 520), (1, 17, 130, 66), (1, 40, 512, 72), (5, 33, 40, 24),
          # long sums over few tiles, odd widths of more tokens than go straight from the tensors, padding of more than a small tile
-         (1, 70, 1000, 96), (2, 70, 65, 33), (1, 300, 130, 263), (1, 90, 520, 1032), (2, 100, 7, 1030), (4, 100, 784, 203)]
+         (1, 8, 1000, 520), (3, 9, 263, 1000), (1, 4, 2500, 3001), (1, 70, 1000, 96), (2, 70, 65, 33), (1, 300, 130, 263), (1, 90, 520, 1032), (2, 100, 7, 1030), (4, 100, 784, 203)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=SHORT.get)
