@@ -153,12 +153,19 @@ struct Packer {
 // What every call is handed: x, dy and y are rows x D, w_gate and w_up F x D, w_down D x F.
 struct Shape { uint32_t W, rows, D, F, type; };
 
+// As check_mat, and rows near enough for 31 bits.
+evg_status check_operand(const evg_mat* m, const Shape& s, uint64_t rows, uint64_t cols, bool written, const char* what) {
+  const evg_status st = check_mat(m, s.W, rows, cols, s.type, written, what);
+  if (st == EVG_OK && rows > 1 && m->row > 0x7FFFFFFF) return fail(EVG_ERR_INVALID, "%s: rows more than 2^31 elements apart", what);
+  return st;
+}
+
 evg_status check_weights(const Shape& s, const evg_mat* x, const evg_mat* w_gate, const evg_mat* w_up, const evg_mat* w_down) {
   evg_status st;
-  if ((st = check_mat(x, s.W, s.rows, s.D, s.type, false, "x")) != EVG_OK) return st;
-  if ((st = check_mat(w_gate, s.W, s.F, s.D, s.type, false, "w_gate")) != EVG_OK) return st;
-  if ((st = check_mat(w_up, s.W, s.F, s.D, s.type, false, "w_up")) != EVG_OK) return st;
-  return check_mat(w_down, s.W, s.D, s.F, s.type, false, "w_down");
+  if ((st = check_operand(x, s, s.rows, s.D, false, "x")) != EVG_OK) return st;
+  if ((st = check_operand(w_gate, s, s.F, s.D, false, "w_gate")) != EVG_OK) return st;
+  if ((st = check_operand(w_up, s, s.F, s.D, false, "w_up")) != EVG_OK) return st;
+  return check_operand(w_down, s, s.D, s.F, false, "w_down");
 }
 
 evg_status check_saved(const evg_ffn* c, const void* saved, uint32_t rows) {
@@ -230,7 +237,7 @@ evg_status evg_ffn_forward(evg_ffn* c, uint32_t rows, const evg_mat* x, const ev
   if (rows > c->cfg.max_rows) return fail(EVG_ERR_INVALID, "rows exceeds the context's max_rows");
   evg_status st;
   if ((st = check_weights(s, x, w_gate, w_up, w_down)) != EVG_OK) return st;
-  if ((st = check_mat(y, s.W, rows, s.D, s.type, true, "y")) != EVG_OK) return st;
+  if ((st = check_operand(y, s, rows, s.D, true, "y")) != EVG_OK) return st;
   if (saved && (st = check_saved(c, saved, rows)) != EVG_OK) return st;
   const Span ins[] = {mat_span(x, s.W, rows, s.D, s.type, "x"), mat_span(w_gate, s.W, s.F, s.D, s.type, "w_gate"),
                       mat_span(w_up, s.W, s.F, s.D, s.type, "w_up"), mat_span(w_down, s.W, s.D, s.F, s.type, "w_down")};
@@ -277,13 +284,13 @@ evg_status evg_ffn_backward(evg_ffn* c, uint32_t rows, const evg_mat* dy, const 
   if (!saved && rows) return fail(EVG_ERR_INVALID, "saved must be given");
   evg_status st;
   if ((st = check_weights(s, x, w_gate, w_up, w_down)) != EVG_OK) return st;
-  if ((st = check_mat(dy, s.W, rows, s.D, s.type, false, "dy")) != EVG_OK) return st;
+  if ((st = check_operand(dy, s, rows, s.D, false, "dy")) != EVG_OK) return st;
   if ((st = check_saved(c, saved, rows)) != EVG_OK) return st;
   const bool has[4] = {dx && dx->p, dw_gate && dw_gate->p, dw_up && dw_up->p, dw_down && dw_down->p};
-  if (has[0] && (st = check_mat(dx, s.W, rows, s.D, s.type, true, "dx")) != EVG_OK) return st;
-  if (has[1] && (st = check_mat(dw_gate, s.W, s.F, s.D, s.type, true, "dw_gate")) != EVG_OK) return st;
-  if (has[2] && (st = check_mat(dw_up, s.W, s.F, s.D, s.type, true, "dw_up")) != EVG_OK) return st;
-  if (has[3] && (st = check_mat(dw_down, s.W, s.D, s.F, s.type, true, "dw_down")) != EVG_OK) return st;
+  if (has[0] && (st = check_operand(dx, s, rows, s.D, true, "dx")) != EVG_OK) return st;
+  if (has[1] && (st = check_operand(dw_gate, s, s.F, s.D, true, "dw_gate")) != EVG_OK) return st;
+  if (has[2] && (st = check_operand(dw_up, s, s.F, s.D, true, "dw_up")) != EVG_OK) return st;
+  if (has[3] && (st = check_operand(dw_down, s, s.D, s.F, true, "dw_down")) != EVG_OK) return st;
   const Span ins[] = {mat_span(x, s.W, rows, s.D, s.type, "x"), mat_span(w_gate, s.W, s.F, s.D, s.type, "w_gate"),
                       mat_span(w_up, s.W, s.F, s.D, s.type, "w_up"), mat_span(w_down, s.W, s.D, s.F, s.type, "w_down"),
                       mat_span(dy, s.W, rows, s.D, s.type, "dy"), saved_span(c, saved, rows)};

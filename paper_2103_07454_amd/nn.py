@@ -126,6 +126,11 @@ class _Operator:
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype or self.dtype, device=self.device)
 
+    def _like(self, t):
+        if t.is_contiguous() and torch._C._cuda_getCurrentRawStream(self._index) == self._raw:
+            return torch.empty_like(t)
+        return self._empty(t.shape)
+
     def _at(self, t, shape, what):
         """Address and strides of a tensor of the given shape, [workers, rows, columns] or [workers, columns]."""
         if t.dtype is not self.dtype or t.get_device() != self._index:
@@ -236,9 +241,9 @@ class BlockNorm(_Operator):
         token, _, _, arg = self._in(residual, branch, gate, post, post_bias, pre, pre_bias)
         same = branch is None and self._keeps and residual_out is None    # residual' is the residual
         if not same and residual_out is None:
-            residual_out = self._empty(token)
+            residual_out = self._like(residual)
         if normed is None and pre is not None:
-            normed = self._empty(token)
+            normed = self._like(residual)
         out = None if same else self._mat(residual_out, token, "residual_out")
         n = None if normed is None else self._mat(normed, token, "normed")
         if out is not None or n is not None:
@@ -259,7 +264,7 @@ class BlockNorm(_Operator):
                 continue
             d = out.get(name) if out else None
             if d is None:
-                d = self._empty(shape)
+                d = self._like(t)
             result[name] = d
             grads += self._at(d, shape, name)
         r = None if d_residual is None else self._mat(d_residual, token, "d_residual")
@@ -292,7 +297,7 @@ class GatedFFN(_Operator):
         """``y``; with ``save``, ``(y, saved)``, the latter for ``backward``."""
         rows = self._rows(x, self.width, "x")
         if out is None:
-            out = self._empty(x.shape)
+            out = self._like(x)
         saved = self._empty(lib().evg_ffn_saved_bytes(self._h, rows), torch.uint8) if save else None
         evg._check(lib().evg_ffn_forward(self._h, rows, self._mat(x, x.shape, "x"), *self._weights(w_gate, w_up, w_down),
                                          self._mat(out, x.shape, "out"), saved.data_ptr() if save else None))
@@ -307,8 +312,8 @@ class GatedFFN(_Operator):
             raise ValueError(f"saved must be the {need} bytes that forward(save=True) returned")
         weights = self._weights(w_gate, w_up, w_down)
         if dx is None and input_gradient:
-            dx = self._empty(x.shape)
-        grads = [self._empty(w.shape) if d is None else d for d, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down))]
+            dx = self._like(x)
+        grads = [self._like(w) if d is None else d for d, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down))]
         evg._check(lib().evg_ffn_backward(
             self._h, rows, self._mat(dy, x.shape, "dy"), self._mat(x, x.shape, "x"), *weights, saved.data_ptr() or None,
             None if dx is None else self._mat(dx, x.shape, "dx"),

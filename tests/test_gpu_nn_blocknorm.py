@@ -185,6 +185,32 @@ def test_what_is_not_finite_stays_in_its_row(nn):
     assert torch.isfinite(d["d_residual"][0, ok]).all() and torch.isfinite(d["d_branch"][0, ok]).all()
 
 
+def test_offsets_beyond_32_bits(nn):
+    T, D = 1_100_001, 2048
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    make = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    t = dict(residual=make(1, T, D), branch=make(1, T, D), pre=make(1, D), post=make(1, D))
+    d_out, d_normed = make(1, T, D), make(1, T, D)
+    op = nn.BlockNorm(D, max_rows=T, eps=EPS)
+    given = {k: v for k, v in t.items() if k != "residual"}
+    r, n = op.forward(t["residual"], **given)
+    d = op.backward(d_out, d_normed, t["residual"], **given)
+    ends = torch.cat([torch.arange(40), torch.arange(T - 300, T)]).cuda()
+    v = {k: (x[0, ends] if x.dim() == 3 else x[0]).cpu().double() for k, x in t.items()}
+    v.update(d_out=d_out[0, ends].cpu().double(), d_normed=d_normed[0, ends].cpu().double())
+    want, size = ref.blocknorm("rms", v, eps=EPS, alpha=1.0, beta=1.0, gate_rows=1)
+    for name, g in (("residual", r), ("normed", n), ("d_residual", d["d_residual"]), ("d_branch", d["d_branch"])):
+        off = (g[0, ends].cpu().double() - want[name]).abs()
+        assert bool((off <= limits(want[name], size[name], 0, torch.bfloat16)).all()), name
+    total = torch.zeros(D, dtype=torch.float64, device="cuda")
+    for a in range(0, T, 100_000):
+        rr = t["residual"][0, a:a + 100_000].double() + ref.unit("rms", t["branch"][0, a:a + 100_000].double(), EPS)[0] * t["post"][0].double()
+        total += (d_normed[0, a:a + 100_000].double() * ref.unit("rms", rr, EPS)[0]).sum(0)
+    # independent terms of size 1: the bound of a sum over T rows, and the rounding
+    off = (d["d_pre"][0].double() - total).abs()
+    assert bool((off <= 128 * ref.U32 * T ** 0.5 * (1 + 4 * T ** 0.5) + ref.rounding(total, torch.bfloat16) * 1.001).all())
+
+
 def test_same_bits_every_time_and_in_a_graph(nn):
     t, d_out, d_normed = tensors(1, 3000, 520, torch.bfloat16, "rms", 1000, seed=6)
     stream = torch.cuda.Stream()

@@ -156,6 +156,36 @@ def test_what_is_not_finite_stays_with_its_token(nn, dtype):
     assert not torch.isfinite(got["y"][0][bad]).any() and torch.isnan(got["dw_gate"][0]).any()
 
 
+def test_offsets_beyond_32_bits(nn):
+    """Tokens whose elements lie beyond 2^31, and rows 2^25 elements apart."""
+    T, D, F = 1_100_001, 2048, 64
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    make = lambda *s, size=1.0: torch.empty(*s, dtype=torch.bfloat16, device="cuda").normal_(generator=gen).mul_(size)
+    t = dict(x=make(1, T, D), w_gate=make(1, F, D, size=D ** -0.5), w_up=make(1, F, D, size=D ** -0.5), w_down=make(1, D, F, size=F ** -0.5), dy=make(1, T, D))
+    _, got = train(nn, t, torch.bfloat16, "silu")
+    ends = torch.cat([torch.arange(40), torch.arange(T - 300, T)]).cuda()
+    some = {k: (v[:, ends] if k in ("x", "dy") else v) for k, v in t.items()}
+    check("silu", torch.bfloat16, some, dict(y=got["y"][:, ends], dx=got["dx"][:, ends]), ("y", "dx"), device="cuda")
+    want = {k: 0.0 for k in NAMES[2:]}
+    for a in range(0, T, 100_000):
+        v = {k: (x[0, a:a + 100_000] if k in ("x", "dy") else x[0]).double() for k, x in t.items()}
+        part = ref.ffn("silu", torch.bfloat16, v["x"], v["w_gate"], v["w_up"], v["w_down"], v["dy"])
+        want = {k: want[k] + part[k][0] for k in want}
+    for k in want:
+        # dg, du and h are rounded, then the sums: each at most a unit off, independently; a million additions in 32 bits stay far below
+        off = float((got[k][0].double() - want[k]).norm() / want[k].norm())
+        print(f"[ffn] {k} of {T} tokens: {off / ref.UNIT[torch.bfloat16]:.2f} units", flush=True)
+        assert off <= 4 * ref.UNIT[torch.bfloat16], k
+    del t, got, some
+    torch.cuda.empty_cache()
+    t = tensors(1, 70, 64, 96, torch.bfloat16, seed=12)
+    far = torch.empty(69 * 2 ** 25 + 64, dtype=torch.bfloat16, device="cuda")
+    x = far.as_strided((1, 70, 64), (far.numel(), 2 ** 25, 1))
+    x.copy_(t["x"])
+    op = nn.GatedFFN(64, 96, max_rows=70)
+    check("silu", torch.bfloat16, t, dict(y=op.forward(x, t["w_gate"], t["w_up"], t["w_down"])), ("y",))
+
+
 def test_same_bits_every_time_and_in_a_graph(nn):
     t = tensors(2, 130, 256, 320, torch.bfloat16, seed=8)
     stream = torch.cuda.Stream()
