@@ -66,27 +66,39 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float (*red)[2][TPR
 
 template <int NV> struct Row { float v[NV * kV]; };
 
-// Elements beyond the width are 0.  Every lane loads, those that have no whole 8 elements from the row's start, so that no branch
-// stands between one tensor's loads and the next one's; only a width that is no multiple of 8 has a lane read some elements singly.
+// Where a lane's 8 elements of a row of at least 8 begin, and how many of them belong to its neighbour: one that has fewer reads the row's
+// last 8, one that has none the first.  So every lane loads 16 bytes, without a branch between one tensor's loads and the next one's.
+struct Place { int at, skip; bool any; };
+__device__ __forceinline__ Place place_of(int c, int width) {
+  const bool any = c < width, whole = c + kV <= width;
+  return {whole ? c : any ? width - kV : 0, any && !whole ? c + kV - width : 0, any};
+}
+
+// Elements beyond the width are 0.
 template <int NV, int TPR, typename T>
 __device__ __forceinline__ void load_row(const T* p, int width, int lane, Row<NV>& r) {
   if (width >= kV) {
+    Place at[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (k * TPR + lane) * kV;
-      const bool whole = c + kV <= width;
-      load_n<kV>(p + (whole ? c : 0), r.v + k * kV);
-#pragma unroll
-      for (int i = 0; i < kV; ++i) r.v[k * kV + i] = whole ? r.v[k * kV + i] : 0.f;
+      at[k] = place_of((k * TPR + lane) * kV, width);
+      load_n<kV>(p + at[k].at, r.v + k * kV);
     }
-  }
-  if (width % kV) {
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (k * TPR + lane) * kV;
-      if (c < width && c + kV > width) load_upto<kV>(p + c, width - c, r.v + k * kV);
-      else if (width < kV) load_upto<kV>(p, 0, r.v + k * kV);
+      float* v = r.v + k * kV;
+      if (width % kV) {
+#pragma unroll
+        for (int s = 1; s < kV; s *= 2)
+#pragma unroll
+          for (int i = 0; i < kV; ++i) v[i] = at[k].skip & s ? (i + s < kV ? v[i + s] : 0.f) : v[i];
+      }
+#pragma unroll
+      for (int i = 0; i < kV; ++i) v[i] = at[k].any ? v[i] : 0.f;
     }
+  } else {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) load_upto<kV>(p, lane || k ? 0 : width, r.v + k * kV);
   }
 }
 
@@ -176,7 +188,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_blocknorm_forward(Nor
 }
 
 // A thread's part of a row as it lies in memory, in whole registers (two 16-bit elements to each).
-template <typename T, int NV> struct Raw { uint32_t w[NV][kV * sizeof(T) / 4]; };
+template <typename T, int NV> struct Raw { uint32_t w[NV][kV * sizeof(T) / 4]; int skip[NV]; };
 
 template <typename T>
 __device__ __forceinline__ float element(const uint32_t* w, int i) {
@@ -191,25 +203,28 @@ __device__ __forceinline__ void load_raw(const T* p, int width, int lane, Raw<T,
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * TPR + lane) * kV;
+    constexpr int N = kV * sizeof(T) / 4;
     if (WHOLE || width >= kV) {
-      typedef uint32_t words __attribute__((ext_vector_type(kV * sizeof(T) / 4), aligned(sizeof(T))));
-      const words* from = reinterpret_cast<const words*>(p + (c + kV <= width ? c : 0));
+      const Place at = place_of(c, width);
+      typedef uint32_t words __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+      const words* from = reinterpret_cast<const words*>(p + (WHOLE && !at.any ? 0 : at.at));
       const words x = ONCE ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
-      for (int i = 0; i < (int)(kV * sizeof(T) / 4); ++i) r.w[k][i] = x[i];
-    }
-    if (!WHOLE && width % kV && c < width && c + kV > width) {
+      for (int i = 0; i < N; ++i) r.w[k][i] = x[i];
+      if (!WHOLE) r.skip[k] = at.skip;
+    } else {
       T e[kV];
 #pragma unroll
       for (int i = 0; i < kV; ++i) e[i] = c + i < width ? p[c + i] : (T)0.f;
       __builtin_memcpy(r.w[k], e, sizeof e);
+      r.skip[k] = 0;
     }
   }
 }
 
 // As values; those beyond the width are 0.  The empty statement keeps the compiler from making them long before they are needed, which
 // would take twice the registers.
-template <int NV, int TPR, typename T>
+template <bool WHOLE, int NV, int TPR, typename T>
 __device__ __forceinline__ void unpack(Raw<T, NV>& r, int width, int lane, Row<NV>& x) {
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -221,6 +236,16 @@ __device__ __forceinline__ void unpack(Raw<T, NV>& r, int width, int lane, Row<N
   for (int k = 0; k < NV; ++k)
 #pragma unroll
     for (int i = 0; i < kV; ++i) x.v[k * kV + i] = (k * TPR + lane) * kV < width ? element<T>(r.w[k], i) : 0.f;
+  if constexpr (!WHOLE) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      float* v = x.v + k * kV;
+#pragma unroll
+      for (int s = 1; s < kV; s *= 2)
+#pragma unroll
+        for (int i = 0; i < kV; ++i) v[i] = r.skip[k] & s ? (i + s < kV ? v[i + s] : 0.f) : v[i];
+    }
+  }
 }
 
 template <bool WHOLE, int NV, int TPR, bool ONCE = false, typename T>
@@ -280,7 +305,7 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
   uint32_t gate_row = gated ? t0 / g.in.gate_rows : 0, until = gated ? (uint32_t)min((uint64_t)g.in.rows, (uint64_t)(gate_row + 1) * g.in.gate_rows) : 0;
   const float alpha = g.alpha, beta = g.beta, inv_width = g.inv_width;
   // The next row's residual and branch, which its first sums need, are on their way while a row is finished (16 bits: there are registers for them).
-  constexpr bool AHEAD = sizeof(T) == 2 && NV == 1;
+  constexpr bool AHEAD = NV == 1;
   Raw<T, NV> n_r, n_b;
   auto ask = [&]() {
     load_raw<WHOLE, NV, TPR, true>(l_r.p, width, lane, n_r);
@@ -303,39 +328,39 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
     auto after = [&](Row<NV>& a) {
       a = b;
       if (post) {
-        unpack<NV, TPR>(w_post, width, lane, a);
+        unpack<WHOLE, NV, TPR>(w_post, width, lane, a);
 #pragma unroll
         for (int i = 0; i < N; ++i) a.v[i] *= b.v[i];
         if (post_bias) {
           Row<NV> e;
-          unpack<NV, TPR>(w_postbias, width, lane, e);
+          unpack<WHOLE, NV, TPR>(w_postbias, width, lane, e);
 #pragma unroll
           for (int i = 0; i < N; ++i) a.v[i] += e.v[i];
         }
       }
     };
     if (branch) {
-      unpack<NV, TPR>(c_b, width, lane, b);
+      unpack<WHOLE, NV, TPR>(c_b, width, lane, b);
       if (post) inv_b = make_unit<NV, TPR, LAYER>(b, g, lane, red, turn);
       Row<NV> a;
       after(a);
       if (gated) {
-        unpack<NV, TPR>(c_gate, width, lane, k);
+        unpack<WHOLE, NV, TPR>(c_gate, width, lane, k);
 #pragma unroll
         for (int i = 0; i < N; ++i) a.v[i] *= k.v[i];
       }
-      unpack<NV, TPR>(c_r, width, lane, r);
+      unpack<WHOLE, NV, TPR>(c_r, width, lane, r);
 #pragma unroll
       for (int i = 0; i < N; ++i) r.v[i] = fmaf(alpha, r.v[i], beta * a.v[i]);
     } else {
-      unpack<NV, TPR>(c_r, width, lane, r);
+      unpack<WHOLE, NV, TPR>(c_r, width, lane, r);
 #pragma unroll
       for (int i = 0; i < N; ++i) r.v[i] *= alpha;
     }
     if (pre) {
       // with q = dn pre:  (q - mean(q) - r mean(q r) / s^2) / s of the centred row r, whose two sums go together
-      unpack<NV, TPR>(c_dn, width, lane, d);
-      unpack<NV, TPR>(w_pre, width, lane, k);
+      unpack<WHOLE, NV, TPR>(c_dn, width, lane, d);
+      unpack<WHOLE, NV, TPR>(w_pre, width, lane, k);
       float mean_q = 0.f;
       if constexpr (LAYER) {
         float sr = 0.f, sq = 0.f;
@@ -365,7 +390,7 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
       for (int i = 0; i < N; ++i) d.v[i] = 0.f;
     }
     if (direct) {
-      unpack<NV, TPR>(c_do, width, lane, k);
+      unpack<WHOLE, NV, TPR>(c_do, width, lane, k);
 #pragma unroll
       for (int i = 0; i < N; ++i) d.v[i] += k.v[i];
     }
@@ -382,7 +407,7 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
       after(k);
 #pragma unroll
       for (int i = 0; i < N; ++i) s_gate.v[i] = fmaf(d.v[i], k.v[i], s_gate.v[i]);
-      unpack<NV, TPR>(c_gate, width, lane, k);
+      unpack<WHOLE, NV, TPR>(c_gate, width, lane, k);
 #pragma unroll
       for (int i = 0; i < N; ++i) d.v[i] *= k.v[i];
       if (t + 1 == until && !g.group_stripes) {
@@ -394,7 +419,7 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
       }
     }
     if (post) {
-      unpack<NV, TPR>(w_post, width, lane, k);
+      unpack<WHOLE, NV, TPR>(w_post, width, lane, k);
       float pb = 0.f, sp = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
