@@ -24,8 +24,9 @@ extern "C" {
 enum { EVG_F32 = 0, EVG_F16 = 1, EVG_BF16 = 2 };
 
 /* A DEVICE tensor of `workers` matrices: element (w, i, j) at p + w * worker + i * row + j, in elements of its type.  The
- * last axis has stride 1.  Rows may be further apart than they are long, not closer (a tensor that is written: rows and
- * workers may not overlap).  p == NULL: absent.  Any alignment of p and any stride that its type allows. */
+ * last axis has stride 1.  Rows may be further apart than they are long.  Those of a tensor that is only read may also be
+ * closer, or one and the same (row or worker 0: broadcast); a written one's rows and workers may not overlap.  p == NULL:
+ * absent.  Any alignment of p and any stride that its type allows. */
 typedef struct {
   void* p;
   int64_t worker;

@@ -145,7 +145,7 @@ struct Loader {
           off[j] = ((d + j * kApart) * ld + k) * (uint32_t)sizeof(T);         // rows beyond the last one lie beyond `left`
         } else {
           const int r = row + j * kApart, c = (place % L::kPerRow ^ L::swizzle(r)) * E;
-          off[j] = (uint32_t)c < room ? (r * ld + c) * (uint32_t)sizeof(T) : kOut;   // and so do rows k
+          off[j] = (uint32_t)c < room ? (r * ld + c) * (uint32_t)sizeof(T) : kOut;
         }
       }
     }
@@ -156,10 +156,11 @@ struct Loader {
     if constexpr (ALIGNED) {
       const uint32_t bytes = (uint32_t)min(left, (uint64_t)0x7FFFFFF0u);
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)bytes, 0x00020000);
-      const uint32_t none = KC && (int)k >= k_left ? kOut : 0;   // rows k beyond the last one lie beyond `left`
 #pragma unroll
-      for (int j = 0; j < N; ++j)
+      for (int j = 0; j < N; ++j) {
+        const uint32_t none = (int)(KC ? k : k + j * kApart) >= k_left ? kOut : 0;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (wave * N + j) * 64), 16, (int)(off[j] | none), 0, 0, 0);
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < N; ++j) {
@@ -215,6 +216,12 @@ __device__ __forceinline__ void wait_and_meet() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// Workgroups go to the eight XCDs in turn.  Each XCD gets a contiguous part of the tiles' order, so that what they share lies in its own L2.
+__device__ __forceinline__ uint32_t place_by_xcd() {
+  const uint32_t x = blockIdx.x & 7, each = gridDim.x >> 3, more = gridDim.x & 7;
+  return x * each + min(x, more) + (blockIdx.x >> 3);
+}
+
 template <typename T, int OP, bool ERF, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, BM == 64 ? 3 : 2) void k_ffn_gemm(GemmArgs g) {
   constexpr bool AKC = OP != GEMM_WEIGHT, BKC = OP == GEMM_GATED || OP == GEMM_DOWN;
@@ -229,17 +236,12 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, BM == 64 ? 3 : 2) void k_ff
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Tiles in an order in which neighbours share operands: four rows of tiles, column by column, so that the 32 workgroups of an XCD read
   // four rows' and eight columns' operands at a time (up to 7 % less time for the products of 8192 x 2048 x 8192 than bands of eight
-  // rows, 20 % less than of sixteen).  Workgroups go to the eight XCDs in turn; each gets a contiguous part of the order, so that
-  // what it shares lies in its own L2.
+  // rows, 20 % less than of sixteen).
   const uint32_t tiles = g.tiles_m * g.tiles_n;
-  uint32_t id = blockIdx.x;
-  {
-    const uint32_t all = gridDim.x, x = id & 7, each = all >> 3, more = all & 7;
-    id = x * each + min(x, more) + (id >> 3);
-  }
+  uint32_t id = place_by_xcd();
   const uint32_t cell = id / tiles, part = cell % g.parts, w = cell / g.parts;
   id %= tiles;
-    constexpr uint32_t BAND = 4;
+  constexpr uint32_t BAND = 4;
   const uint32_t band = BAND * g.tiles_n, first = id / band * BAND, rows = min(BAND, g.tiles_m - first);
   const uint32_t tm = first + id % band % rows, tn = id % band / rows;
   const uint32_t m0 = tm * BM, n0 = tn * (OP == GEMM_GATED ? BN / 2 : BN);

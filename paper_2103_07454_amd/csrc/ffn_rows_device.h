@@ -21,8 +21,8 @@ __device__ __forceinline__ f32x4 mfma16(const Frag<float>& a, const Frag<float>&
 }
 
 // EIGHT: at most 8 tokens and 8 columns.  The matrix instruction's other 8 rows and columns take the second half of a step's k for the same
-// ones, so each of its 16 x 16 corners on the diagonal is half of the sum: twice the workgroups, each lane's load a byte of a weight that no
-// other has, and 128 bytes of a row in one load (one token through 2048 x 5632: 10.2 and 6.0 us instead of 12.2 and 8.1).
+// ones, so each of the two 8 x 8 blocks on the diagonal of its result is half of the sum: twice the workgroups, no weight loaded by two lanes,
+// and 128 bytes of a row in one load (one token through 2048 x 5632: 10.2 and 6.0 us instead of 12.2 and 8.1).
 template <typename T, int OP, bool ERF, int G, int kRowWaves, bool EIGHT>
 __global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
   static_assert(!EIGHT || G == 1, "");

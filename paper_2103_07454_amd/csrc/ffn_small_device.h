@@ -17,7 +17,7 @@ __global__ __launch_bounds__(kSplit * 64) void k_ffn_small(GemmArgs g) {
   __shared__ u32x4 lds0[kSplit][UNITS], lds1[kSplit][UNITS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t tiles = g.tiles_m * g.tiles_n;
-  const uint32_t cell = blockIdx.x / tiles, part = cell % g.parts, w = cell / g.parts, id = blockIdx.x % tiles;
+  const uint32_t place = place_by_xcd(), cell = place / tiles, part = cell % g.parts, w = cell / g.parts, id = place % tiles;
   const uint32_t m0 = id % g.tiles_m * 32, n0 = id / g.tiles_m * (OP == GEMM_GATED ? 32 : 32 * TN);
 
   Loader<T, 32, AKC, 1, ALIGNED, false> la;

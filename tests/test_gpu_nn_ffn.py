@@ -120,6 +120,22 @@ def test_workers_side_by_side(nn):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=SHORT.get)
+@pytest.mark.parametrize("size", [(2, 70, 72, 136), (1, 90, 65, 33), (1, 9, 64, 64)], ids=str)
+def test_broadcast_tokens(nn, dtype, size):
+    """One row of memory for all tokens, as a gradient of a sum over them has; rows that lie closer than they are long."""
+    W, T, D, F = size
+    t = tensors(*size, dtype, seed=13)
+    for k in ("x", "dy"):
+        t[k] = t[k][:, :1].expand(W, T, D)
+    _, got = train(nn, t, dtype, "silu")
+    check("silu", dtype, t, got, NAMES)
+    flat = torch.randn(W, 8 * T + D, generator=torch.Generator().manual_seed(14)).to(dtype).cuda()
+    t = dict(tensors(*size, dtype, seed=15), x=flat.as_strided((W, T, D), (flat.shape[1], 8, 1)))
+    _, got = train(nn, t, dtype, "silu")
+    check("silu", dtype, t, got, NAMES)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=SHORT.get)
 def test_no_tokens(nn, dtype):
     t = tensors(2, 0, 24, 40, dtype)
     _, got = train(nn, t, dtype, "silu")
