@@ -37,9 +37,9 @@ struct GemmArgs {
   uint32_t pitch;                  // padded hidden width
 };
 
-// Tiles: 256 x 256 and 128 x 128 (aligned operands of 16 bits), 64 x 128; few tokens (GEMM_GATED and GEMM_DOWN of at most kMostRows); 32 x 64
-// and 32 x 32 with k shared out among the wavefronts.
-enum GemmTile : uint32_t { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_ROWS = 3, TILE_SMALL = 4, TILE_SMALL_NARROW = 5 };
+// Tiles: 256 x 256 and 128 x 128 (aligned operands of 16 bits), 64 x 128; few tokens (GEMM_GATED and GEMM_DOWN of at most kMostRows); 32 x 64,
+// 32 x 32 and 64 x 64 (aligned) with k shared out among the wavefronts.
+enum GemmTile : uint32_t { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_ROWS = 3, TILE_SMALL = 4, TILE_SMALL_NARROW = 5, TILE_SMALL_SQUARE = 6 };
 constexpr uint32_t kMostRows = 64;
 
 // Copies of operands whose rows are no whole 16-byte units, with rows of `pitch` elements that are: zeros up to the next unit.

@@ -186,14 +186,13 @@ hipError_t launch_any(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g,
     if (op != GEMM_GATED) return hipErrorInvalidValue;
     return erf ? launch_rows<T, GEMM_GATED, true>(g, s) : launch_rows<T, GEMM_GATED, false>(g, s);
   }
-  if (tile == TILE_SMALL || tile == TILE_SMALL_NARROW) {
-    const bool narrow = tile == TILE_SMALL_NARROW;
+  if (tile == TILE_SMALL || tile == TILE_SMALL_NARROW || tile == TILE_SMALL_SQUARE) {
     switch (op) {
-      case GEMM_GATED: return erf ? launch_small<T, GEMM_GATED, true>(narrow, aligned, g, s) : launch_small<T, GEMM_GATED, false>(narrow, aligned, g, s);
-      case GEMM_GATED_BWD: return erf ? launch_small<T, GEMM_GATED_BWD, true>(narrow, aligned, g, s) : launch_small<T, GEMM_GATED_BWD, false>(narrow, aligned, g, s);
-      case GEMM_DOWN: return launch_small<T, GEMM_DOWN, false>(narrow, aligned, g, s);
-      case GEMM_INPUT: return launch_small<T, GEMM_INPUT, false>(narrow, aligned, g, s);
-      case GEMM_WEIGHT: return launch_small<T, GEMM_WEIGHT, false>(narrow, aligned, g, s);
+      case GEMM_GATED: return erf ? launch_small<T, GEMM_GATED, true>(tile, aligned, g, s) : launch_small<T, GEMM_GATED, false>(tile, aligned, g, s);
+      case GEMM_GATED_BWD: return erf ? launch_small<T, GEMM_GATED_BWD, true>(tile, aligned, g, s) : launch_small<T, GEMM_GATED_BWD, false>(tile, aligned, g, s);
+      case GEMM_DOWN: return launch_small<T, GEMM_DOWN, false>(tile, aligned, g, s);
+      case GEMM_INPUT: return launch_small<T, GEMM_INPUT, false>(tile, aligned, g, s);
+      case GEMM_WEIGHT: return launch_small<T, GEMM_WEIGHT, false>(tile, aligned, g, s);
       default: return hipErrorInvalidValue;
     }
   }

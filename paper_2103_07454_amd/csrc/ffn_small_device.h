@@ -1,26 +1,26 @@
 // The products where there are few tiles: small tiles, and k shared out among a workgroup's wavefronts.
 //
-// A workgroup has 32 rows and 32 TN columns; each of its four or eight wavefronts takes every fourth or eighth step of k through buffers of its
+// A workgroup has 32 TM rows and 32 TN columns; each of its four or eight wavefronts takes every fourth or eighth step of k through buffers of its
 // own, so none waits for another until their sums meet in LDS, in a fixed order.  Then four of them finish a quarter of the columns each.
 #pragma once
 #include "ffn_gemm_device.h"
 
 namespace evg {
 
-template <typename T, int OP, bool ERF, int TN, int kSplit, bool ALIGNED>
+template <typename T, int OP, bool ERF, int TM, int TN, int kSplit, bool ALIGNED>
 __global__ __launch_bounds__(kSplit * 64) void k_ffn_small(GemmArgs g) {
   constexpr bool AKC = OP != GEMM_WEIGHT, BKC = OP == GEMM_GATED || OP == GEMM_DOWN;
   static_assert(OP != GEMM_GATED || TN == 2, "gate's columns and up's");
-  using LA = Tile<T, 32, AKC>;
+  using LA = Tile<T, 32 * TM, AKC>;
   using LB = Tile<T, 32 * TN, BKC>;
   constexpr int UNITS = LA::kUnits + LB::kUnits, BK = LA::BK;
   __shared__ u32x4 lds0[kSplit][UNITS], lds1[kSplit][UNITS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t tiles = g.tiles_m * g.tiles_n;
   const uint32_t place = place_by_xcd(), cell = place / tiles, part = cell % g.parts, w = cell / g.parts, id = place % tiles;
-  const uint32_t m0 = id % g.tiles_m * 32, n0 = id / g.tiles_m * (OP == GEMM_GATED ? 32 : 32 * TN);
+  const uint32_t m0 = id % g.tiles_m * (32 * TM), n0 = id / g.tiles_m * (OP == GEMM_GATED ? 32 : 32 * TN);
 
-  Loader<T, 32, AKC, 1, ALIGNED, false> la;
+  Loader<T, 32 * TM, AKC, 1, ALIGNED, false> la;
   // Gate's rows of the tile and up's come from two matrices: a loader for each.
   constexpr bool PAIR = OP == GEMM_GATED;
   Loader<T, PAIR ? 32 : 32 * TN, BKC, 1, ALIGNED, false> lb, lb2;
@@ -58,19 +58,24 @@ __global__ __launch_bounds__(kSplit * 64) void k_ffn_small(GemmArgs g) {
     __builtin_amdgcn_wave_barrier();
   };
 
-  f32x16 acc[TN];
+  f32x16 acc[TM][TN];
 #pragma unroll
-  for (int j = 0; j < TN; ++j)
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[j][e] = 0.f;
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
   auto multiply = [&](const u32x4* lds) {
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
-      const Frag<T> a = read_frag<T, 32, AKC>(lds, 0, 0, ks, lane);
+      Frag<T> a[TM];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) a[i] = read_frag<T, 32 * TM, AKC>(lds, 0, i * 32, ks, lane);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         const Frag<T> b = read_frag<T, 32 * TN, BKC>(lds, LA::kUnits, j * 32, ks, lane);
-        acc[j] = mfma(b, a, acc[j]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[i][j] = mfma(b, a[i], acc[i][j]);
       }
     }
   };
@@ -111,87 +116,96 @@ __global__ __launch_bounds__(kSplit * 64) void k_ffn_small(GemmArgs g) {
   }
 
   __syncthreads();
-  f32x4* const sums = (f32x4*)&lds0[0][0];   // [wavefront][j][q][lane]
+  f32x4* const sums = (f32x4*)&lds0[0][0];   // [wavefront][i][j][q][lane]
 #pragma unroll
-  for (int j = 0; j < TN; ++j)
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) sums[((wave * TN + j) * 4 + q) * 64 + lane] = f32x4{acc[j][q * 4], acc[j][q * 4 + 1], acc[j][q * 4 + 2], acc[j][q * 4 + 3]};
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        sums[(((wave * TM + i) * TN + j) * 4 + q) * 64 + lane] = f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
   __syncthreads();
   if (wave >= 4) return;
-  const int q = wave;
-  f32x4 v[TN];
-#pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    v[j] = sums[(j * 4 + q) * 64 + lane];
-#pragma unroll
-    for (int s = 1; s < kSplit; ++s) v[j] += sums[((s * TN + j) * 4 + q) * 64 + lane];
-  }
-
-  const uint32_t m = m0 + (lane & 31), inner = 8 * q + 4 * (lane >> 5);
-  if (m >= g.M) return;
+  const int q = wave, inner = 8 * q + 4 * (lane >> 5);
   const GemmOperand& co = g.c[OP == GEMM_WEIGHT ? part : 0];
-  T* const c = (T*)co.p + (int64_t)w * co.worker + (int64_t)m * co.ld;
-  if constexpr (OP == GEMM_GATED) {
-    const uint32_t n = n0 + inner;
-    if (n >= g.pitch) return;
-    f32x4 gate, up;
-    float h[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool real = n + e < g.N;   // the columns up to `pitch` are 0
-      gate[e] = real ? v[0][e] : 0.f;
-      up[e] = real ? v[1][e] : 0.f;
-      float a, slope;
-      activate<ERF, sizeof(T) == 2>(g.activation, gate[e], a, slope);
-      h[e] = real ? a * up[e] : 0.f;
-    }
-    store_n<4>(c + n, h);
-    if (g.proj) {
-      float* p = proj_at(g, w, m0, n0, q, lane);
-      *(f32x4*)p = gate;
-      *(f32x4*)(p + 1024) = up;
-    }
-  } else {
+  for (int i = 0; i < TM; ++i) {
+    const uint32_t rows0 = m0 + i * 32, m = rows0 + (lane & 31);
+    if (m >= g.M) return;
+    f32x4 v[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const uint32_t n = n0 + j * 32 + inner;
-      if constexpr (OP == GEMM_GATED_BWD) {
-        if (n >= g.pitch) continue;
-        const float* p = proj_at(g, w, m0, n0 + j * 32, q, lane);
-        const f32x4 gate = *(const f32x4*)p, up = *(const f32x4*)(p + 1024);
-        float dg[4], du[4];
+      v[j] = sums[((i * TN + j) * 4 + q) * 64 + lane];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float a, slope;
-          activate<ERF, sizeof(T) == 2>(g.activation, gate[e], a, slope);
-          const bool real = n + e < g.N;
-          dg[e] = real ? v[j][e] * up[e] * slope : 0.f;
-          du[e] = real ? v[j][e] * a : 0.f;
+      for (int s = 1; s < kSplit; ++s) v[j] += sums[(((s * TM + i) * TN + j) * 4 + q) * 64 + lane];
+    }
+    T* const c = (T*)co.p + (int64_t)w * co.worker + (int64_t)m * co.ld;
+    if constexpr (OP == GEMM_GATED) {
+      const uint32_t n = n0 + inner;
+      if (n >= g.pitch) return;
+      f32x4 gate, up;
+      float h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool real = n + e < g.N;   // the columns up to `pitch` are 0
+        gate[e] = real ? v[0][e] : 0.f;
+        up[e] = real ? v[1][e] : 0.f;
+        float a, slope;
+        activate<ERF, sizeof(T) == 2>(g.activation, gate[e], a, slope);
+        h[e] = real ? a * up[e] : 0.f;
+      }
+      store_n<4>(c + n, h);
+      if (g.proj) {
+        float* p = proj_at(g, w, rows0, n0, q, lane);
+        *(f32x4*)p = gate;
+        *(f32x4*)(p + 1024) = up;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const uint32_t n = n0 + j * 32 + inner;
+        if constexpr (OP == GEMM_GATED_BWD) {
+          if (n >= g.pitch) continue;
+          const float* p = proj_at(g, w, rows0, n0 + j * 32, q, lane);
+          const f32x4 gate = *(const f32x4*)p, up = *(const f32x4*)(p + 1024);
+          float dg[4], du[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float a, slope;
+            activate<ERF, sizeof(T) == 2>(g.activation, gate[e], a, slope);
+            const bool real = n + e < g.N;
+            dg[e] = real ? v[j][e] * up[e] * slope : 0.f;
+            du[e] = real ? v[j][e] * a : 0.f;
+          }
+          store_n<4>(c + n, dg);
+          store_n<4>(c + g.pitch + n, du);
+        } else {
+          const float y[4] = {v[j][0], v[j][1], v[j][2], v[j][3]};
+          if (n < g.N) store_upto<4>(c + n, (int)(g.N - n), y);
         }
-        store_n<4>(c + n, dg);
-        store_n<4>(c + g.pitch + n, du);
-      } else {
-        const float y[4] = {v[j][0], v[j][1], v[j][2], v[j][3]};
-        if (n < g.N) store_upto<4>(c + n, (int)(g.N - n), y);
       }
     }
   }
 }
 
 template <typename T, int OP, bool ERF>
-hipError_t launch_small(bool narrow, bool aligned, GemmArgs g, hipStream_t s) {
-  const uint32_t n = OP == GEMM_GATED || OP == GEMM_GATED_BWD ? g.pitch : g.N, bn = OP == GEMM_GATED || narrow ? 32 : 64;
-  g.tiles_m = (g.M + 31) / 32;
+hipError_t launch_small(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) {
+  const bool narrow = tile == TILE_SMALL_NARROW && OP != GEMM_GATED, square = tile == TILE_SMALL_SQUARE;
+  if (square && !aligned) return hipErrorInvalidValue;
+  const uint32_t n = OP == GEMM_GATED || OP == GEMM_GATED_BWD ? g.pitch : g.N, bm = square ? 64 : 32, bn = OP == GEMM_GATED || narrow ? 32 : 64;
+  g.tiles_m = (g.M + bm - 1) / bm;
   g.tiles_n = (n + bn - 1) / bn;
   const uint64_t grid = (uint64_t)g.tiles_m * g.tiles_n * g.workers * g.parts;
   if (!grid) return hipSuccess;
   if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
-  if (OP == GEMM_GATED || !narrow) {
-    if (aligned) k_ffn_small<T, OP, ERF, 2, 4, true><<<(uint32_t)grid, 256, 0, s>>>(g);
-    else k_ffn_small<T, OP, ERF, 2, 4, false><<<(uint32_t)grid, 256, 0, s>>>(g);
+  if (square) {
+    k_ffn_small<T, OP, ERF, 2, 2, 4, true><<<(uint32_t)grid, 256, 0, s>>>(g);
+  } else if (!narrow) {
+    if (aligned) k_ffn_small<T, OP, ERF, 1, 2, 4, true><<<(uint32_t)grid, 256, 0, s>>>(g);
+    else k_ffn_small<T, OP, ERF, 1, 2, 4, false><<<(uint32_t)grid, 256, 0, s>>>(g);
   } else if constexpr (OP != GEMM_GATED) {
-    if (aligned) k_ffn_small<T, OP, ERF, 1, 8, true><<<(uint32_t)grid, 512, 0, s>>>(g);
-    else k_ffn_small<T, OP, ERF, 1, 8, false><<<(uint32_t)grid, 512, 0, s>>>(g);
+    if (aligned) k_ffn_small<T, OP, ERF, 1, 1, 8, true><<<(uint32_t)grid, 512, 0, s>>>(g);
+    else k_ffn_small<T, OP, ERF, 1, 1, 8, false><<<(uint32_t)grid, 512, 0, s>>>(g);
   }
   return hipGetLastError();
 }

@@ -81,6 +81,15 @@ def test_large_tiles(nn, dtype, size):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=SHORT.get)
+@pytest.mark.parametrize("size", [(1, 2000, 392, 648), (1, 130, 1040, 4008), (3, 270, 390, 1365)], ids=str)
+def test_long_sums(nn, dtype, size):
+    """Sizes at which a product's k is shared out among wavefronts, with more tiles than CUs where those are small."""
+    t = tensors(*size, dtype, seed=16)
+    _, got = train(nn, t, dtype, "silu")
+    check("silu", dtype, t, got, NAMES)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=SHORT.get)
 def test_strides_and_alignment(nn, dtype):
     """Rows further apart than they are long, workers next to each other, tensors that begin anywhere; what lies between is NaN and is not touched."""
     W, T, D, F = 2, 37, 72, 88
