@@ -206,6 +206,19 @@ __device__ __forceinline__ float* proj_at(const GemmArgs& g, uint32_t w, uint32_
   return g.proj + w * g.proj_worker + ((uint64_t)(m >> 5) * (g.pitch >> 5) + (n >> 5)) * 2048 + q * 256 + lane * 4;
 }
 
+// Large tiles, whose products have many, move them past the caches, which keep the operands instead: forward and backward of 2048 tokens,
+// 2048 x 8192, in 675 instead of 762 us, of 8192 in 2245 instead of 2294; where 64 rows are a tile it makes no difference.
+template <bool ONCE>
+__device__ __forceinline__ void put_proj(float* p, f32x4 v) {
+  if constexpr (ONCE) __builtin_nontemporal_store(v, (f32x4*)p);
+  else *(f32x4*)p = v;
+}
+template <bool ONCE>
+__device__ __forceinline__ f32x4 get_proj(const float* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load((const f32x4*)p);
+  else return *(const f32x4*)p;
+}
+
 // This wavefront's loads into LDS have arrived and its reads of LDS are done; then the workgroup meets.
 __device__ __forceinline__ void wait_and_meet() {
   __builtin_amdgcn_sched_barrier(0);
@@ -408,8 +421,8 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, BM == 64 ? 3 : 2) void k_ff
           }
           if (g.proj && n < g.pitch) {
             float* p = proj_at(g, w, rows0, n, q, lane);
-            *(f32x4*)p = gate;
-            *(f32x4*)(p + 1024) = up;
+            put_proj<(BM >= 128)>(p, gate);
+            put_proj<(BM >= 128)>(p + 1024, up);
           }
         }
       leave(Cols{}, c, rows0, first, g.pitch, [&](int j, int q) { return h[j][q]; });
@@ -423,8 +436,8 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, BM == 64 ? 3 : 2) void k_ff
         const float* p = proj_at(g, w, rows0, min(first + j * 32, g.pitch - 32), 0, lane);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          gate[q] = *(const f32x4*)(p + q * 256);
-          up[q] = *(const f32x4*)(p + 1024 + q * 256);
+          gate[q] = get_proj<(BM >= 128)>(p + q * 256);
+          up[q] = get_proj<(BM >= 128)>(p + 1024 + q * 256);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
