@@ -9,8 +9,9 @@
 //     d_pre = sum dn ur,  d_pre_bias = sum dn,  d_post = sum da ub,  d_post_bias = sum da     over a worker's rows
 // The backward pass makes both norms anew from residual and branch: nothing has to be kept, and r' is not read in rounded form.
 //
-// Both passes are bound by memory.  A row stays in the registers of 64 to 1024 threads, 8 or 16 elements of each tensor in a
-// thread, so that each tensor is read once; the sums over a row go through the wavefront and one exchange in LDS.
+// Both passes are bound by memory.  A row stays in the registers of 16 to 1024 threads (64 and more in the backward pass), 8 or 16 elements
+// of each tensor in a thread, so that each tensor is read once; the sums over a row go through the wavefront and one exchange in LDS.
+// Several narrow rows to a wavefront: 11 x 5331 rows of 64 forward in 17 instead of 36 us, 8000 of 256 in 7 instead of 10.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -24,7 +25,6 @@
 namespace evg {
 namespace {
 
-constexpr uint32_t kStripes = 1024;      // of all workers together, about
 constexpr int kV = 8;                    // elements of a thread that lie together
 
 struct NormArgs {
@@ -46,13 +46,23 @@ __device__ __forceinline__ T* at(const evg_mat& m, uint32_t w, uint64_t row) {
   return (T*)m.p + (int64_t)w * m.worker + (int64_t)row * m.row;
 }
 
+template <int TPR> constexpr int kRowWaves = TPR < 64 ? 1 : TPR / 64;   // that share a row
+
 // The sums of two values over the threads that share a row.  `red` alternates between two sets, so one barrier is enough.
 template <int TPR>
-__device__ __forceinline__ void row_sum2(float& a, float& b, float (*red)[2][TPR / 64], int& turn) {
+__device__ __forceinline__ void row_sum2(float& a, float& b, float (*red)[2][kRowWaves<TPR>], int& turn) {
+  if constexpr (TPR < 64) {
+#pragma unroll
+    for (int m = 1; m < TPR; m *= 2) {   // all lanes get the same bits: each adds the same pairs
+      a += __shfl_xor(a, m);
+      b += __shfl_xor(b, m);
+    }
+    return;
+  }
   a = wave_sum_uniform(a);
   b = wave_sum_uniform(b);
   if constexpr (TPR > 64) {
-    float(&set)[2][TPR / 64] = red[turn];
+    float(&set)[2][kRowWaves<TPR>] = red[turn];
     turn ^= 1;
     const int wave = threadIdx.x % TPR / 64;
     if (threadIdx.x % 64 == 0) { set[0][wave] = a; set[1][wave] = b; }
@@ -136,10 +146,10 @@ __device__ __forceinline__ float make_unit(Row<NV>& x, const NormArgs& g, int la
 template <typename T, int NV, int TPR, bool LAYER>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_blocknorm_forward(NormArgs g) {
   constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;   // rows of a workgroup
-  __shared__ float shared[ROWS][2][2][TPR / 64];
+  __shared__ float shared[ROWS][2][2][kRowWaves<TPR>];
   int turn = 0;
   const int lane = threadIdx.x % TPR;
-  float(*red)[2][TPR / 64] = shared[threadIdx.x / TPR];
+  float(*red)[2][kRowWaves<TPR>] = shared[threadIdx.x / TPR];
   const uint64_t row0 = (uint64_t)blockIdx.x * ROWS + threadIdx.x / TPR, all = (uint64_t)g.workers * g.in.rows;
   const bool real = row0 < all;
   const uint64_t row = real ? row0 : all - 1;       // all threads of a workgroup meet at its barriers
@@ -463,7 +473,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_blocknorm_join(NormArgs g, 
   float sum = 0.f;
   if (c < g.padded) {
     const float* p = g.partials + ((uint64_t)w * g.stripes * 5 + min(which, 4u)) * g.padded + c;
-#pragma unroll 4
+#pragma unroll 8
     for (uint32_t s = s0 + wave; s < s1; s += kJoinWaves) sum += p[(uint64_t)s * 5 * g.padded];
   }
   part[wave][lane] = sum;
@@ -484,6 +494,8 @@ hipError_t forward_sized(const NormArgs& g, hipStream_t s) {
 
 template <typename T, bool LAYER>
 hipError_t launch_forward(const NormArgs& g, hipStream_t s) {
+  if (g.width <= 128) return forward_sized<T, 1, 16, LAYER>(g, s);
+  if (g.width <= 256) return forward_sized<T, 1, 32, LAYER>(g, s);
   if (g.width <= 512) return forward_sized<T, 1, 64, LAYER>(g, s);
   if (g.width <= 1024) return forward_sized<T, 2, 64, LAYER>(g, s);
   if (g.width <= 2048) return forward_sized<T, 2, 128, LAYER>(g, s);
@@ -544,9 +556,16 @@ struct evg_blocknorm {
 
 namespace {
 
-// Rows of a stripe such that all workers together have about kStripes of them.
-uint32_t stripe_rows(uint32_t workers, uint32_t rows) {
-  const uint64_t r = ((uint64_t)workers * rows + kStripes - 1) / kStripes;
+// Stripes of all workers together, about.  A stripe is a workgroup, and the more wavefronts that has the fewer fill the chip; every one
+// leaves a row of sums for the join, which is the slower the more of them one worker has.  Backward and join, 1024 / 2048 / 4096 of them:
+// 16384 rows of 4096 179 / 190 / 222 us, of 1024 66 / 55 / 68; 8 x 2000 of 512 48 / 36 / 33; 11 x 5331 of 64 103 / 65 / 50; 1 x 16384 of 64
+// 40 / 36 / 43.
+uint32_t most_stripes(uint32_t workers, uint32_t width) { return width > 1024 ? 1024 : width > 512 || workers == 1 ? 2048 : 4096; }
+
+// Rows of a stripe such that there are about so many.
+uint32_t stripe_rows(uint32_t workers, uint32_t width, uint32_t rows) {
+  const uint32_t most = most_stripes(workers, width);
+  const uint64_t r = ((uint64_t)workers * rows + most - 1) / most;
   return (uint32_t)(r < 1 ? 1 : r > rows ? (rows ? rows : 1) : r);
 }
 
@@ -604,7 +623,7 @@ evg_status evg_blocknorm_init(evg_blocknorm** out, const evg_blocknorm_config* c
   c->stream = static_cast<hipStream_t>(hip_stream);
   c->padded = (cfg->width + 63) / 64 * 64;
   // Stripes of whole gate groups are at least half as long as those asked for, and a group's last one may be short (backward).
-  const uint64_t per = (kStripes + cfg->workers - 1) / cfg->workers;
+  const uint64_t per = ((uint64_t)most_stripes(cfg->workers, cfg->width) + cfg->workers - 1) / cfg->workers;
   c->max_stripes = 3 * (per < cfg->max_rows ? per : cfg->max_rows) + 2;
   const hipError_t e = hipMalloc((void**)&c->partials, cfg->workers * c->max_stripes * 5 * c->padded * sizeof(float));
   if (e != hipSuccess) {
@@ -673,7 +692,7 @@ evg_status evg_blocknorm_backward(evg_blocknorm* c, const evg_blocknorm_in* in, 
   if (has_normed) g.d_normed = *d_normed;
   g.d = *out;
   if (in->rows) {
-    g.stripe_rows = stripe_rows(W, in->rows);
+    g.stripe_rows = stripe_rows(W, D, in->rows);
     g.stripes = (in->rows + g.stripe_rows - 1) / g.stripe_rows;
     if (out->gate.p && in->gate_rows <= g.stripe_rows) {
       g.stripe_rows = g.stripe_rows / in->gate_rows * in->gate_rows;

@@ -93,6 +93,15 @@ def test_sizes(nn, dtype, kind, size):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=SHORT.get)
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("size", [(1, 3, 8), (1, 17, 127), (2, 15, 128), (1, 33, 129), (3, 7, 255), (1, 9, 256), (1, 5, 257), (2, 2500, 33), (1, 4100, 130)], ids=str)
+def test_narrow_rows(nn, dtype, kind, size):
+    """Widths around what 16 and 32 threads hold; rows that fill a workgroup and do not; more rows than stripes."""
+    t, d_out, d_normed = tensors(*size, dtype, kind, 3, seed=6)
+    check(nn, kind, dtype, t, d_out, d_normed, 3)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=SHORT.get)
 @pytest.mark.parametrize("rows,gate_rows", [(1, 1), (9, 1), (9, 4), (9, 9), (9, 100), (2500, 1), (2500, 2), (2500, 3), (2500, 7), (2500, 1000),
                                             (2500, 2500), (1025, 1024)])
 def test_gates(nn, dtype, rows, gate_rows):
