@@ -8,6 +8,9 @@
 //     d_branch = (p - mean(p) - ub mean(p ub)) / s_b           (da itself without post)
 //     d_pre = sum dn ur,  d_pre_bias = sum dn,  d_post = sum da ub,  d_post_bias = sum da     over a worker's rows
 // The backward pass makes both norms anew from residual and branch: nothing has to be kept, and r' is not read in rounded form.
+// A mean in 32 bits is off by units of where the row lies, which may be more than its spread.  The differences from it are exact where that is so;
+// what they still add up to, delta a value, is summed beside their squares and taken back: from the row, from the variance (mean of squares
+// - delta^2) and from sums of products with the row.  Rows of 1e4 with a spread of 0.05 were off by 1e-2 without.
 //
 // Both passes are bound by memory.  A row stays in the registers of 16 to 1024 threads (64 and more in the backward pass), 8 or 16 elements
 // of each tensor in a thread, so that each tensor is read once; the sums over a row go through the wavefront and one exchange in LDS.
@@ -48,29 +51,34 @@ __device__ __forceinline__ T* at(const evg_mat& m, uint32_t w, uint64_t row) {
 
 template <int TPR> constexpr int kRowWaves = TPR < 64 ? 1 : TPR / 64;   // that share a row
 
-// The sums of two values over the threads that share a row.  `red` alternates between two sets, so one barrier is enough.
-template <int TPR>
-__device__ __forceinline__ void row_sum2(float& a, float& b, float (*red)[2][kRowWaves<TPR>], int& turn) {
+// The sums of two or three values over the threads that share a row.  `red` alternates between two sets, so one barrier is enough.
+constexpr int kSums = 3;
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*red)[kSums][kRowWaves<TPR>], int& turn) {
+  static_assert(N <= kSums, "");
   if constexpr (TPR < 64) {
 #pragma unroll
-    for (int m = 1; m < TPR; m *= 2) {   // all lanes get the same bits: each adds the same pairs
-      a += __shfl_xor(a, m);
-      b += __shfl_xor(b, m);
-    }
+    for (int m = 1; m < TPR; m *= 2)     // all lanes get the same bits: each adds the same pairs
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] += __shfl_xor(v[n], m);
     return;
   }
-  a = wave_sum_uniform(a);
-  b = wave_sum_uniform(b);
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = wave_sum_uniform(v[n]);
   if constexpr (TPR > 64) {
-    float(&set)[2][kRowWaves<TPR>] = red[turn];
+    float(&set)[kSums][kRowWaves<TPR>] = red[turn];
     turn ^= 1;
     const int wave = threadIdx.x % TPR / 64;
-    if (threadIdx.x % 64 == 0) { set[0][wave] = a; set[1][wave] = b; }
-    __syncthreads();
-    a = set[0][0];
-    b = set[1][0];
+    if (threadIdx.x % 64 == 0)
 #pragma unroll
-    for (int i = 1; i < TPR / 64; ++i) { a += set[0][i]; b += set[1][i]; }
+      for (int n = 0; n < N; ++n) set[n][wave] = v[n];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = set[n][0];
+#pragma unroll
+    for (int i = 1; i < TPR / 64; ++i)
+#pragma unroll
+      for (int n = 0; n < N; ++n) v[n] += set[n][i];
   }
 }
 
@@ -121,35 +129,48 @@ __device__ __forceinline__ void store_row(T* p, int width, int lane, const Row<N
   }
 }
 
+// From the mean of the squares about a mean that is off by delta.  A NaN stays one.
+template <bool LAYER>
+__device__ __forceinline__ float variance(float squares, float delta) {
+  if (!LAYER) return squares;
+  const float v = fmaf(-delta, delta, squares);
+  return v < 0.f ? 0.f : v;
+}
+
 // x becomes its unit row; the elements beyond the width stay 0.  Returns 1 / s.
 template <int NV, int TPR, bool LAYER, typename R>
 __device__ __forceinline__ float make_unit(Row<NV>& x, const NormArgs& g, int lane, R red, int& turn) {
+  auto within = [&](int i) { return ((i / kV) * TPR + lane) * kV + i % kV < (int)g.width; };
   if constexpr (LAYER) {
-    float s = 0.f, none = 0.f;
+    float s[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < NV * kV; ++i) s += x.v[i];
-    row_sum2<TPR>(s, none, red, turn);
-    const float mean = s * g.inv_width;
+    for (int i = 0; i < NV * kV; ++i) s[0] += x.v[i];
+    row_sums<TPR>(s, red, turn);
+    const float mean = s[0] / (float)g.width;
 #pragma unroll
-    for (int i = 0; i < NV * kV; ++i) x.v[i] = ((i / kV) * TPR + lane) * kV + i % kV < (int)g.width ? x.v[i] - mean : 0.f;
+    for (int i = 0; i < NV * kV; ++i) x.v[i] = within(i) ? x.v[i] - mean : 0.f;
   }
-  float s = 0.f, none = 0.f;
+  float s[2] = {0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < NV * kV; ++i) s = fmaf(x.v[i], x.v[i], s);
-  row_sum2<TPR>(s, none, red, turn);
-  const float inv = 1.f / sqrtf(s * g.inv_width + g.eps);
+  for (int i = 0; i < NV * kV; ++i) {
+    s[0] = fmaf(x.v[i], x.v[i], s[0]);
+    if (LAYER) s[1] += x.v[i];
+  }
+  row_sums<TPR>(s, red, turn);
+  const float delta = LAYER ? s[1] * g.inv_width : 0.f;
+  const float inv = 1.f / sqrtf(variance<LAYER>(s[0] * g.inv_width, delta) + g.eps);
 #pragma unroll
-  for (int i = 0; i < NV * kV; ++i) x.v[i] *= inv;
+  for (int i = 0; i < NV * kV; ++i) x.v[i] = LAYER ? (within(i) ? (x.v[i] - delta) * inv : 0.f) : x.v[i] * inv;
   return inv;
 }
 
 template <typename T, int NV, int TPR, bool LAYER>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_blocknorm_forward(NormArgs g) {
   constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;   // rows of a workgroup
-  __shared__ float shared[ROWS][2][2][kRowWaves<TPR>];
+  __shared__ float shared[ROWS][2][kSums][kRowWaves<TPR>];
   int turn = 0;
   const int lane = threadIdx.x % TPR;
-  float(*red)[2][kRowWaves<TPR>] = shared[threadIdx.x / TPR];
+  float(*red)[kSums][kRowWaves<TPR>] = shared[threadIdx.x / TPR];
   const uint64_t row0 = (uint64_t)blockIdx.x * ROWS + threadIdx.x / TPR, all = (uint64_t)g.workers * g.in.rows;
   const bool real = row0 < all;
   const uint64_t row = real ? row0 : all - 1;       // all threads of a workgroup meet at its barriers
@@ -284,7 +305,7 @@ template <typename T> struct Lines {
 template <typename T, int NV, int TPR, bool LAYER, int GATED, int POST>
 __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
   constexpr bool WHOLE = GATED >= 0;
-  __shared__ float red[2][2][TPR / 64];
+  __shared__ float red[2][kSums][TPR / 64];
   int turn = 0;
   const int lane = threadIdx.x;
   const uint32_t w = blockIdx.x / g.stripes, stripe = blockIdx.x % g.stripes;
@@ -373,24 +394,30 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
       unpack<WHOLE, NV, TPR>(w_pre, width, lane, k);
       float mean_q = 0.f;
       if constexpr (LAYER) {
-        float sr = 0.f, sq = 0.f;
+        float s[2] = {0.f, 0.f};   // r, q
 #pragma unroll
-        for (int i = 0; i < N; ++i) { sr += r.v[i]; sq = fmaf(d.v[i], k.v[i], sq); }
-        row_sum2<TPR>(sr, sq, red, turn);
-        const float mean = sr * inv_width;
-        mean_q = sq * inv_width;
+        for (int i = 0; i < N; ++i) { s[0] += r.v[i]; s[1] = fmaf(d.v[i], k.v[i], s[1]); }
+        row_sums<TPR>(s, red, turn);
+        const float mean = s[0] / (float)width;
+        mean_q = s[1] * inv_width;
 #pragma unroll
         for (int i = 0; i < N; ++i) r.v[i] = ((i / kV) * TPR + lane) * kV + i % kV < width ? r.v[i] - mean : 0.f;
       }
-      float ss = 0.f, qr = 0.f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) { ss = fmaf(r.v[i], r.v[i], ss); qr = fmaf(d.v[i] * k.v[i], r.v[i], qr); }
-      row_sum2<TPR>(ss, qr, red, turn);
-      const float inv = 1.f / sqrtf(ss * inv_width + g.eps);
-      const float c = qr * inv_width * inv;
+      float s[LAYER ? 3 : 2] = {};   // r^2, q r, r
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float u = r.v[i] * inv;
+        s[0] = fmaf(r.v[i], r.v[i], s[0]);
+        s[1] = fmaf(d.v[i] * k.v[i], r.v[i], s[1]);
+        if constexpr (LAYER) s[2] += r.v[i];
+      }
+      row_sums<TPR>(s, red, turn);
+      float delta = 0.f;
+      if constexpr (LAYER) delta = s[2] * inv_width;
+      const float inv = 1.f / sqrtf(variance<LAYER>(s[0] * inv_width, delta) + g.eps);
+      const float c = (LAYER ? fmaf(-delta, mean_q, s[1] * inv_width) : s[1] * inv_width) * inv;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float u = (LAYER ? r.v[i] - delta : r.v[i]) * inv;   // what lies beyond the width meets a d and a sum that are not used there
         s_pre.v[i] = fmaf(d.v[i], u, s_pre.v[i]);
         if (LAYER) s_prebias.v[i] += d.v[i];
         d.v[i] = (d.v[i] * k.v[i] - mean_q - u * c) * inv;
@@ -430,18 +457,17 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
     }
     if (post) {
       unpack<WHOLE, NV, TPR>(w_post, width, lane, k);
-      float pb = 0.f, sp = 0.f;
+      float s[2] = {0.f, 0.f};   // p b, p
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         s_post.v[i] = fmaf(d.v[i], b.v[i], s_post.v[i]);
         if (LAYER) s_postbias.v[i] += d.v[i];
         d.v[i] *= k.v[i];
-        pb = fmaf(d.v[i], b.v[i], pb);
-        if (LAYER) sp += d.v[i];
+        s[0] = fmaf(d.v[i], b.v[i], s[0]);
+        if (LAYER) s[1] += d.v[i];
       }
-      row_sum2<TPR>(pb, sp, red, turn);
-      pb *= inv_width;
-      sp *= inv_width;
+      row_sums<TPR>(s, red, turn);
+      const float pb = s[0] * inv_width, sp = s[1] * inv_width;
 #pragma unroll
       for (int i = 0; i < N; ++i) d.v[i] = (d.v[i] - sp - b.v[i] * pb) * inv_b;
     }
