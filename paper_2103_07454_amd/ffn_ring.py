@@ -8,13 +8,16 @@ Every worker has its own copy of the parameters in the ring's arena and its own 
     the ring    Ring.step: triggers, sends, averaging with the neighbours and momentum SGD
 
 In 32 bits the operators read the ring's arena itself.  In 16 bits they read a rounded copy of it and fill a 16-bit gradient
-arena, which clipping widens.
+arena, which clipping widens.  The gradients of float16 are those of ``loss_scale`` times the loss: the loss is a mean over a
+worker's values, so the gradient of one of them would lie among the subnormals.  Clipping takes the scale back, and a worker whose
+scaled gradient overflows sits the step out.
 
     python -m paper_2103_07454_amd.ffn_ring --workers 8 --width 512 --hidden 2048 --blocks 2 --tokens 256 --dtype bf16
 """
 from __future__ import annotations
 
 import argparse
+import math
 
 import numpy as np
 import torch
@@ -27,9 +30,13 @@ _BLOCK = ("pre", "w_gate", "w_up", "w_down", "gate", "post")
 
 class FFNRing:
     def __init__(self, workers=4, *, width=64, hidden=192, blocks=2, tokens=32, dtype=torch.float32, activation="silu",
-                 lr=0.05, momentum=0.9, max_norm=1.0, seed=0, **ring_options):
+                 lr=0.05, momentum=0.9, max_norm=1.0, seed=0, loss_scale=None, **ring_options):
         self.workers, self.width, self.hidden, self.blocks, self.tokens = workers, width, hidden, blocks, tokens
         self.dtype, self.max_norm = dtype, max_norm
+        half = dtype == torch.float16
+        # An error of 1 becomes a gradient of about 1, or less where there are so many tokens that a weight's gradient, a sum over
+        # them, would reach float16's 65504.  A power of two: taking it back is exact.
+        self.loss_scale = loss_scale or (2.0 ** round(math.log2(width * min(tokens, 4096))) if half else 1.0)
         shape = dict(pre=(width,), w_gate=(hidden, width), w_up=(hidden, width), w_down=(width, hidden), gate=(width,), post=(width,))
         self.names = [(b, n) for b in range(blocks) for n in _BLOCK] + [(blocks, "pre")]      # the last norm has no block behind it
         self.shapes = [shape[n] for _, n in self.names]
@@ -51,7 +58,8 @@ class FFNRing:
         self.norm = nn.BlockNorm(width, workers=workers, max_rows=tokens, dtype=dtype, gate_rows=tokens)
         self.ffn = nn.GatedFFN(width, hidden, workers=workers, max_rows=tokens, dtype=dtype, activation=nn.ACTIVATIONS[activation],
                                train=True)
-        self.clip = nn.GradClip(numel, workers, dtype=dtype, out_dtype=torch.float32)
+        self.clip = nn.GradClip(numel, workers, dtype=dtype, out_dtype=torch.float32,
+                                nonfinite=nn.NONFINITE_ZERO if half else nn.NONFINITE_PASS)
         self.k = 0
 
     def _views(self, arena):
@@ -91,8 +99,8 @@ class FFNRing:
             self.low.copy_(self.ring.x)
         out, kept = self.forward(x)
         error = out.float() - target.float()
-        self.backward((error / error[0].numel()).to(self.dtype), kept)
-        _, norm = self.clip.clip(self.low_grad, self.max_norm, out=self.grad)
+        self.backward((error / (error[0].numel() / self.loss_scale)).to(self.dtype), kept)
+        _, norm = self.clip.clip(self.low_grad, self.max_norm, out=self.grad, scale=1.0 / self.loss_scale)
         self.ring.step(self.k, self.grad)
         self.k += 1
         return 0.5 * error.square().mean((1, 2)), norm
