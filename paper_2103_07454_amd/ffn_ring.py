@@ -71,7 +71,9 @@ class FFNRing:
         return out
 
     def forward(self, x):
-        """The output [workers, tokens, width] and what the backward pass needs."""
+        """The output [workers, tokens, width] of the ring's present parameters, and what the backward pass needs."""
+        if self.low is not self.ring.x:
+            self.low.copy_(self.ring.x)
         p, kept = self.params, []
         residual, normed = self.norm.forward(x, pre=p[0, "pre"])
         for b in range(self.blocks):
@@ -95,8 +97,6 @@ class FFNRing:
 
     def step(self, x, target):
         """One iteration on inputs and targets [workers, tokens, width]; each worker's loss and gradient norm, on the GPU."""
-        if self.low is not self.ring.x:
-            self.low.copy_(self.ring.x)
         out, kept = self.forward(x)
         error = out.float() - target.float()
         self.backward((error / (error[0].numel() / self.loss_scale)).to(self.dtype), kept)
