@@ -30,7 +30,8 @@ _BLOCK = ("pre", "w_gate", "w_up", "w_down", "gate", "post")
 
 class FFNRing:
     def __init__(self, workers=4, *, width=64, hidden=192, blocks=2, tokens=32, dtype=torch.float32, activation="silu",
-                 lr=0.05, momentum=0.9, max_norm=1.0, seed=0, loss_scale=None, **ring_options):
+                 lr=0.05, momentum=0.9, max_norm=1.0, seed=0, loss_scale=None,
+                 device="cuda:0", stream=None, **ring_options):
         self.workers, self.width, self.hidden, self.blocks, self.tokens = workers, width, hidden, blocks, tokens
         self.dtype, self.max_norm = dtype, max_norm
         half = dtype == torch.float16
@@ -49,17 +50,22 @@ class FFNRing:
             else:
                 first.append(np.full(s, 0.5 if n == "gate" else 1.0))
         x0 = np.broadcast_to(np.concatenate(first).astype(np.float32), (workers, sum(numel)))
-        self.ring = evg.Ring(x0, numel, lr=lr, momentum=momentum, grad_mode=evg.GRAD_BUFFER, **ring_options)
-        arena = self.ring.x
-        self.grad = torch.zeros_like(arena)                                   # what the ring takes
-        self.low = arena if dtype == torch.float32 else torch.empty_like(arena, dtype=dtype)
-        self.low_grad = self.grad if dtype == torch.float32 else torch.zeros_like(self.low)
-        self.params, self.grads = self._views(self.low), self._views(self.low_grad)
-        self.norm = nn.BlockNorm(width, workers=workers, max_rows=tokens, dtype=dtype, gate_rows=tokens)
-        self.ffn = nn.GatedFFN(width, hidden, workers=workers, max_rows=tokens, dtype=dtype, activation=nn.ACTIVATIONS[activation],
-                               train=True)
-        self.clip = nn.GradClip(numel, workers, dtype=dtype, out_dtype=torch.float32,
-                                nonfinite=nn.NONFINITE_ZERO if half else nn.NONFINITE_PASS)
+        # The ring and the operators share one stream: what one writes the next reads.
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        where = dict(device=device, stream=self.stream)
+        with torch.cuda.stream(self.stream):
+            self.ring = evg.Ring(x0, numel, lr=lr, momentum=momentum, grad_mode=evg.GRAD_BUFFER, **where, **ring_options)
+            arena = self.ring.x
+            self.grad = torch.zeros_like(arena)                                   # what the ring takes
+            self.low = arena if dtype == torch.float32 else torch.empty_like(arena, dtype=dtype)
+            self.low_grad = self.grad if dtype == torch.float32 else torch.zeros_like(self.low)
+            self.params, self.grads = self._views(self.low), self._views(self.low_grad)
+            self.norm = nn.BlockNorm(width, workers=workers, max_rows=tokens, dtype=dtype, gate_rows=tokens, **where)
+            self.ffn = nn.GatedFFN(width, hidden, workers=workers, max_rows=tokens, dtype=dtype, activation=nn.ACTIVATIONS[activation],
+                                   train=True, **where)
+            self.clip = nn.GradClip(numel, workers, dtype=dtype, out_dtype=torch.float32,
+                                    nonfinite=nn.NONFINITE_ZERO if half else nn.NONFINITE_PASS, **where)
+        self.stream.synchronize()
         self.k = 0
 
     def _views(self, arena):
