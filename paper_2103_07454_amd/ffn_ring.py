@@ -12,11 +12,15 @@ arena, which clipping widens.  The gradients of float16 are those of ``loss_scal
 worker's values, so the gradient of one of them would lie among the subnormals.  Clipping takes the scale back, and a worker whose
 scaled gradient overflows sits the step out.
 
+All work is on the stream that the object was made with.  ``forward``, ``backward`` and ``step`` may be called under any other: they
+begin behind what the caller's stream has been given so far, and the caller's stream goes on behind them.
+
     python -m paper_2103_07454_amd.ffn_ring --workers 8 --width 512 --hidden 2048 --blocks 2 --tokens 256 --dtype bf16
 """
 from __future__ import annotations
 
 import argparse
+import contextlib
 import math
 
 import numpy as np
@@ -76,40 +80,62 @@ class FFNRing:
             out[key] = v[:, None] if key[1] == "gate" else v.unflatten(1, shape) if len(shape) == 2 else v
         return out
 
+    @contextlib.contextmanager
+    def _ordered(self):
+        """The block's work goes to the object's stream, between what the caller's has been given before and after.  Yields what hands
+        tensors of the block to the caller: their memory is not used again before the caller's stream is done with them."""
+        caller = torch.cuda.current_stream(self.stream.device)
+        if caller == self.stream:
+            yield lambda *tensors: None
+            return
+        self.stream.wait_stream(caller)
+        try:
+            with torch.cuda.stream(self.stream):
+                yield lambda *tensors: [t.record_stream(caller) for t in tensors]
+        finally:
+            caller.wait_stream(self.stream)
+
     def forward(self, x):
         """The output [workers, tokens, width] of the ring's present parameters, and what the backward pass needs."""
-        if self.low is not self.ring.x:
-            self.low.copy_(self.ring.x)
-        p, kept = self.params, []
-        residual, normed = self.norm.forward(x, pre=p[0, "pre"])
-        for b in range(self.blocks):
-            y, saved = self.ffn.forward(normed, p[b, "w_gate"], p[b, "w_up"], p[b, "w_down"], save=True)
-            kept.append((residual, normed, y, saved))
-            residual, normed = self.norm.forward(residual, y, gate=p[b, "gate"], post=p[b, "post"], pre=p[b + 1, "pre"])
+        with self._ordered() as hand_over:
+            if self.low is not self.ring.x:
+                self.low.copy_(self.ring.x)
+            p, kept = self.params, []
+            residual, normed = self.norm.forward(x, pre=p[0, "pre"])
+            for b in range(self.blocks):
+                y, saved = self.ffn.forward(normed, p[b, "w_gate"], p[b, "w_up"], p[b, "w_down"], save=True)
+                kept.append((residual, normed, y, saved))
+                hand_over(*kept[-1])
+                residual, normed = self.norm.forward(residual, y, gate=p[b, "gate"], post=p[b, "post"], pre=p[b + 1, "pre"])
+            hand_over(normed)
         return normed, kept
 
     def backward(self, d_out, kept):
         """Fills the gradient arena from the gradient of the output."""
-        p, g = self.params, self.grads
-        d_residual, d_normed = None, d_out
-        for b in reversed(range(self.blocks)):
-            residual, normed, y, saved = kept[b]
-            d = self.norm.backward(d_residual, d_normed, residual, y, gate=p[b, "gate"], post=p[b, "post"], pre=p[b + 1, "pre"],
-                                   out=dict(d_gate=g[b, "gate"], d_post=g[b, "post"], d_pre=g[b + 1, "pre"]))
-            d_residual = d["d_residual"]
-            d_normed, *_ = self.ffn.backward(d["d_branch"], normed, p[b, "w_gate"], p[b, "w_up"], p[b, "w_down"], saved,
-                                             dw_gate=g[b, "w_gate"], dw_up=g[b, "w_up"], dw_down=g[b, "w_down"])
-        self.norm.backward(d_residual, d_normed, kept[0][0], pre=p[0, "pre"], out=dict(d_pre=g[0, "pre"]))
+        with self._ordered():
+            p, g = self.params, self.grads
+            d_residual, d_normed = None, d_out
+            for b in reversed(range(self.blocks)):
+                residual, normed, y, saved = kept[b]
+                d = self.norm.backward(d_residual, d_normed, residual, y, gate=p[b, "gate"], post=p[b, "post"], pre=p[b + 1, "pre"],
+                                       out=dict(d_gate=g[b, "gate"], d_post=g[b, "post"], d_pre=g[b + 1, "pre"]))
+                d_residual = d["d_residual"]
+                d_normed, *_ = self.ffn.backward(d["d_branch"], normed, p[b, "w_gate"], p[b, "w_up"], p[b, "w_down"], saved,
+                                                 dw_gate=g[b, "w_gate"], dw_up=g[b, "w_up"], dw_down=g[b, "w_down"])
+            self.norm.backward(d_residual, d_normed, kept[0][0], pre=p[0, "pre"], out=dict(d_pre=g[0, "pre"]))
 
     def step(self, x, target):
         """One iteration on inputs and targets [workers, tokens, width]; each worker's loss and gradient norm, on the GPU."""
-        out, kept = self.forward(x)
-        error = out.float() - target.float()
-        self.backward((error / (error[0].numel() / self.loss_scale)).to(self.dtype), kept)
-        _, norm = self.clip.clip(self.low_grad, self.max_norm, out=self.grad, scale=1.0 / self.loss_scale)
-        self.ring.step(self.k, self.grad)
-        self.k += 1
-        return 0.5 * error.square().mean((1, 2)), norm
+        with self._ordered() as hand_over:
+            out, kept = self.forward(x)
+            error = out.float() - target.float()
+            self.backward((error / (error[0].numel() / self.loss_scale)).to(self.dtype), kept)
+            _, norm = self.clip.clip(self.low_grad, self.max_norm, out=self.grad, scale=1.0 / self.loss_scale)
+            self.ring.step(self.k, self.grad)
+            self.k += 1
+            loss = 0.5 * error.square().mean((1, 2))
+            hand_over(loss, norm)
+        return loss, norm
 
 
 def main(argv=None):
