@@ -37,11 +37,12 @@ typedef struct {
  * For each worker r, over all its tensors' elements (and nothing that lies between the tensors):
  *     norm[r] = |scale| * sqrt(sum of g^2)                                    (squares and sum in 64 bits)
  *     out     = g * (scale * min(1, max_norm / (norm[r] + eps)))              (the factor and the product in 32 bits)
+ * where a quotient of two zeros or of two infinities is 1: what does not exceed the bound is not clipped.
  * Arenas are laid out as evg_step's: evg_padded_numel elements for each worker, tensors at evg_layer_offsets, here of
  * any of the types; padding is neither read nor written. */
 enum {
-  EVG_NONFINITE_PASS = 0, /* the formula as it stands: a NaN makes all of a worker's gradient NaN, an infinity makes the finite
-                             elements 0 and the infinite ones NaN                                                          */
+  EVG_NONFINITE_PASS = 0, /* the formula as it stands: a NaN makes all of a worker's gradient NaN, an infinity (or a norm beyond 32
+                             bits) makes the finite elements 0 and the infinite ones NaN where max_norm is finite            */
   EVG_NONFINITE_ZERO = 1  /* a worker whose norm is not finite gets zeros: it sits the step out                              */
 };
 

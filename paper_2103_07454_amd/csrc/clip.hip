@@ -86,8 +86,9 @@ __device__ __forceinline__ float clip_factor(const ClipTables& t, const ClipCall
   for (uint32_t i = threadIdx.x; i < t.nchunks; i += kClipThreads) sum += t.partials[(uint64_t)r * t.nchunks + i];
   sum = group_sum(sum, part);
   const float norm = (float)(sqrt(sum) * fabs((double)call.scale));
-  const float keep = call.max_norm / (norm + call.eps);
-  float factor = call.scale * (keep > 1.f ? 1.f : keep);   // a NaN stays one
+  // Compared, not only divided: infinity / infinity and 0 / 0 keep the gradient too.  A NaN stays one.
+  const float bound = norm + call.eps;
+  float factor = call.scale * (bound <= call.max_norm ? 1.f : call.max_norm / bound);
   if (call.zero_nonfinite && !(norm <= 3.402823466e38f)) factor = 0.f;
   if (norm_out && threadIdx.x == 0) norm_out[r] = norm;
   return factor;
