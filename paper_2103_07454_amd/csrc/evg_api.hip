@@ -30,6 +30,8 @@ evg_status evg::fail(evg_status s, const char* fmt, ...) {
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
   g_err = buf;
+  // The runtime keeps the last error: reported here, it must not surface after the next launch, the library's or its caller's.
+  if (s == EVG_ERR_OOM || s == EVG_ERR_HIP) (void)hipGetLastError();
   return s;
 }
 
