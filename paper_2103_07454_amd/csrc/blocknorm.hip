@@ -42,6 +42,7 @@ struct NormArgs {
   uint32_t group_stripes;                // stripes of a gate's group; 0: a stripe has whole groups
   float* partials;                       // [workers][stripes][5][padded width]: pre, pre_bias, post, post_bias, gate
   uint32_t padded;
+  uint32_t first;                        // workgroup of a launch in pieces
 };
 
 template <typename T>
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_blocknorm_forward(Nor
   int turn = 0;
   const int lane = threadIdx.x % TPR;
   float(*red)[kSums][kRowWaves<TPR>] = shared[threadIdx.x / TPR];
-  const uint64_t row0 = (uint64_t)blockIdx.x * ROWS + threadIdx.x / TPR, all = (uint64_t)g.workers * g.in.rows;
+  const uint64_t row0 = ((uint64_t)g.first + blockIdx.x) * ROWS + threadIdx.x / TPR, all = (uint64_t)g.workers * g.in.rows;
   const bool real = row0 < all;
   const uint64_t row = real ? row0 : all - 1;       // all threads of a workgroup meet at its barriers
   const uint32_t w = (uint32_t)(row / g.in.rows), t = (uint32_t)(row % g.in.rows);
@@ -308,7 +309,7 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
   __shared__ float red[2][kSums][TPR / 64];
   int turn = 0;
   const int lane = threadIdx.x;
-  const uint32_t w = blockIdx.x / g.stripes, stripe = blockIdx.x % g.stripes;
+  const uint32_t block = g.first + blockIdx.x, w = block / g.stripes, stripe = block % g.stripes;
   const int width = (int)g.width;
   uint32_t t0, t1;
   if (g.group_stripes) {
@@ -490,12 +491,12 @@ constexpr int kJoinWaves = 16;
 template <typename T>
 __global__ __launch_bounds__(kJoinWaves * 64) void k_blocknorm_join(NormArgs g, uint32_t groups) {
   __shared__ float part[kJoinWaves][64];
-  const uint32_t blocks = (g.width + 63) / 64, cell = blockIdx.x / blocks;   // cells: worker x (four weights, then the gate's groups)
+  const uint32_t block = g.first + blockIdx.x, blocks = (g.width + 63) / 64, cell = block / blocks;   // cells: worker x (four weights, then the gate's groups)
   const uint32_t w = cell / (4 + groups), which = cell % (4 + groups);
   const evg_mat& out = which == 0 ? g.d.pre : which == 1 ? g.d.pre_bias : which == 2 ? g.d.post : which == 3 ? g.d.post_bias : g.d.gate;
   if (!out.p) return;
   const uint32_t s0 = which < 4 ? 0 : (which - 4) * g.group_stripes, s1 = which < 4 ? g.stripes : s0 + g.group_stripes;
-  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x % blocks * 64 + lane;
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = block % blocks * 64 + lane;
   float sum = 0.f;
   if (c < g.padded) {
     const float* p = g.partials + ((uint64_t)w * g.stripes * 5 + min(which, 4u)) * g.padded + c;
@@ -511,10 +512,13 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_blocknorm_join(NormArgs g, 
 }
 
 template <typename T, int NV, int TPR, bool LAYER>
-hipError_t forward_sized(const NormArgs& g, hipStream_t s) {
+hipError_t forward_sized(NormArgs g, hipStream_t s) {
   constexpr int rows = TPR < 256 ? 256 / TPR : 1;
   const uint64_t all = (uint64_t)g.workers * g.in.rows;
-  k_blocknorm_forward<T, NV, TPR, LAYER><<<(uint32_t)((all + rows - 1) / rows), TPR * rows, 0, s>>>(g);
+  launch_pieces((all + rows - 1) / rows, TPR * rows, [&](uint32_t first, uint32_t grid) {
+    g.first = first;
+    k_blocknorm_forward<T, NV, TPR, LAYER><<<grid, TPR * rows, 0, s>>>(g);
+  });
   return hipGetLastError();
 }
 
@@ -531,16 +535,21 @@ hipError_t launch_forward(const NormArgs& g, hipStream_t s) {
 }
 
 template <typename T, bool LAYER, int GATED, int POST>
-hipError_t backward_sized(const NormArgs& g, hipStream_t s) {
-  const uint32_t grid = g.workers * g.stripes;
-  if (!grid) return hipSuccess;
-  if (g.width <= 512) k_blocknorm_backward<T, 1, 64, LAYER, GATED, POST><<<grid, 64, 0, s>>>(g);
-  else if (g.width <= 1024) k_blocknorm_backward<T, 1, 128, LAYER, GATED, POST><<<grid, 128, 0, s>>>(g);
-  else if (g.width <= 2048) k_blocknorm_backward<T, 1, 256, LAYER, GATED, POST><<<grid, 256, 0, s>>>(g);
-  else if (g.width <= 4096) k_blocknorm_backward<T, 1, 512, LAYER, GATED, POST><<<grid, 512, 0, s>>>(g);
-  else if (g.width <= 8192) k_blocknorm_backward<T, 1, 1024, LAYER, GATED, POST><<<grid, 1024, 0, s>>>(g);
-  else k_blocknorm_backward<T, 2, 1024, LAYER, GATED, POST><<<grid, 1024, 0, s>>>(g);
-  return hipGetLastError();
+hipError_t backward_sized(NormArgs g, hipStream_t s) {
+  auto launch = [&](auto kernel, uint32_t threads) {
+    launch_pieces((uint64_t)g.workers * g.stripes, threads, [&](uint32_t first, uint32_t grid) {
+      g.first = first;
+      kernel<<<grid, threads, 0, s>>>(g);
+    });
+    return hipGetLastError();
+  };
+  if (!g.stripes) return hipSuccess;
+  if (g.width <= 512) return launch(k_blocknorm_backward<T, 1, 64, LAYER, GATED, POST>, 64);
+  if (g.width <= 1024) return launch(k_blocknorm_backward<T, 1, 128, LAYER, GATED, POST>, 128);
+  if (g.width <= 2048) return launch(k_blocknorm_backward<T, 1, 256, LAYER, GATED, POST>, 256);
+  if (g.width <= 4096) return launch(k_blocknorm_backward<T, 1, 512, LAYER, GATED, POST>, 512);
+  if (g.width <= 8192) return launch(k_blocknorm_backward<T, 1, 1024, LAYER, GATED, POST>, 1024);
+  return launch(k_blocknorm_backward<T, 2, 1024, LAYER, GATED, POST>, 1024);
 }
 
 template <typename T, bool LAYER>
@@ -551,13 +560,16 @@ hipError_t launch_backward(const NormArgs& g, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t launch_blocknorm(const NormArgs& g, uint32_t kind, bool backward, hipStream_t s) {
+hipError_t launch_blocknorm(NormArgs g, uint32_t kind, bool backward, hipStream_t s) {
   if (!backward) return kind == EVG_NORM_LAYER ? launch_forward<T, true>(g, s) : launch_forward<T, false>(g, s);
   const hipError_t e = kind == EVG_NORM_LAYER ? launch_backward<T, true>(g, s) : launch_backward<T, false>(g, s);
   if (e != hipSuccess) return e;
   const uint32_t groups = g.d.gate.p && g.group_stripes ? g.stripes / g.group_stripes : 0;
   if (!g.d.pre.p && !g.d.pre_bias.p && !g.d.post.p && !g.d.post_bias.p && !groups) return hipSuccess;
-  k_blocknorm_join<T><<<(g.width + 63) / 64 * g.workers * (4 + groups), kJoinWaves * 64, 0, s>>>(g, groups);
+  launch_pieces((uint64_t)((g.width + 63) / 64) * g.workers * (4 + groups), kJoinWaves * 64, [&](uint32_t first, uint32_t grid) {
+    g.first = first;
+    k_blocknorm_join<T><<<grid, kJoinWaves * 64, 0, s>>>(g, groups);
+  });
   return hipGetLastError();
 }
 

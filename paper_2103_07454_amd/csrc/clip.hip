@@ -31,6 +31,7 @@ struct ClipTables {
   uint64_t pitch;        // elements of a worker's slice
   double* partials;      // [P][nchunks]
   float* factor;         // [P], where a launch of its own finds them
+  uint32_t first;        // workgroup of a launch in pieces
 };
 
 struct ClipCall {
@@ -55,7 +56,7 @@ template <typename T>
 __global__ __launch_bounds__(kClipThreads) void k_clip_squares(ClipTables t, const T* __restrict__ grad) {
   constexpr int E = 16 / sizeof(T), U = 8;
   __shared__ double part[kClipThreads / 64];
-  const uint32_t r = blockIdx.x / t.nchunks, c = blockIdx.x % t.nchunks;
+  const uint32_t block = t.first + blockIdx.x, r = block / t.nchunks, c = block % t.nchunks;
   const ClipChunk d = t.chunks[c];
   const T* g = grad + (uint64_t)r * t.pitch + d.off;
   double sum[2] = {0.0, 0.0};
@@ -96,15 +97,16 @@ __device__ __forceinline__ float clip_factor(const ClipTables& t, const ClipCall
 
 __global__ __launch_bounds__(kClipThreads) void k_clip_factor(ClipTables t, ClipCall call) {
   __shared__ double part[kClipThreads / 64];
-  const float f = clip_factor(t, call, blockIdx.x, part, call.norm);
-  if (threadIdx.x == 0) t.factor[blockIdx.x] = f;
+  const uint32_t r = t.first + blockIdx.x;
+  const float f = clip_factor(t, call, r, part, call.norm);
+  if (threadIdx.x == 0) t.factor[r] = f;
 }
 
 template <typename T, typename U, bool OWN>
 __global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipTables t, ClipCall call, const T* __restrict__ grad, U* __restrict__ out, bool in_place) {
   constexpr int E = 16 / sizeof(U), N = 8;
   __shared__ double part[OWN ? kClipThreads / 64 : 1];
-  const uint32_t r = blockIdx.x / t.nchunks, c = blockIdx.x % t.nchunks;
+  const uint32_t block = t.first + blockIdx.x, r = block / t.nchunks, c = block % t.nchunks;
   const float f = OWN ? clip_factor(t, call, r, part, c == 0 ? call.norm : nullptr) : t.factor[r];
   if (in_place && f == 1.f) return;
   const bool zero = call.zero_nonfinite && f == 0.f;   // also where an element is not finite
@@ -133,14 +135,20 @@ __global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipTables t, ClipC
 }
 
 template <typename T, typename U>
-hipError_t launch_clip(const ClipTables& t, const ClipCall& call, const void* grad, void* out, hipStream_t s) {
-  const uint32_t grid = t.P * t.nchunks;
-  k_clip_squares<T><<<grid, kClipThreads, 0, s>>>(t, (const T*)grad);
+hipError_t launch_clip(ClipTables t, const ClipCall& call, const void* grad, void* out, hipStream_t s) {
+  auto launch = [&](uint64_t groups, auto kernel, auto... args) {
+    launch_pieces(groups, kClipThreads, [&](uint32_t first, uint32_t grid) {
+      t.first = first;
+      kernel<<<grid, kClipThreads, 0, s>>>(t, args...);
+    });
+  };
+  const uint64_t groups = (uint64_t)t.P * t.nchunks;
+  launch(groups, k_clip_squares<T>, (const T*)grad);
   if (t.nchunks <= kOwnSums) {
-    k_clip_scale<T, U, true><<<grid, kClipThreads, 0, s>>>(t, call, (const T*)grad, (U*)out, grad == out);
+    launch(groups, k_clip_scale<T, U, true>, call, (const T*)grad, (U*)out, grad == out);
   } else {
-    k_clip_factor<<<t.P, kClipThreads, 0, s>>>(t, call);
-    k_clip_scale<T, U, false><<<grid, kClipThreads, 0, s>>>(t, call, (const T*)grad, (U*)out, grad == out);
+    launch(t.P, k_clip_factor, call);
+    launch(groups, k_clip_scale<T, U, false>, call, (const T*)grad, (U*)out, grad == out);
   }
   return hipGetLastError();
 }

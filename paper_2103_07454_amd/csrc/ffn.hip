@@ -36,7 +36,7 @@ namespace {
 template <typename T>
 __global__ __launch_bounds__(256) void k_ffn_pack(PackArgs a) {
   constexpr int E = 16 / sizeof(T);
-  const uint64_t id = (uint64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t id = ((uint64_t)a.first + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (id >= a.lines) return;
   uint32_t k = 0;
   while (k + 1 < a.count && id >= a.one[k + 1].first) ++k;
@@ -60,12 +60,15 @@ __global__ __launch_bounds__(256) void k_ffn_pack(PackArgs a) {
 
 }  // namespace
 
-hipError_t launch_pack(uint32_t type, const PackArgs& a, hipStream_t s) {
+hipError_t launch_pack(uint32_t type, PackArgs a, hipStream_t s) {
   if (!a.lines) return hipSuccess;
-  const uint64_t grid = (a.lines + 3) / 4;
-  if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
-  if (type == EVG_F32) k_ffn_pack<float><<<(uint32_t)grid, 256, 0, s>>>(a);
-  else k_ffn_pack<half_t><<<(uint32_t)grid, 256, 0, s>>>(a);   // bits
+  const uint64_t groups = (a.lines + 3) / 4;
+  if (groups > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  launch_pieces(groups, 256, [&](uint32_t first, uint32_t grid) {
+    a.first = first;
+    if (type == EVG_F32) k_ffn_pack<float><<<grid, 256, 0, s>>>(a);
+    else k_ffn_pack<half_t><<<grid, 256, 0, s>>>(a);   // bits
+  });
   return hipGetLastError();
 }
 

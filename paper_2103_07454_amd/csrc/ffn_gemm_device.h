@@ -230,9 +230,9 @@ __device__ __forceinline__ void wait_and_meet() {
 }
 
 // Workgroups go to the eight XCDs in turn.  Each XCD gets a contiguous part of the tiles' order, so that what they share lies in its own L2.
-__device__ __forceinline__ uint32_t place_by_xcd() {
+__device__ __forceinline__ uint32_t place_by_xcd(const GemmArgs& g) {
   const uint32_t x = blockIdx.x & 7, each = gridDim.x >> 3, more = gridDim.x & 7;
-  return x * each + min(x, more) + (blockIdx.x >> 3);
+  return g.first + x * each + min(x, more) + (blockIdx.x >> 3);
 }
 
 template <typename T, int OP, bool ERF, int BM, int BN, int WAVES_M, int WAVES_N, bool ALIGNED>
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, BM == 64 ? 3 : 2) void k_ff
   // four rows' and eight columns' operands at a time (up to 7 % less time for the products of 8192 x 2048 x 8192 than bands of eight
   // rows, 20 % less than of sixteen).
   const uint32_t tiles = g.tiles_m * g.tiles_n;
-  uint32_t id = place_by_xcd();
+  uint32_t id = place_by_xcd(g);
   const uint32_t cell = id / tiles, part = cell % g.parts, w = cell / g.parts;
   id %= tiles;
   constexpr uint32_t BAND = 4;
@@ -468,6 +468,16 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, BM == 64 ? 3 : 2) void k_ff
   }
 }
 
+template <typename Kernel>
+hipError_t launch_groups(Kernel kernel, uint64_t groups, uint32_t threads, GemmArgs g, hipStream_t s) {
+  if (groups > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  launch_pieces(groups, threads, [&](uint32_t first, uint32_t grid) {
+    g.first = first;
+    kernel<<<grid, threads, 0, s>>>(g);
+  });
+  return hipGetLastError();
+}
+
 template <typename T, int OP, bool ERF>
 hipError_t launch_op(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) {
   constexpr uint32_t share = OP == GEMM_GATED ? 2 : 1;   // a tile's columns are gate's and up's
@@ -476,19 +486,16 @@ hipError_t launch_op(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) {
   // padding columns are written too where there are any
   const uint32_t n = OP == GEMM_GATED || OP == GEMM_GATED_BWD ? g.pitch : g.N;
   g.tiles_n = (n + bn - 1) / bn;
-  const uint64_t grid = (uint64_t)g.tiles_m * g.tiles_n * g.workers * g.parts;
-  if (!grid) return hipSuccess;
-  if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  const uint64_t groups = (uint64_t)g.tiles_m * g.tiles_n * g.workers * g.parts;
+  if (!groups) return hipSuccess;
   if constexpr (sizeof(T) == 2) {
     if constexpr (OP != GEMM_GATED_BWD) {   // which overlaps its reading and writing with a second workgroup's products
-      if (aligned && tile == TILE_256) { k_ffn_gemm<T, OP, ERF, 256, 256, 2, 4, true><<<(uint32_t)grid, 512, 0, s>>>(g); return hipGetLastError(); }
+      if (aligned && tile == TILE_256) return launch_groups(k_ffn_gemm<T, OP, ERF, 256, 256, 2, 4, true>, groups, 512, g, s);
     }
-    if (aligned && tile == TILE_128) { k_ffn_gemm<T, OP, ERF, 128, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g); return hipGetLastError(); }
+    if (aligned && tile == TILE_128) return launch_groups(k_ffn_gemm<T, OP, ERF, 128, 128, 2, 2, true>, groups, 256, g, s);
   }
   if (tile != TILE_64) return hipErrorInvalidValue;
-  if (aligned) k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, true><<<(uint32_t)grid, 256, 0, s>>>(g);
-  else k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, false><<<(uint32_t)grid, 256, 0, s>>>(g);
-  return hipGetLastError();
+  return launch_groups(aligned ? k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, true> : k_ffn_gemm<T, OP, ERF, 64, 128, 2, 2, false>, groups, 256, g, s);
 }
 
 }  // namespace evg

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "launch_pieces.h"
+
 namespace evg {
 
 enum GemmOp : uint32_t {
@@ -30,6 +32,7 @@ struct GemmArgs {
   GemmOperand a[2], b[2], c[2];   // phases of the product (GEMM_INPUT), gate and up (GEMM_GATED), or parts (GEMM_WEIGHT)
   uint32_t M, N, K, workers, parts;
   uint32_t tiles_m, tiles_n;
+  uint32_t first;                  // workgroup of a launch in pieces
   Activation activation;
   // GEMM_GATED, GEMM_GATED_BWD: the projections in 32 bits, in the accumulators' order; the gradients are rows of c[0], gate's at 0, up's at `pitch`
   float* proj;
@@ -51,10 +54,10 @@ struct PackOne {
 };
 struct PackArgs {
   PackOne one[4];
-  uint32_t count;
+  uint32_t count, first;           // first workgroup of a launch in pieces
   uint64_t lines;
 };
-hipError_t launch_pack(uint32_t type, const PackArgs& a, hipStream_t s);
+hipError_t launch_pack(uint32_t type, PackArgs a, hipStream_t s);
 
 template <typename T> hipError_t launch_gemm(GemmOp op, GemmTile tile, bool aligned, const GemmArgs& g, hipStream_t s);
 

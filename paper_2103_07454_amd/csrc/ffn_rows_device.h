@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void k_ffn_rows(GemmArgs g) {
   constexpr int AHEAD = EIGHT ? (B == 2 ? 4 : 6) : G == 1 ? 4 : 2;
   __shared__ f32x4 sums[kRowWaves][B * G][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t groups = g.tiles_n, w = blockIdx.x / groups, n0 = blockIdx.x % groups * COLS;
+  const uint32_t block = g.first + blockIdx.x, groups = g.tiles_n, w = block / groups, n0 = block % groups * COLS;
   const int row = lane & (COLS - 1), quarter = lane >> 4, within = quarter * E + (EIGHT ? (lane >> 3 & 1) * (STEP / 2) : 0);   // of a step's k
   // A fragment's lane has 16 bytes of one row.  Rows that there are not read the last one's, and what comes of them is not stored.
   const T* wp[B];
@@ -167,14 +167,12 @@ hipError_t launch_rows(GemmArgs g, hipStream_t s) {
   const bool eight = g.M <= 8;
   const uint32_t cols = eight ? 8 : 16;
   g.tiles_n = ((OP == GEMM_GATED ? g.pitch : g.N) + cols - 1) / cols;
-  const uint64_t grid = (uint64_t)g.tiles_n * g.workers;
-  if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  const uint64_t groups = (uint64_t)g.tiles_n * g.workers;
   constexpr int waves = OP == GEMM_GATED ? 8 : 16;   // columns of gate and of up, or of one product: as many loads
-  if (eight) k_ffn_rows<T, OP, ERF, 1, waves, true><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
-  else if (g.M <= 16) k_ffn_rows<T, OP, ERF, 1, waves, false><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
-  else if (g.M <= 32) k_ffn_rows<T, OP, ERF, 2, waves, false><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
-  else k_ffn_rows<T, OP, ERF, 4, waves, false><<<(uint32_t)grid, waves * 64, 0, s>>>(g);
-  return hipGetLastError();
+  if (eight) return launch_groups(k_ffn_rows<T, OP, ERF, 1, waves, true>, groups, waves * 64, g, s);
+  if (g.M <= 16) return launch_groups(k_ffn_rows<T, OP, ERF, 1, waves, false>, groups, waves * 64, g, s);
+  if (g.M <= 32) return launch_groups(k_ffn_rows<T, OP, ERF, 2, waves, false>, groups, waves * 64, g, s);
+  return launch_groups(k_ffn_rows<T, OP, ERF, 4, waves, false>, groups, waves * 64, g, s);
 }
 
 template <typename T>

@@ -17,7 +17,7 @@ __global__ __launch_bounds__(kSplit * 64) void k_ffn_small(GemmArgs g) {
   __shared__ u32x4 lds0[kSplit][UNITS], lds1[kSplit][UNITS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t tiles = g.tiles_m * g.tiles_n;
-  const uint32_t place = place_by_xcd(), cell = place / tiles, part = cell % g.parts, w = cell / g.parts, id = place % tiles;
+  const uint32_t place = place_by_xcd(g), cell = place / tiles, part = cell % g.parts, w = cell / g.parts, id = place % tiles;
   const uint32_t m0 = id % g.tiles_m * (32 * TM), n0 = id / g.tiles_m * (OP == GEMM_GATED ? 32 : 32 * TN);
 
   Loader<T, 32 * TM, AKC, 1, ALIGNED, false> la;
@@ -195,19 +195,13 @@ hipError_t launch_small(GemmTile tile, bool aligned, GemmArgs g, hipStream_t s) 
   const uint32_t n = OP == GEMM_GATED || OP == GEMM_GATED_BWD ? g.pitch : g.N, bm = square ? 64 : 32, bn = OP == GEMM_GATED || narrow ? 32 : 64;
   g.tiles_m = (g.M + bm - 1) / bm;
   g.tiles_n = (n + bn - 1) / bn;
-  const uint64_t grid = (uint64_t)g.tiles_m * g.tiles_n * g.workers * g.parts;
-  if (!grid) return hipSuccess;
-  if (grid > 0x7FFFFFFFull) return hipErrorInvalidValue;
-  if (square) {
-    k_ffn_small<T, OP, ERF, 2, 2, 4, true><<<(uint32_t)grid, 256, 0, s>>>(g);
-  } else if (!narrow) {
-    if (aligned) k_ffn_small<T, OP, ERF, 1, 2, 4, true><<<(uint32_t)grid, 256, 0, s>>>(g);
-    else k_ffn_small<T, OP, ERF, 1, 2, 4, false><<<(uint32_t)grid, 256, 0, s>>>(g);
-  } else if constexpr (OP != GEMM_GATED) {
-    if (aligned) k_ffn_small<T, OP, ERF, 1, 1, 8, true><<<(uint32_t)grid, 512, 0, s>>>(g);
-    else k_ffn_small<T, OP, ERF, 1, 1, 8, false><<<(uint32_t)grid, 512, 0, s>>>(g);
+  const uint64_t groups = (uint64_t)g.tiles_m * g.tiles_n * g.workers * g.parts;
+  if (!groups) return hipSuccess;
+  if (square) return launch_groups(k_ffn_small<T, OP, ERF, 2, 2, 4, true>, groups, 256, g, s);
+  if constexpr (OP != GEMM_GATED) {
+    if (narrow) return launch_groups(aligned ? k_ffn_small<T, OP, ERF, 1, 1, 8, true> : k_ffn_small<T, OP, ERF, 1, 1, 8, false>, groups, 512, g, s);
   }
-  return hipGetLastError();
+  return launch_groups(aligned ? k_ffn_small<T, OP, ERF, 1, 2, 4, true> : k_ffn_small<T, OP, ERF, 1, 2, 4, false>, groups, 256, g, s);
 }
 
 }  // namespace evg

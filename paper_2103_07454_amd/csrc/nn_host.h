@@ -4,6 +4,7 @@
 
 #include "../../include/evg_nn.h"
 #include "evg_host.h"
+#include "launch_pieces.h"
 
 namespace evg {
 
