@@ -86,6 +86,8 @@ typedef struct {
   uint32_t kind;       /* EVG_NORM_RMS or EVG_NORM_LAYER         */
   float eps;           /* >= 0                                   */
   float residual_scale, branch_scale; /* finite                  */
+  uint32_t forward_only; /* nonzero: backward will not be called; the sums that it keeps (a few thousand rows of D in 32 bits) are not
+                            allocated                            */
 } evg_blocknorm_config;
 #define EVG_BLOCKNORM_MAX_WIDTH 16384u
 

@@ -40,10 +40,14 @@ struct NormArgs {
   // backward: stripes of rows
   uint32_t stripes, stripe_rows;         // of a worker
   uint32_t group_stripes;                // stripes of a gate's group; 0: a stripe has whole groups
-  float* partials;                       // [workers][stripes][5][padded width]: pre, pre_bias, post, post_bias, gate
+  float* partials;                       // [workers][stripes][slots][padded width]: pre, pre_bias, post, post_bias, gate; RMS: no biases
+  uint32_t slots;
   uint32_t padded;
   uint32_t first;                        // workgroup of a launch in pieces
 };
+
+// Rows of sums that a stripe leaves: of both weights, the gate and a layer norm's biases.
+__host__ __device__ constexpr uint32_t slots_of(bool layer) { return layer ? 5 : 3; }
 
 template <typename T>
 __device__ __forceinline__ T* at(const evg_mat& m, uint32_t w, uint64_t row) {
@@ -477,13 +481,14 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
       o_b.next();
     }
   }
-  float* p = g.partials + ((uint64_t)w * g.stripes + stripe) * 5 * g.padded;
+  constexpr int SLOTS = slots_of(LAYER), P_POST = LAYER ? 2 : 1;
+  float* p = g.partials + ((uint64_t)w * g.stripes + stripe) * SLOTS * g.padded;
   const int padded = (int)g.padded;   // a multiple of 64
   if (g.d.pre.p) put_row<true, NV, TPR>(p, padded, lane, s_pre);
   if (LAYER && g.d.pre_bias.p) put_row<true, NV, TPR>(p + padded, padded, lane, s_prebias);
-  if (g.d.post.p) put_row<true, NV, TPR>(p + 2 * padded, padded, lane, s_post);
+  if (g.d.post.p) put_row<true, NV, TPR>(p + P_POST * padded, padded, lane, s_post);
   if (LAYER && g.d.post_bias.p) put_row<true, NV, TPR>(p + 3 * padded, padded, lane, s_postbias);
-  if (g.d.gate.p && g.group_stripes) put_row<true, NV, TPR>(p + 4 * padded, padded, lane, s_gate);
+  if (g.d.gate.p && g.group_stripes) put_row<true, NV, TPR>(p + (SLOTS - 1) * padded, padded, lane, s_gate);
 }
 
 // Adds the stripes' shares, in their order: 64 columns to a workgroup, each of its wavefronts has every 16th stripe.
@@ -499,9 +504,10 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_blocknorm_join(NormArgs g, 
   const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = block % blocks * 64 + lane;
   float sum = 0.f;
   if (c < g.padded) {
-    const float* p = g.partials + ((uint64_t)w * g.stripes * 5 + min(which, 4u)) * g.padded + c;
+    const uint32_t slot = g.slots == slots_of(true) ? min(which, 4u) : min(which, 4u) / 2;
+    const float* p = g.partials + ((uint64_t)w * g.stripes * g.slots + slot) * g.padded + c;
 #pragma unroll 8
-    for (uint32_t s = s0 + wave; s < s1; s += kJoinWaves) sum += p[(uint64_t)s * 5 * g.padded];
+    for (uint32_t s = s0 + wave; s < s1; s += kJoinWaves) sum += p[(uint64_t)s * g.slots * g.padded];
   }
   part[wave][lane] = sum;
   __syncthreads();
@@ -635,6 +641,7 @@ NormArgs norm_args(const evg_blocknorm* c, const evg_blocknorm_in* in) {
   g.beta = c->cfg.branch_scale;
   g.inv_width = (float)(1.0 / c->cfg.width);
   g.partials = c->partials;
+  g.slots = slots_of(c->cfg.kind == EVG_NORM_LAYER);
   g.padded = c->padded;
   return g;
 }
@@ -660,10 +667,13 @@ evg_status evg_blocknorm_init(evg_blocknorm** out, const evg_blocknorm_config* c
   c->cfg = *cfg;
   c->stream = static_cast<hipStream_t>(hip_stream);
   c->padded = (cfg->width + 63) / 64 * 64;
-  // Stripes of whole gate groups are at least half as long as those asked for, and a group's last one may be short (backward).
+  // Stripes that fit the gate's groups (backward) are at most twice as many as those asked for, s = ceil(rows / n) of n rows.  Whole groups to a
+  // stripe: more than n / 2 rows.  a groups of g > n rows in b stripes each: s >= (a - 1)(b - 1) + 1, and a b is at most twice that where a and b
+  // are 2 or more; a = 1 is b = s.
   const uint64_t per = ((uint64_t)most_stripes(cfg->workers, cfg->width) + cfg->workers - 1) / cfg->workers;
-  c->max_stripes = 3 * (per < cfg->max_rows ? per : cfg->max_rows) + 2;
-  const hipError_t e = hipMalloc((void**)&c->partials, cfg->workers * c->max_stripes * 5 * c->padded * sizeof(float));
+  c->max_stripes = 2 * (per < cfg->max_rows ? per : cfg->max_rows);
+  const uint64_t bytes = cfg->workers * c->max_stripes * slots_of(cfg->kind == EVG_NORM_LAYER) * c->padded * sizeof(float);
+  const hipError_t e = cfg->forward_only || !bytes ? hipSuccess : hipMalloc((void**)&c->partials, bytes);
   if (e != hipSuccess) {
     delete c;
     return fail(e == hipErrorOutOfMemory ? EVG_ERR_OOM : EVG_ERR_HIP, "workspace: %s", hipGetErrorString(e));
@@ -700,6 +710,7 @@ evg_status evg_blocknorm_forward(evg_blocknorm* c, const evg_blocknorm_in* in, c
 evg_status evg_blocknorm_backward(evg_blocknorm* c, const evg_blocknorm_in* in, const evg_mat* d_residual, const evg_mat* d_normed,
                                   const evg_blocknorm_grads* out) {
   if (!c || !in || !out) return fail(EVG_ERR_INVALID, "context, in and out must be non-NULL");
+  if (c->cfg.forward_only) return fail(EVG_ERR_STATE, "the context was made forward_only");
   evg_status st = check_norm_in(c, in);
   if (st != EVG_OK) return st;
   const uint32_t W = c->cfg.workers, D = c->cfg.width, ty = c->cfg.type;

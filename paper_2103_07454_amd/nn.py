@@ -42,7 +42,8 @@ class ClipConfig(C.Structure):
 
 class BlockNormConfig(C.Structure):
     _fields_ = [("workers", C.c_uint32), ("width", C.c_uint32), ("max_rows", C.c_uint32), ("type", C.c_uint32),
-                ("kind", C.c_uint32), ("eps", C.c_float), ("residual_scale", C.c_float), ("branch_scale", C.c_float)]
+                ("kind", C.c_uint32), ("eps", C.c_float), ("residual_scale", C.c_float), ("branch_scale", C.c_float),
+                ("forward_only", C.c_uint32)]
 
 
 _INPUTS = ("residual", "branch", "gate", "post", "post_bias", "pre", "pre_bias")
@@ -203,19 +204,19 @@ class BlockNorm(_Operator):
     """``residual' = residual_scale * residual + branch_scale * gate * N(branch; post)`` and ``normed = N(residual'; pre)``.
 
     ``kind``: ``RMS`` or ``LAYER``.  ``gate_rows`` tokens share a row of the gate (0: there is none).  Which norms there are
-    follows from the weights that a call is given.  [workers, rows, width]: residual, branch; [workers, ceil(rows /
+    follows from the weights that a call is given.  Without ``train`` there is no ``backward``, nor the memory for its sums.  [workers, rows, width]: residual, branch; [workers, ceil(rows /
     gate_rows), width]: gate; [workers, width]: weights and biases.
     """
 
     _destroy = "evg_blocknorm_destroy"
 
     def __init__(self, width, *, workers=1, max_rows, dtype=torch.bfloat16, kind=RMS, eps=1e-6, residual_scale=1.0,
-                 branch_scale=1.0, gate_rows=0, device="cuda", stream=None):
+                 branch_scale=1.0, gate_rows=0, train=True, device="cuda", stream=None):
         self._open(dtype, device, stream)
         self.width, self.workers, self.max_rows, self.gate_rows = int(width), int(workers), int(max_rows), int(gate_rows)
         self._keeps = residual_scale == 1.0
         self._make(lib().evg_blocknorm_init, BlockNormConfig(self.workers, self.width, self.max_rows, _TYPES[dtype], kind, eps,
-                                                             residual_scale, branch_scale))
+                                                             residual_scale, branch_scale, not train))
 
     def _in(self, residual, branch, gate, post, post_bias, pre, pre_bias):
         """The shapes of tokens, the gate and weights, and the inputs as the library takes them."""
