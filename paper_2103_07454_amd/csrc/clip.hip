@@ -22,7 +22,9 @@ constexpr int kClipThreads = 256;
 // Up to so many sums, each workgroup that writes adds up its worker's for itself (a load or two for each thread); more are added by a launch between.
 constexpr uint32_t kOwnSums = 512;
 
-// A run of elements of a worker's slice without padding in it.
+constexpr int kMostChunk = 8192;
+
+// A run of at most kMostChunk elements of a worker's slice without padding in it.
 struct ClipChunk { uint32_t off, len; };   // off: a multiple of 4
 
 struct ClipTables {
@@ -61,14 +63,16 @@ __global__ __launch_bounds__(kClipThreads) void k_clip_squares(ClipTables t, con
   const T* g = grad + (uint64_t)r * t.pitch + d.off;
   double sum[2] = {0.0, 0.0};
   uint32_t j = threadIdx.x * E;
-  for (; j + (U - 1) * kClipThreads * E + E <= d.len; j += U * kClipThreads * E) {   // U loads under way at once
-    float v[U][E];
+  if constexpr (U * kClipThreads * E <= kMostChunk) {   // 32 bits: a whole chunk's loads are under way at once
+    for (; j + (U - 1) * kClipThreads * E + E <= d.len; j += U * kClipThreads * E) {
+      float v[U][E];
 #pragma unroll
-    for (int u = 0; u < U; ++u) load_n<E>(g + j + u * kClipThreads * E, v[u]);
+      for (int u = 0; u < U; ++u) load_n<E>(g + j + u * kClipThreads * E, v[u]);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < E; ++i) sum[i & 1] = fma((double)v[u][i], (double)v[u][i], sum[i & 1]);
+        for (int i = 0; i < E; ++i) sum[i & 1] = fma((double)v[u][i], (double)v[u][i], sum[i & 1]);
+    }
   }
   for (; j < d.len; j += kClipThreads * E) {
     float v[E];
@@ -114,15 +118,17 @@ __global__ __launch_bounds__(kClipThreads) void k_clip_scale(ClipTables t, ClipC
   const T* g = grad + (uint64_t)r * t.pitch + d.off;
   U* o = out + (uint64_t)r * t.pitch + d.off;
   uint32_t j = threadIdx.x * E;
-  for (; j + (N - 1) * kClipThreads * E + E <= d.len; j += N * kClipThreads * E) {
-    float v[N][E];
+  if constexpr (N * kClipThreads * E <= kMostChunk) {   // results of 32 bits
+    for (; j + (N - 1) * kClipThreads * E + E <= d.len; j += N * kClipThreads * E) {
+      float v[N][E];
 #pragma unroll
-    for (int u = 0; u < N; ++u) load_n_once<E>(g + j + u * kClipThreads * E, v[u]);
+      for (int u = 0; u < N; ++u) load_n_once<E>(g + j + u * kClipThreads * E, v[u]);
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
+      for (int u = 0; u < N; ++u) {
 #pragma unroll
-      for (int i = 0; i < E; ++i) v[u][i] = zero ? 0.f : v[u][i] * f;
-      store_n_once<E>(o + j + u * kClipThreads * E, v[u]);
+        for (int i = 0; i < E; ++i) v[u][i] = zero ? 0.f : v[u][i] * f;
+        store_n_once<E>(o + j + u * kClipThreads * E, v[u]);
+      }
     }
   }
   for (; j < d.len; j += kClipThreads * E) {
@@ -183,7 +189,7 @@ evg_status evg_clip_init(evg_clip** out, const evg_clip_config* cfg, void* hip_s
   try {
     std::vector<ClipChunk> chunks;
     // Tensors whose length is a multiple of 4 run into the next one without padding.
-    const uint64_t most = (uint64_t)cfg->P * pitch <= (8u << 20) ? 2048 : 8192;
+    const uint64_t most = (uint64_t)cfg->P * pitch <= (8u << 20) ? 2048 : kMostChunk;
     uint64_t at = 0, begin = 0;
     for (uint32_t l = 0; l < cfg->L; ++l) {
       at += cfg->layer_numel[l];
