@@ -305,8 +305,9 @@ class GatedFFN(_Operator):
         return (out, saved) if save else out
 
     def backward(self, dy, x, w_gate, w_up, w_down, saved, *, dx=None, dw_gate=None, dw_up=None, dw_down=None,
-                 input_gradient=True):
-        """``(dx, dw_gate, dw_up, dw_down)``; ``dx`` is None without ``input_gradient``."""
+                 input_gradient=True, weight_gradients=True):
+        """``(dx, dw_gate, dw_up, dw_down)``.  Only tensors that are given are filled, and the others None, without ``input_gradient``
+        for ``dx`` and without ``weight_gradients`` for the rest; what is not asked for is not computed."""
         rows = self._rows(x, self.width, "x")
         need = lib().evg_ffn_saved_bytes(self._h, rows)
         if saved.numel() * saved.element_size() != need or saved.device != self.device or not saved.is_contiguous():
@@ -314,9 +315,10 @@ class GatedFFN(_Operator):
         weights = self._weights(w_gate, w_up, w_down)
         if dx is None and input_gradient:
             dx = self._like(x)
-        grads = [self._like(w) if d is None else d for d, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down))]
+        grads = [self._like(w) if d is None and weight_gradients else d for d, w in ((dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down))]
         evg._check(lib().evg_ffn_backward(
             self._h, rows, self._mat(dy, x.shape, "dy"), self._mat(x, x.shape, "x"), *weights, saved.data_ptr() or None,
             None if dx is None else self._mat(dx, x.shape, "dx"),
-            *(self._mat(d, w.shape, what) for d, w, what in zip(grads, (w_gate, w_up, w_down), ("dw_gate", "dw_up", "dw_down")))))
+            *(None if d is None else self._mat(d, w.shape, what)
+              for d, w, what in zip(grads, (w_gate, w_up, w_down), ("dw_gate", "dw_up", "dw_down")))))
         return (dx, *grads)
