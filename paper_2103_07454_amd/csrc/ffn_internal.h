@@ -3,18 +3,10 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "ffn_choose.h"
 #include "launch_pieces.h"
 
 namespace evg {
-
-enum GemmOp : uint32_t {
-  GEMM_GATED = 0,     // h = act(A Bg^T) * (A Bu^T), both K-contiguous; writes h and, for a backward pass, both projections
-  GEMM_DOWN = 1,      // C = A B^T, both K-contiguous
-  GEMM_GATED_BWD = 2, // dh = A B, B N-contiguous; writes the gradients of both projections
-  GEMM_INPUT = 3,     // C = A0 B0 + A1 B1, B N-contiguous
-  GEMM_WEIGHT = 4,    // C = A^T B, A M-contiguous, B N-contiguous; two of them at once
-  GEMM_OPS = 5
-};
 
 // a = x s(x): s the logistic function of x (c0 + c1 x^2), the step, or (erf) the normal distribution.
 struct Activation {
@@ -39,11 +31,6 @@ struct GemmArgs {
   uint64_t proj_worker;
   uint32_t pitch;                  // padded hidden width
 };
-
-// Tiles: 256 x 256 and 128 x 128 (aligned operands of 16 bits), 64 x 128; few tokens (GEMM_GATED and GEMM_DOWN of at most kMostRows); 32 x 64,
-// 32 x 32 and 64 x 64 (aligned) with k shared out among the wavefronts.
-enum GemmTile : uint32_t { TILE_256 = 0, TILE_128 = 1, TILE_64 = 2, TILE_ROWS = 3, TILE_SMALL = 4, TILE_SMALL_NARROW = 5, TILE_SMALL_SQUARE = 6 };
-constexpr uint32_t kMostRows = 64;
 
 // Copies of operands whose rows are no whole 16-byte units, with rows of `pitch` elements that are: zeros up to the next unit.
 struct PackOne {
