@@ -85,11 +85,17 @@ template <int CTRL, int ROWS>
 __device__ __forceinline__ float moved(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, false));
 }
+// Over each 2, 4, 8 or 16 lanes, in all of them: each adds the same pairs, so they get the same bits.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+  v += moved<0xB1, 0xf>(v);                               // lanes 1 0 3 2
+  if constexpr (LANES >= 4) v += moved<0x4E, 0xf>(v);     // lanes 2 3 0 1
+  if constexpr (LANES >= 8) v += moved<0x141, 0xf>(v);    // mirrored within 8
+  if constexpr (LANES >= 16) v += moved<0x140, 0xf>(v);   // mirrored within 16
+  return v;
+}
 __device__ __forceinline__ float wave_sum_uniform(float v) {
-  v += moved<0xB1, 0xf>(v);    // lanes 1 0 3 2
-  v += moved<0x4E, 0xf>(v);    // lanes 2 3 0 1
-  v += moved<0x141, 0xf>(v);   // mirrored within 8
-  v += moved<0x140, 0xf>(v);   // mirrored within 16
+  v = lanes_sum<16>(v);
   v += moved<0x142, 0xa>(v);   // row 0's into row 1, row 2's into row 3
   v += moved<0x143, 0xc>(v);   // the lower half's into the upper one
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
