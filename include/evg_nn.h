@@ -122,8 +122,11 @@ evg_status evg_blocknorm_destroy(evg_blocknorm* c);
  * For each worker, x of rows x D, w_gate and w_up of F x D, w_down of D x F (F = hidden):
  *     h = act(x w_gate^T) * (x w_up^T),   y = h w_down^T
  * h, and in the backward pass the gradients of both projections, are rounded to the tensors' type, as the matrix cores take them; all else
- * stays in 32 bits.  Rows are at most 2^31 elements apart.  Tensors whose addresses, strides and widths are multiples of 16 bytes are read
- * as they are; a width that is not is copied first where there are more than 64 tokens (init then allocates room for the copies). */
+ * stays in 32 bits.  With 16-bit types the activation's exponential and quotient are the hardware's, a few units of 2^-23 off.
+ * Rows are at most 2^31 elements apart.  Tensors whose addresses, strides and widths are multiples of 16 bytes are read as they are; a width that
+ * is not is copied first where there are more than 64 tokens (init then allocates room for the copies).  Tensors of whole widths at other addresses or
+ * strides, as at the offsets of 16-bit arenas (multiples of 4 elements), are not copied: a product that reads one takes all its operands
+ * through registers, which took up to 1.75 times as long.  That, and rows of 4 MB and more, is a matter of speed alone. */
 enum { EVG_ACT_SILU = 0, EVG_ACT_GELU = 1, EVG_ACT_GELU_TANH = 2, EVG_ACT_RELU = 3 };
 
 typedef struct evg_ffn evg_ffn;

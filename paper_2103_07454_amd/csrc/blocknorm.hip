@@ -355,7 +355,8 @@ __global__ __launch_bounds__(TPR) void k_blocknorm_backward(NormArgs g) {
   Lines<T> o_r(g.d.residual, w, t0), o_b(g.d.branch, w, t0);
   uint32_t gate_row = gated ? t0 / g.in.gate_rows : 0, until = gated ? (uint32_t)min((uint64_t)g.in.rows, (uint64_t)(gate_row + 1) * g.in.gate_rows) : 0;
   const float alpha = g.alpha, beta = g.beta, inv_width = g.inv_width;
-  // The next row's residual and branch, which its first sums need, are on their way while a row is finished (16 bits: there are registers for them).
+  // The next row's residual and branch, which its first sums need, are on their way while a row is finished, where a thread has 8 elements of it
+  // (of 16 there are no registers for them).
   constexpr bool AHEAD = NV == 1;
   Raw<T, NV> n_r, n_b;
   auto ask = [&]() {
@@ -555,6 +556,9 @@ hipError_t launch_forward(const NormArgs& g, hipStream_t s) {
   return forward_sized<T, 2, 1024, LAYER>(g, s);
 }
 
+// 1024 threads leave 128 registers to each, and that is not enough for the sums of every weight: of 4097 to 8192 elements most forms with a norm behind
+// the block spill some (up to 52, 157 where the width is no multiple of 8), above 8192 all do (up to 497).  2^25 elements of bf16, layer norms
+// and a gate, widths 4096 / 8192 / 8200: 166 / 212 / 910 us, of float32 229 / 447 / 1552.
 template <typename T, bool LAYER, int GATED, int POST>
 hipError_t backward_sized(NormArgs g, hipStream_t s) {
   auto launch = [&](auto kernel, uint32_t threads) {
@@ -618,7 +622,8 @@ namespace {
 // Stripes of all workers together, about.  A stripe is a workgroup, and the more wavefronts that has the fewer fill the chip; every one
 // leaves a row of sums for the join, which is the slower the more of them one worker has.  Backward and join, 1024 / 2048 / 4096 of them:
 // 16384 rows of 4096 179 / 190 / 222 us, of 1024 66 / 55 / 68; 8 x 2000 of 512 48 / 36 / 33; 11 x 5331 of 64 103 / 65 / 50; 1 x 16384 of 64
-// 40 / 36 / 43.
+// 40 / 36 / 43.  One worker's rows of at most 512 with 2048 / 4096: 4000 of 64 18 / 25, 16384 of 256 34 / 40 (float32 37 / 47), 6000 of 512 25 / 28,
+// 65536 of 512 96 / 104; only very many narrow ones are the other way, 100 000 of 64 111 / 99, 65536 of 256 85 / 78 (float32 101 / 109).
 uint32_t most_stripes(uint32_t workers, uint32_t width) { return width > 1024 ? 1024 : width > 512 || workers == 1 ? 2048 : 4096; }
 
 // Rows of a stripe such that there are about so many.

@@ -2,8 +2,9 @@
 //
 // With s the scale, for worker r:  norm = |s| sqrt(sum_j g_j^2) over all its tensors,  out_j = g_j * (s * min(1, max / (norm + eps))).
 // No product can be written before the last square is summed, so the gradient is read twice.  Both passes are bound by memory: 12 bytes an
-// element in 32 bits, 64 workers of 11 million elements in 1380 us, 6.2 TB/s.  What the second pass reads and writes is not read again and goes
-// past the caches (1521 us without).  Squaring and scaling by groups of workers, so that the second pass finds a group in the 256 MB
+// element in 32 bits, 64 workers of 11 million elements in 1390 to 1407 us, 6.1 TB/s.  What the second pass reads and writes of whole chunks of 8192 is
+// not read again and goes past the caches (1521 us without): results of 32 bits in arenas of more than 8 M elements.  Shorter chunks, which the
+// caches hold, and results of 16 bits go through them, a load at a time; so do the squares of 16 bits.  Squaring and scaling by groups of workers, so that the second pass finds a group in the 256 MB
 // last-level cache, is no faster: 1404 us in launches that square one group and scale the one before, 1564 in launches of their own.
 #include <hip/hip_runtime.h>
 

@@ -107,7 +107,8 @@ struct Packer {
   const evg_ffn* c;
   PackArgs a{};
   explicit Packer(const evg_ffn* ctx) : c(ctx) {}
-  // The operand, or its copy to be: products read the latter by whole units.
+  // The operand, or its copy to be: products read the latter by whole units.  There is room where the width is odd; what only begins beside a unit stays as
+  // it is (bf16, forward and backward, 8 bytes beside one: 1024 tokens 1024 x 4096 138 -> 213 us, 2048 tokens 2048 x 8192 688 -> 1205).
   GemmOperand take(const GemmOperand& o, void* room, uint32_t rows, uint32_t cols, uint32_t pitch) {
     if (!room || whole_units(o, cols, type_bytes(c->cfg.type))) return o;
     a.one[a.count++] = {o, room, rows, cols, pitch, a.lines};

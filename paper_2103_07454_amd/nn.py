@@ -8,6 +8,9 @@ Argument marshalling only, as in ``evg``: every operation runs in the library's 
 operator is bound to one stream (the current one when it is made, or the one given) and its calls only enqueue work there.
 Tensors that another stream made or will read have to be ordered against it by the caller, as with ``Ring``; outputs
 that a call allocates belong to the operator's stream.
+
+The operators are no part of torch's automatic differentiation: ``requires_grad`` of what they are given is ignored, their outputs carry
+no graph, and gradients come from ``backward`` alone.
 """
 from __future__ import annotations
 
