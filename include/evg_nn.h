@@ -3,7 +3,9 @@
  * Scope.  evg_step takes each worker's gradient (EVG_GRAD_BUFFER); these operators are what comes before it when the workers
  * train transformer feed-forward blocks: the norms on both sides of a block with its gate and residual scale (evg_blocknorm),
  * the gated feed-forward block (evg_ffn), both with their backward passes, and clipping by the global norm over a worker's
- * tensors (evg_clip).  All W workers of a ring, each with its own weights and tokens, go in one call; W = 1 is one model.
+ * tensors (evg_clip).  Tokens become rows of the residual stream (evg_embed); blocks of several experts need a router (evg_router) and
+ * tokens in the experts' order and back (evg_experts), all three with their backward passes; matrices' gradients become orthogonal
+ * updates (evg_ortho).  All W workers of a ring, each with its own weights and tokens, go in one call; W = 1 is one model.
  *
  * Conventions: those of evg.h (statuses, evg_error_text, the current device, one stream for each context, calls on one
  * context must not overlap).  Calls other than init and destroy only enqueue work on the context's stream, call no
@@ -153,6 +155,137 @@ evg_status evg_ffn_backward(evg_ffn* c, uint32_t rows, const evg_mat* dy, const 
                             const evg_mat* w_up, const evg_mat* w_down, const void* saved, const evg_mat* dx,
                             const evg_mat* dw_gate, const evg_mat* dw_up, const evg_mat* dw_down);
 evg_status evg_ffn_destroy(evg_ffn* c);
+
+/* ---- embeddings ------------------------------------------------------------------------------------------------------
+ * For each worker, a table of V x D (V = vocab, D = width) and T tokens:
+ *     y[t] = scale * table[id[t]],    d_table[v] = scale * sum of dy[t] over the tokens t with id[t] = v
+ * A token whose number is not in 0 .. V-1 (padding) has a row of zeros and no part in the gradient.  Sums are in 32 bits, over a number's tokens
+ * in their order. */
+typedef struct evg_embed evg_embed;
+
+typedef struct {
+  uint32_t workers;    /* 1 .. 65535                              */
+  uint32_t vocab;      /* V, 1 .. 2^24                            */
+  uint32_t width;      /* D, 1 .. 2^20                            */
+  uint32_t max_tokens; /* most tokens of a worker that a call has, <= 2^26 */
+  uint32_t type;       /* of table, rows and their gradients      */
+  float scale;         /* finite                                  */
+  uint32_t train;      /* nonzero: backward will be called        */
+} evg_embed_config;
+
+/* DEVICE token numbers: that of worker w's token t at p + w * worker + t, of 32 or (wide) 64 bits, signed. */
+typedef struct {
+  const void* p;
+  int64_t worker; /* in numbers, >= 0 */
+  uint32_t wide;
+} evg_ids;
+
+evg_status evg_embed_init(evg_embed** out, const evg_embed_config* cfg, void* hip_stream);
+evg_status evg_embed_forward(evg_embed* c, uint32_t tokens, const evg_ids* ids, const evg_mat* table, const evg_mat* y);
+/* accumulate: the sums are added to d_table (in 32 bits, rounded once) and rows that no token names are left as they are;
+ * otherwise those are 0. */
+evg_status evg_embed_backward(evg_embed* c, uint32_t tokens, const evg_ids* ids, const evg_mat* dy, const evg_mat* d_table, uint32_t accumulate);
+evg_status evg_embed_destroy(evg_embed* c);
+
+/* ---- which experts a token goes to --------------------------------------------------------------------------------------
+ * For each token, from E logits: the K experts with the largest, the largest first, equal ones in the order of their numbers, and
+ *     w = softmax(logits) at the chosen, or (over_chosen) the softmax over the chosen alone.
+ * An expert at minus infinity is never chosen: where there are fewer than K others, the last places have -1 and weight 0.  A NaN goes before
+ * all else, and makes the weights that the formula makes of it.  Backward, from dw:
+ *     d_logits = w (dw - sum w dw) at the chosen, 0 elsewhere (over_chosen),   or   p (dw - sum w dw),  p the softmax, dw = 0 elsewhere. */
+typedef struct evg_router evg_router;
+
+typedef struct {
+  uint32_t workers;    /* >= 1                                    */
+  uint32_t experts;    /* E, 1 .. EVG_ROUTER_MAX_EXPERTS          */
+  uint32_t top;        /* K, 1 .. E                               */
+  uint32_t max_tokens; /* most tokens of a worker that a call has */
+  uint32_t type;       /* of logits and their gradient            */
+  uint32_t over_chosen;
+} evg_router_config;
+#define EVG_ROUTER_MAX_EXPERTS 1024u
+
+evg_status evg_router_init(evg_router** out, const evg_router_config* cfg, void* hip_stream);
+/* logits: tokens x E for each worker.  chosen, weights: DEVICE, [workers][tokens][K]. */
+evg_status evg_router_forward(evg_router* c, uint32_t tokens, const evg_mat* logits, int32_t* chosen, float* weights);
+/* chosen: what forward wrote.  What d_weights has where chosen is -1 does not count. */
+evg_status evg_router_backward(evg_router* c, uint32_t tokens, const float* d_weights, const evg_mat* logits, const int32_t* chosen,
+                               const evg_mat* d_logits);
+evg_status evg_router_destroy(evg_router* c);
+
+/* ---- tokens by expert and back ----------------------------------------------------------------------------------------
+ * For each worker, T tokens with K experts each (chosen, T x K numbers): entry i = t K + k.  Entries are sorted by expert, those of one expert stay in
+ * their order, and each gets a slot:
+ *     capacity 0:  the slots 0 .. T K - 1 one after the other, expert by expert; those behind the last entry stay empty
+ *     capacity C:  expert e has the slots e C .. e C + C - 1; what exceeds them is left out
+ * Entries whose number is not in 0 .. E-1 are left out too.  With capacity C the rows of all experts are E matrices of C x D, as evg_ffn with W E
+ * workers takes them.
+ *     dispatch            rows[slot[i]] = x[t],  empty slots 0
+ *     combine             y[t] = sum_k weights[i] rows[slot[i]]                  (in 32 bits, in k's order; without weights: all 1)
+ *     combine_backward    d_rows[slot[i]] = weights[i] dy[t], empty slots 0;  d_weights[i] = <dy[t], rows[slot[i]]>, 0 where left out
+ * and the gradient of dispatch is combine without weights. */
+typedef struct evg_experts evg_experts;
+
+typedef struct {
+  uint32_t workers;    /* 1 .. 65535                              */
+  uint32_t experts;    /* E, 1 .. EVG_ROUTER_MAX_EXPERTS          */
+  uint32_t top;        /* K, 1 .. E                               */
+  uint32_t width;      /* D, 1 .. 2^20                            */
+  uint32_t max_tokens; /* most tokens of a worker that a call has; K times as many below 2^28 */
+  uint32_t capacity;   /* C, or 0; E C below 2^31                 */
+  uint32_t type;       /* of rows and their gradients             */
+} evg_experts_config;
+
+/* Where entries went: DEVICE, [workers][tokens][K], [workers][slots], [workers][E]. */
+typedef struct {
+  int32_t* slot;   /* -1: left out                                                       */
+  int32_t* source; /* the entry in a slot, -1: empty                                     */
+  int32_t* counts; /* entries of each expert, with those that found no room              */
+} evg_experts_plan;
+
+evg_status evg_experts_init(evg_experts** out, const evg_experts_config* cfg, void* hip_stream);
+/* Slots of each worker for so many tokens.  0 if c is NULL. */
+uint64_t evg_experts_slots(const evg_experts* c, uint32_t tokens);
+/* x: tokens x D; rows: slots x D.  The plan is written. */
+evg_status evg_experts_dispatch(evg_experts* c, uint32_t tokens, const evg_mat* x, const int32_t* chosen, const evg_mat* rows,
+                                const evg_experts_plan* plan);
+/* Only the plan's slots are read; weights may be NULL. */
+evg_status evg_experts_combine(evg_experts* c, uint32_t tokens, const evg_mat* rows, const float* weights, const evg_experts_plan* plan,
+                               const evg_mat* y);
+/* The plan's slots and sources are read.  d_rows or d_weights may be absent, rows is needed for d_weights only. */
+evg_status evg_experts_combine_backward(evg_experts* c, uint32_t tokens, const evg_mat* dy, const evg_mat* rows, const float* weights,
+                                        const evg_experts_plan* plan, const evg_mat* d_rows, float* d_weights);
+evg_status evg_experts_destroy(evg_experts* c);
+
+/* ---- orthogonal updates ------------------------------------------------------------------------------------------------
+ * For each of W matrices G of R x C:
+ *     m' = momentum * m + G,   u = G + momentum * m' (nesterov) or m'           (in 32 bits; without m: u = G)
+ *     X  = u / (|u| + eps),    |u| = sqrt(sum u^2)                             (sum in 64 bits)
+ *     steps times:  S = X X^T,  X <- a X + (b S + c S S) X                      (S = X^T X, X <- a X + X (b S + c S S) where R > C)
+ *     out = scale * X
+ * which takes every singular value s of X to p(s) = a s + b s^3 + c s^5, again and again: with the usual constants close to 1, singular vectors stay.
+ * Products are of float16 operands with sums in 32 bits.  X is kept as two of them, 22 bits; so are S and b S + c S S, and a product is three, in the last two
+ * steps with float16 tensors, in all steps with 32-bit ones.  What that leaves is below the rounding of a result of the tensors' type.  A zero matrix stays zero, a matrix with a NaN or an infinity becomes NaN. */
+typedef struct evg_ortho evg_ortho;
+
+typedef struct {
+  uint32_t matrices; /* W, 1 .. 65535                                                     */
+  uint32_t rows, cols; /* 1 .. 65536, the smaller of them at most 16384                   */
+  uint32_t type;     /* of G                                                              */
+  uint32_t out_type; /* type or EVG_F32; the products' precision goes by type             */
+  uint32_t steps;    /* 1 .. 64                                                           */
+  float a, b, c;     /* finite; constants under which a singular value of 0 .. 1 passes 3 are refused */
+  float momentum;    /* finite                                                            */
+  uint32_t nesterov;
+  float eps;         /* >= 0, finite                                                      */
+  float scale;       /* finite                                                            */
+} evg_ortho_config;
+
+evg_status evg_ortho_init(evg_ortho** out, const evg_ortho_config* cfg, void* hip_stream);
+/* momentum: float, R x C for each matrix, or absent; momentum_out: where m' goes, momentum itself or apart from it, given exactly if momentum is.
+ * out may be grad itself where the types are the same. */
+evg_status evg_ortho_update(evg_ortho* c, const evg_mat* grad, const evg_mat* momentum, const evg_mat* momentum_out, const evg_mat* out);
+evg_status evg_ortho_destroy(evg_ortho* c);
 
 #ifdef __cplusplus
 }

@@ -9,7 +9,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libevg.so")
 SOURCES = ["evg_api.hip", "kernels_update.hip", "kernels_walk.hip", "kernels_parts.hip", "kernels_ring.hip", "kernels_trigger.hip", "kernels_topk.hip", "kernels_choose.hip",
-           "clip.hip", "blocknorm.hip", "ffn.hip", "ffn_bf16.hip", "ffn_f16.hip", "ffn_f32.hip"]
+           "clip.hip", "blocknorm.hip", "ffn.hip", "ffn_bf16.hip", "ffn_f16.hip", "ffn_f32.hip",
+           "embed.hip", "router.hip", "experts.hip", "ortho.hip", "ortho_single.hip", "ortho_split.hip"]
 
 # -ffp-contract=off: every fused multiply-add in the kernels is written out, so
 #   results do not depend on what the compiler decides to contract.

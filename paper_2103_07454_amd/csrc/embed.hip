@@ -1,0 +1,498 @@
+// Embeddings and their gradient by sorted tokens (include/evg_nn.h, evg_embed_*).
+//
+//     y[t] = s table[id[t]],    d_table[v] = s sum over t with id[t] = v of dy[t]
+//
+// Forward: a wavefront takes 64 vectors of 16 bytes of one token's row.  Bound by memory, rows of the table in any order.
+//
+// Backward: the tokens are sorted by their number, those of one number stay in their order; then a wavefront adds up the rows of a
+// chunk of 32 sorted tokens, 64 vectors wide, and writes a sum where the number changes.  Numbers that go on in the next chunk leave partial sums in 32 bits,
+// which a launch behind adds in the chunks' order: no atomics, so the same tokens give the same bits, and a number that half of all
+// tokens have costs no more than others.  The rows that no token names are zeroed by the same launch; a bit for each number says which.
+// Bound by memory: dy once, the gradient's table once.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+
+#include "key_sort_device.h"
+#include "nn_device.h"
+#include "nn_host.h"
+
+namespace evg {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr uint32_t kChunk = 32;          // sorted tokens that a wavefront adds up
+constexpr int kOneWaves = 16;            // of the workgroup that sorts alone
+constexpr uint32_t kOneSort = 4096;      // most tokens of a worker that one workgroup sorts
+constexpr uint32_t kZeroRows = 4;        // rows that a wavefront may have to zero
+
+struct EmbedArgs {
+  const void* ids;
+  int64_t ids_worker;
+  uint32_t wide;
+  evg_mat table, rows;         // rows: y or dy
+  uint32_t workers, tokens, vocab, width, blocks;   // blocks: of 64 vectors across a row
+  float scale;
+  uint32_t accumulate;
+  uint32_t first;              // workgroup of a launch in pieces
+  // workspace
+  uint32_t *key[2], *pos[2];   // [workers][tokens]
+  uint32_t *counts;            // [workers][runs][bins]
+  uint32_t *real;              // [workers]: sorted tokens
+  uint32_t *seen;              // [workers][ceil(vocab / 32)]
+  float *partial;              // [workers][chunks][2][width]
+  uint32_t run, runs, bins, bits, shift, last;   // of a sorting pass
+  uint32_t chunks, sum_groups;
+};
+
+__device__ __forceinline__ uint32_t token_id(const EmbedArgs& a, uint32_t w, uint32_t t) {
+  const int64_t at = (int64_t)w * a.ids_worker + t;
+  const int64_t id = a.wide ? ((const int64_t*)a.ids)[at] : (int64_t)((const int32_t*)a.ids)[at];
+  return id >= 0 && id < (int64_t)a.vocab ? (uint32_t)id : 0xFFFFFFFFu;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedArgs a) {
+  constexpr int E = 16 / sizeof(T);
+  const uint64_t job = ((uint64_t)a.first + blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t line = job / a.blocks;
+  if (line >= (uint64_t)a.workers * a.tokens) return;
+  const uint32_t w = (uint32_t)(line / a.tokens), t = (uint32_t)(line % a.tokens);
+  const uint32_t col = (uint32_t)(job % a.blocks) * 64 * E + (threadIdx.x & 63) * E;
+  const int n = (int)a.width - (int)col;
+  if (n <= 0) return;
+  const uint32_t id = token_id(a, w, t);
+  float v[E] = {};
+  if (id != 0xFFFFFFFFu) load_upto<E>((const T*)a.table.p + (int64_t)w * a.table.worker + (int64_t)id * a.table.row + col, n, v);
+#pragma unroll
+  for (int i = 0; i < E; ++i) v[i] *= a.scale;
+  store_upto<E>((T*)a.rows.p + (int64_t)w * a.rows.worker + (int64_t)t * a.rows.row + col, n, v);
+}
+
+// ---- sorting -----------------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t seen_words(uint32_t vocab) { return (vocab + 31) / 32; }
+
+// A worker's tokens by one workgroup, digits of 8 bits from the lowest up, all in LDS.
+__global__ __launch_bounds__(kOneWaves * 64) void k_embed_sort_alone(EmbedArgs a, int bits) {
+  constexpr uint32_t BINS = 256;
+  __shared__ uint32_t key[2][kOneSort], pos[2][kOneSort], counts[kOneWaves * BINS], first[BINS], part[kOneWaves];
+  const uint32_t w = a.first + blockIdx.x, threads = kOneWaves * 64;
+  uint32_t* const seen = a.seen + (uint64_t)w * seen_words(a.vocab);
+  for (uint32_t i = threadIdx.x; i < seen_words(a.vocab); i += threads) seen[i] = 0;
+  __threadfence();   // before other threads' bits
+  uint32_t n = a.tokens;
+  int from = 0;
+  for (int shift = 0; shift == 0 || shift < bits; shift += 8, from ^= 1) {
+    for (uint32_t i = threadIdx.x; i < kOneWaves * BINS; i += threads) counts[i] = 0;
+    if (shift == 0)
+      for (uint32_t i = threadIdx.x; i < n; i += threads) {
+        key[0][i] = token_id(a, w, i);
+        pos[0][i] = i;
+      }
+    __syncthreads();
+    // Tokens outside the table are left out by the first pass.
+    auto digit = [&](uint32_t i) { return key[from][i] == 0xFFFFFFFFu ? BINS : key[from][i] >> shift & (BINS - 1); };
+    count_keys<kOneWaves>(counts + threadIdx.x / 64 * BINS, BINS, n, digit);
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < BINS; b += threads) {
+      uint32_t sum = 0;
+      for (int v = 0; v < kOneWaves; ++v) sum += counts[v * BINS + b];
+      first[b] = sum;
+    }
+    __syncthreads();
+    const uint32_t left = scan_bins<kOneWaves>(first, BINS, part);
+    places_of_waves<kOneWaves>(counts, first, BINS);
+    __syncthreads();
+    place_keys<kOneWaves>(counts + threadIdx.x / 64 * BINS, BINS, 8, n, digit, [&](uint32_t i, uint32_t, uint32_t at) {
+      key[from ^ 1][at] = key[from][i];
+      pos[from ^ 1][at] = pos[from][i];
+    });
+    n = left;
+    __syncthreads();
+  }
+  for (uint32_t i = threadIdx.x; i < n; i += threads) {
+    const uint32_t k = key[from][i];
+    a.key[0][(uint64_t)w * a.tokens + i] = k;
+    a.pos[0][(uint64_t)w * a.tokens + i] = pos[from][i];
+    if (i == 0 || key[from][i - 1] != k) atomicOr(&seen[k >> 5], 1u << (k & 31));
+  }
+  if (threadIdx.x == 0) a.real[w] = n;
+}
+
+// Many tokens: a pass over one digit is two launches, counting and placing.  Pass p goes from buffer p & 1 to the other; the first reads the
+// tokens themselves.
+__device__ __forceinline__ uint32_t sort_digit(const EmbedArgs& a, const uint32_t* keys, uint32_t w, uint32_t i) {
+  const uint32_t k = keys ? keys[i] : token_id(a, w, i);
+  return k == 0xFFFFFFFFu ? a.bins : k >> a.shift & (a.bins - 1);
+}
+
+__global__ __launch_bounds__(kThreads) void k_embed_count(EmbedArgs a, const uint32_t* keys) {
+  __shared__ uint32_t counts[kMostBins];
+  const uint32_t block = a.first + blockIdx.x, w = block / a.runs, r = block % a.runs, begin = r * a.run;
+  const uint32_t n = keys ? a.real[w] : a.tokens;
+  for (uint32_t i = threadIdx.x; i < a.bins; i += kThreads) counts[i] = 0;
+  if (!keys) {   // numbers are marked by the last pass
+    uint32_t* const seen = a.seen + (uint64_t)w * seen_words(a.vocab);
+    for (uint32_t i = r * kThreads + threadIdx.x; i < seen_words(a.vocab); i += a.runs * kThreads) seen[i] = 0;
+  }
+  __syncthreads();
+  const uint32_t* const own = keys ? keys + (uint64_t)w * a.tokens : nullptr;
+  if (begin < n)
+    count_keys<kWaves>(counts, a.bins, min(a.run, n - begin), [&](uint32_t i) { return sort_digit(a, own, w, begin + i); });
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < a.bins; i += kThreads) a.counts[((uint64_t)w * a.runs + r) * a.bins + i] = counts[i];
+}
+
+__global__ __launch_bounds__(kThreads) void k_embed_place(EmbedArgs a, const uint32_t* keys, const uint32_t* poss, uint32_t* key_out, uint32_t* pos_out) {
+  __shared__ uint32_t counts[kWaves * kMostBins], first[kMostBins], part[kWaves];
+  const uint32_t block = a.first + blockIdx.x, w = block / a.runs, r = block % a.runs, begin = r * a.run;
+  const uint32_t n = keys ? a.real[w] : a.tokens;
+  const uint32_t* const all = a.counts + (uint64_t)w * a.runs * a.bins;
+  constexpr uint32_t EACH = kMostBins / kThreads;
+  uint32_t ahead[EACH];   // keys of a bin in the runs ahead of this one
+#pragma unroll
+  for (uint32_t j = 0; j < EACH; ++j) {
+    const uint32_t b = j * kThreads + threadIdx.x;
+    ahead[j] = 0;
+    if (b < a.bins) {
+      uint32_t sum = 0;
+      for (uint32_t q = 0; q < a.runs; ++q) {
+        const uint32_t c = all[(uint64_t)q * a.bins + b];
+        if (q == r) ahead[j] = sum;
+        sum += c;
+      }
+      first[b] = sum;
+    }
+  }
+  for (uint32_t i = threadIdx.x; i < kWaves * a.bins; i += kThreads) counts[i] = 0;
+  __syncthreads();
+  const uint32_t left = scan_bins<kWaves>(first, a.bins, part);
+#pragma unroll
+  for (uint32_t j = 0; j < EACH; ++j) {
+    const uint32_t b = j * kThreads + threadIdx.x;
+    if (b < a.bins) first[b] += ahead[j];
+  }
+  const uint32_t* const own = keys ? keys + (uint64_t)w * a.tokens : nullptr;
+  const uint32_t here = begin < n ? min(a.run, n - begin) : 0;
+  auto digit = [&](uint32_t i) { return sort_digit(a, own, w, begin + i); };
+  count_keys<kWaves>(counts + threadIdx.x / 64 * a.bins, a.bins, here, digit);
+  __syncthreads();
+  places_of_waves<kWaves>(counts, first, a.bins);
+  __syncthreads();
+  uint32_t* const seen = a.seen + (uint64_t)w * seen_words(a.vocab);
+  place_keys<kWaves>(counts + threadIdx.x / 64 * a.bins, a.bins, (int)a.bits, here, digit, [&](uint32_t i, uint32_t, uint32_t at) {
+    const uint32_t k = own ? own[begin + i] : token_id(a, w, begin + i);
+    key_out[(uint64_t)w * a.tokens + at] = k;
+    pos_out[(uint64_t)w * a.tokens + at] = own ? poss[(uint64_t)w * a.tokens + begin + i] : begin + i;
+    if (a.last) atomicOr(&seen[k >> 5], 1u << (k & 31));
+  });
+  // All passes place the same tokens, so that what the first finds holds for the others.
+  if (!keys && r == 0 && threadIdx.x == 0) a.real[w] = left;
+}
+
+// ---- sums --------------------------------------------------------------------------------------------------------------------
+
+template <int E, typename T>
+__device__ __forceinline__ void leave_sum(const EmbedArgs& a, uint32_t w, uint32_t id, uint32_t col, int n, float* v) {
+  T* const p = (T*)a.table.p + (int64_t)w * a.table.worker + (int64_t)id * a.table.row + col;
+  float old[E] = {};
+  if (a.accumulate) load_upto<E>(p, n, old);
+#pragma unroll
+  for (int i = 0; i < E; ++i) v[i] = a.accumulate ? fmaf(v[i], a.scale, old[i]) : v[i] * a.scale;
+  store_upto<E>(p, n, v);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_embed_sum(EmbedArgs a) {
+  constexpr int E = 16 / sizeof(T);
+  constexpr uint32_t AHEAD = 8;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t group = (uint64_t)a.first + blockIdx.x;
+  if (group >= a.sum_groups) {   // rows that no token names
+    const uint64_t sets = (a.vocab + kZeroRows - 1) / kZeroRows, job = (group - a.sum_groups) * kWaves + wave;
+    const uint32_t w = (uint32_t)(job / sets), v0 = (uint32_t)(job % sets) * kZeroRows;
+    if (w >= a.workers) return;
+    const uint32_t word = a.seen[(uint64_t)w * seen_words(a.vocab) + (v0 >> 5)] >> (v0 & 31);
+    const float zero[E] = {};
+    for (uint32_t v = v0; v < min(v0 + kZeroRows, a.vocab); ++v) {
+      if (word >> (v - v0) & 1) continue;
+      T* const p = (T*)a.table.p + (int64_t)w * a.table.worker + (int64_t)v * a.table.row;
+      for (uint32_t col = lane * E; col < a.width; col += 64 * E) store_upto<E>(p + col, (int)(a.width - col), zero);
+    }
+    return;
+  }
+  const uint64_t job = group * kWaves + wave, line = job / a.blocks;
+  const uint32_t w = (uint32_t)(line / a.chunks), c = (uint32_t)(line % a.chunks);
+  if (w >= a.workers) return;
+  const uint32_t real = a.real[w], begin = c * kChunk;
+  if (begin >= real) return;
+  const uint32_t m = min(kChunk, real - begin), col = (uint32_t)(job % a.blocks) * 64 * E + lane * E;
+  const int n = (int)a.width - (int)col;
+  const uint32_t* const keys = a.key[0] + (uint64_t)w * a.tokens;
+  const uint32_t* const poss = a.pos[0] + (uint64_t)w * a.tokens;
+  const uint32_t my_key = keys[begin + min((uint32_t)lane, m - 1)], my_pos = poss[begin + min((uint32_t)lane, m - 1)];
+  const uint32_t before = begin ? keys[begin - 1] : 0xFFFFFFFFu, after = begin + m < real ? keys[begin + m] : 0xFFFFFFFFu;
+  const T* const dy = (const T*)a.rows.p + (int64_t)w * a.rows.worker + col;
+  float* const partial = a.partial + ((uint64_t)w * a.chunks + c) * 2 * a.width + col;
+  float acc[E] = {};
+  uint32_t now = (uint32_t)__builtin_amdgcn_readlane((int)my_key, 0);
+  bool head = true;   // the chunk's first number
+  auto leave = [&](bool tail) {
+    const bool goes_back = head && before == now, goes_on = tail && after == now;
+    if (n > 0) {
+      if (goes_back || goes_on) store_upto<E>(partial + (goes_back ? 0 : a.width), n, acc);
+      else leave_sum<E, T>(a, w, now, col, n, acc);
+    }
+  };
+  for (uint32_t i = 0; i < m; i += AHEAD) {
+    float v[AHEAD][E];
+#pragma unroll
+    for (uint32_t j = 0; j < AHEAD; ++j) {
+      const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)my_pos, (int)min(i + j, m - 1));
+      load_upto<E>(dy + (int64_t)at * a.rows.row, n, v[j]);
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < AHEAD; ++j) {
+      if (i + j >= m) break;
+      const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)my_key, (int)(i + j));
+      if (k != now) {
+        leave(false);
+        now = k;
+        head = false;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += v[j][e];
+    }
+  }
+  leave(true);
+}
+
+// The numbers that go on from chunk c, where they begin, into the next ones.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_embed_join(EmbedArgs a) {
+  constexpr int E = 16 / sizeof(T);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t job = ((uint64_t)a.first + blockIdx.x) * kWaves + wave, line = job / a.blocks;
+  const uint32_t w = (uint32_t)(line / a.chunks), c = (uint32_t)(line % a.chunks);
+  if (w >= a.workers) return;
+  const uint32_t real = a.real[w], begin = c * kChunk;
+  if (begin + kChunk >= real) return;
+  const uint32_t* const keys = a.key[0] + (uint64_t)w * a.tokens;
+  const uint32_t k = keys[begin + kChunk - 1];
+  if (keys[begin + kChunk] != k) return;
+  if (begin && keys[begin] == k && keys[begin - 1] == k) return;   // begins further ahead
+  const uint32_t col = (uint32_t)(job % a.blocks) * 64 * E + lane * E;
+  const int n = (int)a.width - (int)col;
+  if (n <= 0) return;
+  const float* p = a.partial + ((uint64_t)w * a.chunks + c) * 2 * a.width + col;
+  float acc[E];
+  load_upto<E>(p + a.width, n, acc);
+  for (uint32_t at = begin + kChunk; at < real && keys[at] == k; at += kChunk) {
+    p += 2 * (uint64_t)a.width;
+    float v[E];
+    load_upto<E>(p, n, v);
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] += v[e];
+  }
+  leave_sum<E, T>(a, w, k, col, n, acc);
+}
+
+}  // namespace
+}  // namespace evg
+
+using namespace evg;
+
+struct evg_embed {
+  evg_embed_config cfg{};
+  hipStream_t stream = nullptr;
+  void* owned = nullptr;
+  EmbedArgs at{};       // the workspace's parts
+  int bits = 1;         // of a token's number
+  uint32_t passes = 1;  // of the sort in many workgroups
+};
+
+namespace {
+
+template <typename Kernel, typename... More>
+hipError_t launch(uint64_t groups, uint32_t threads, hipStream_t s, EmbedArgs& a, Kernel kernel, More... more) {
+  launch_pieces(groups, threads, [&](uint32_t first, uint32_t grid) {
+    a.first = first;
+    kernel<<<grid, threads, 0, s>>>(a, more...);
+  });
+  return hipGetLastError();
+}
+
+uint64_t ids_bytes(const evg_ids* ids, uint32_t workers, uint32_t tokens) {
+  return ((uint64_t)(workers - 1) * (uint64_t)ids->worker + tokens) * (ids->wide ? 8 : 4);
+}
+
+evg_status check_ids(const evg_ids* ids, uint32_t workers, uint32_t tokens) {
+  if (!ids || (tokens && !ids->p)) return fail(EVG_ERR_INVALID, "ids must be given");
+  if (!tokens) return EVG_OK;
+  if ((uintptr_t)ids->p % (ids->wide ? 8 : 4)) return fail(EVG_ERR_ALIGN, "ids is not aligned to its numbers");
+  if (workers > 1 && (ids->worker < 0 || ids->worker >> 44)) return fail(EVG_ERR_INVALID, "ids: the stride is out of range");
+  evg_ids one = *ids;
+  if (workers <= 1) one.worker = 0;
+  return check_device_array(ids->p, ids_bytes(&one, workers, tokens), "ids");
+}
+
+Span ids_span(const evg_ids* ids, uint32_t workers, uint32_t tokens) {
+  Span s;
+  s.what = "ids";
+  if (!tokens) return s;
+  evg_ids one = *ids;
+  if (workers <= 1) one.worker = 0;
+  s.begin = (uintptr_t)ids->p;
+  s.end = s.begin + ids_bytes(&one, workers, tokens);
+  return s;
+}
+
+EmbedArgs embed_args(const evg_embed* c, uint32_t tokens, const evg_ids* ids, const evg_mat* table, const evg_mat* rows) {
+  const evg_embed_config& g = c->cfg;
+  EmbedArgs a = c->at;
+  a.ids = ids->p;
+  a.ids_worker = g.workers > 1 ? ids->worker : 0;
+  a.wide = ids->wide;
+  a.table = *table;
+  a.rows = *rows;
+  if (g.workers <= 1) a.table.worker = a.rows.worker = 0;
+  if (tokens <= 1) a.rows.row = 0;
+  if (g.vocab <= 1) a.table.row = 0;
+  a.workers = g.workers, a.tokens = tokens, a.vocab = g.vocab, a.width = g.width;
+  const uint32_t across = 64 * 16 / type_bytes(g.type);
+  a.blocks = (g.width + across - 1) / across;
+  a.scale = g.scale;
+  return a;
+}
+
+template <typename T>
+hipError_t embed_backward(const evg_embed* c, EmbedArgs& a) {
+  hipStream_t s = c->stream;
+  hipError_t e;
+  if (a.tokens <= kOneSort) {
+    if ((e = launch(a.workers, kOneWaves * 64, s, a, k_embed_sort_alone, c->bits)) != hipSuccess) return e;
+  } else {
+    const Runs runs = cut_runs(a.tokens);
+    a.run = runs.each, a.runs = runs.count;
+    a.bits = (c->bits + c->passes - 1) / c->passes;
+    a.bins = 1u << a.bits;
+    for (uint32_t p = 0; p < c->passes; ++p) {
+      // The last pass ends in buffer 0.
+      const uint32_t to = (c->passes - 1 - p) & 1;
+      a.shift = p * a.bits;
+      a.last = p + 1 == c->passes;
+      const uint32_t* keys = p ? a.key[to ^ 1] : nullptr;
+      if ((e = launch((uint64_t)a.workers * a.runs, kThreads, s, a, k_embed_count, keys)) != hipSuccess) return e;
+      if ((e = launch((uint64_t)a.workers * a.runs, kThreads, s, a, k_embed_place, keys, (const uint32_t*)a.pos[to ^ 1], a.key[to], a.pos[to])) != hipSuccess) return e;
+    }
+  }
+  a.chunks = (a.tokens + kChunk - 1) / kChunk;
+  const uint64_t jobs = (uint64_t)a.workers * a.chunks * a.blocks, groups = (jobs + kWaves - 1) / kWaves;
+  const uint64_t zero = a.accumulate ? 0 : ((uint64_t)a.workers * ((a.vocab + kZeroRows - 1) / kZeroRows) + kWaves - 1) / kWaves;
+  a.sum_groups = (uint32_t)groups;
+  if ((e = launch(groups + zero, kThreads, s, a, k_embed_sum<T>)) != hipSuccess) return e;
+  return a.chunks > 1 ? launch(groups, kThreads, s, a, k_embed_join<T>) : hipSuccess;
+}
+
+}  // namespace
+
+extern "C" {
+
+evg_status evg_embed_init(evg_embed** out, const evg_embed_config* cfg, void* hip_stream) {
+  if (!out || !cfg) return fail(EVG_ERR_INVALID, "out and cfg must be non-NULL");
+  *out = nullptr;
+  if (cfg->workers < 1 || cfg->workers > 65535) return fail(EVG_ERR_INVALID, "workers must be 1 .. 65535");
+  if (cfg->vocab < 1 || cfg->vocab > (1u << 24)) return fail(EVG_ERR_INVALID, "vocab must be 1 .. 2^24");
+  if (cfg->width < 1 || cfg->width > (1u << 20)) return fail(EVG_ERR_INVALID, "width must be 1 .. 2^20");
+  if (cfg->max_tokens > (1u << 26)) return fail(EVG_ERR_INVALID, "max_tokens must be at most 2^26");
+  evg_status st;
+  if ((st = check_type(cfg->type, "type")) != EVG_OK) return st;
+  if (!std::isfinite(cfg->scale)) return fail(EVG_ERR_INVALID, "scale must be finite");
+  evg_embed* c = new (std::nothrow) evg_embed();
+  if (!c) return fail(EVG_ERR_OOM, "host allocation failed");
+  c->cfg = *cfg;
+  c->stream = static_cast<hipStream_t>(hip_stream);
+  while ((cfg->vocab - 1) >> c->bits) ++c->bits;
+  c->passes = (uint32_t)(c->bits + 9) / 10;
+  if (cfg->train) {
+    const uint64_t W = cfg->workers, T = cfg->max_tokens;
+    const bool many = T > kOneSort;
+    // Fewer tokens may be cut into as many runs.
+    const uint32_t bins = 1u << ((c->bits + c->passes - 1) / c->passes), runs = many ? 128 : 0;
+    const uint64_t chunks = (T + kChunk - 1) / kChunk;
+    const uint64_t words[] = {W * T, W * T, many && c->passes > 1 ? W * T : 0, many && c->passes > 1 ? W * T : 0, W * runs * bins, W,
+                              W * ((cfg->vocab + 31) / 32), chunks > 1 ? W * chunks * 2 * cfg->width : 0};
+    uint64_t total = 0;
+    for (uint64_t n : words) total += (n + 63) / 64 * 64;
+    const hipError_t e = total >> 46 ? hipErrorOutOfMemory : hipMalloc(&c->owned, total * 4);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      delete c;
+      return fail(e == hipErrorOutOfMemory ? EVG_ERR_OOM : EVG_ERR_HIP, "workspace: %s", hipGetErrorString(e));
+    }
+    uint32_t* p = (uint32_t*)c->owned;
+    uint32_t** const to[] = {&c->at.key[0], &c->at.pos[0], &c->at.key[1], &c->at.pos[1], &c->at.counts, &c->at.real, &c->at.seen, (uint32_t**)&c->at.partial};
+    for (int i = 0; i < 8; ++i) {
+      *to[i] = p;
+      p += (words[i] + 63) / 64 * 64;
+    }
+  }
+  *out = c;
+  return EVG_OK;
+}
+
+evg_status evg_embed_forward(evg_embed* c, uint32_t tokens, const evg_ids* ids, const evg_mat* table, const evg_mat* y) {
+  if (!c) return fail(EVG_ERR_INVALID, "context must be non-NULL");
+  const evg_embed_config& g = c->cfg;
+  if (tokens > g.max_tokens) return fail(EVG_ERR_INVALID, "tokens exceeds the context's max_tokens");
+  evg_status st;
+  if ((st = check_ids(ids, g.workers, tokens)) != EVG_OK) return st;
+  if ((st = check_mat(table, g.workers, g.vocab, g.width, g.type, false, "table")) != EVG_OK) return st;
+  if ((st = check_mat(y, g.workers, tokens, g.width, g.type, true, "y")) != EVG_OK) return st;
+  const Span ins[] = {mat_span(table, g.workers, g.vocab, g.width, g.type, "table"), ids_span(ids, g.workers, tokens)};
+  const Span outs[] = {mat_span(y, g.workers, tokens, g.width, g.type, "y")};
+  if ((st = check_apart(outs, 1, ins, 2)) != EVG_OK) return st;
+  if (!tokens) return EVG_OK;
+  EmbedArgs a = embed_args(c, tokens, ids, table, y);
+  const uint64_t groups = ((uint64_t)g.workers * tokens * a.blocks + kWaves - 1) / kWaves;
+  if (groups > 0x7FFFFFFFull) return fail(EVG_ERR_INVALID, "tokens is out of range");
+  HIP_TRY(g.type == EVG_F32   ? launch(groups, kThreads, c->stream, a, k_embed_rows<float>)
+          : g.type == EVG_F16 ? launch(groups, kThreads, c->stream, a, k_embed_rows<half_t>)
+                              : launch(groups, kThreads, c->stream, a, k_embed_rows<bf16_t>));
+  return EVG_OK;
+}
+
+evg_status evg_embed_backward(evg_embed* c, uint32_t tokens, const evg_ids* ids, const evg_mat* dy, const evg_mat* d_table, uint32_t accumulate) {
+  if (!c) return fail(EVG_ERR_INVALID, "context must be non-NULL");
+  const evg_embed_config& g = c->cfg;
+  if (!g.train) return fail(EVG_ERR_STATE, "the context was made without train");
+  if (tokens > g.max_tokens) return fail(EVG_ERR_INVALID, "tokens exceeds the context's max_tokens");
+  evg_status st;
+  if ((st = check_ids(ids, g.workers, tokens)) != EVG_OK) return st;
+  if ((st = check_mat(dy, g.workers, tokens, g.width, g.type, false, "dy")) != EVG_OK) return st;
+  if ((st = check_mat(d_table, g.workers, g.vocab, g.width, g.type, true, "d_table")) != EVG_OK) return st;
+  const Span ins[] = {mat_span(dy, g.workers, tokens, g.width, g.type, "dy"), ids_span(ids, g.workers, tokens)};
+  const Span outs[] = {mat_span(d_table, g.workers, g.vocab, g.width, g.type, "d_table")};
+  if ((st = check_apart(outs, 1, ins, 2)) != EVG_OK) return st;
+  EmbedArgs a = embed_args(c, tokens, ids, d_table, dy);
+  a.accumulate = accumulate != 0;
+  const uint64_t rows = (uint64_t)g.workers * g.vocab, sums = (uint64_t)g.workers * ((tokens + kChunk - 1) / kChunk) * a.blocks;
+  if ((rows / kZeroRows + g.workers + sums) / kWaves > 0x7FFF0000ull) return fail(EVG_ERR_INVALID, "vocab or tokens is out of range");
+  HIP_TRY(g.type == EVG_F32 ? embed_backward<float>(c, a) : g.type == EVG_F16 ? embed_backward<half_t>(c, a) : embed_backward<bf16_t>(c, a));
+  return EVG_OK;
+}
+
+evg_status evg_embed_destroy(evg_embed* c) {
+  if (!c) return EVG_OK;
+  hipError_t e = hipStreamSynchronize(c->stream);
+  if (c->owned) { const hipError_t f = hipFree(c->owned); if (e == hipSuccess) e = f; }
+  delete c;
+  HIP_TRY(e);
+  return EVG_OK;
+}
+
+}  // extern "C"

@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "ffn_choose.h"
+#include "gemm_operand.h"
 #include "launch_pieces.h"
 
 namespace evg {
@@ -12,11 +13,6 @@ namespace evg {
 struct Activation {
   float c0, c1;
   uint32_t relu, erf;
-};
-
-struct GemmOperand {
-  const void* p;      // null: this part is left out
-  int64_t worker, ld; // elements between workers and between rows of what lies in memory
 };
 
 // C (M x N) from products over K; for each of `workers` and `parts`.

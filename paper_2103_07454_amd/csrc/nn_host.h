@@ -74,6 +74,21 @@ inline Span mat_span(const evg_mat* m, uint32_t workers, uint64_t rows, uint64_t
   return s;
 }
 
+// An array of `count` 32-bit values.
+inline evg_status check_array(const void* p, uint64_t count, const char* what) {
+  if (!p) return fail(EVG_ERR_INVALID, "%s must be given", what);
+  if ((uintptr_t)p % 4) return fail(EVG_ERR_ALIGN, "%s is not aligned to its elements", what);
+  return count ? check_device_array(p, count * 4, what) : EVG_OK;
+}
+
+inline Span array_span(const void* p, uint64_t count, const char* what) {
+  Span s;
+  s.what = what;
+  s.begin = (uintptr_t)p;
+  s.end = s.begin + (p ? count * 4 : 0);
+  return s;
+}
+
 // Do pieces of `a` and `b` bytes, each repeated every `every` bytes, `apart` bytes from one another, stay clear of each other?
 inline bool pieces_apart(uint64_t a, uint64_t b, uint64_t every, uintptr_t from, uintptr_t to) {
   if (!every) return false;

@@ -1,0 +1,300 @@
+// Which experts a token goes to, and the gradient of their weights (include/evg_nn.h, evg_router_*).
+//
+// A token's logits lie in the registers of 1 to 64 lanes, eight to a lane (sixteen above 512 experts).  K times the lanes find the largest
+// among those not chosen yet: a lane its own, then the group by exchanges, of one word that has the logit's rank above and
+// the expert's number, turned round, below.  So equal logits go to the lowest number, and the order of the lanes is of no matter.
+//
+// Bound by memory where tokens are many (E values in, K pairs out); a choice is about sixty instructions.
+#include <hip/hip_runtime.h>
+
+#include <new>
+
+#include "nn_device.h"
+#include "nn_host.h"
+
+namespace evg {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct RouterArgs {
+  evg_mat logits, d_logits;
+  int32_t* chosen;
+  float* weights;             // d_weights in the backward pass
+  uint64_t lines;             // workers * tokens
+  uint32_t tokens, experts, top, over_chosen, first;
+};
+
+// Ranks of floats as whole numbers: minus infinity lowest but 0, a NaN of any kind highest; both zeros are one.
+__device__ __forceinline__ uint32_t rank_of(float v) {
+  if (v != v) return 0xFFFFFFFFu;
+  const uint32_t b = __float_as_uint(v + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+constexpr uint32_t kRankOfNone = 0x007FFFFFu;   // minus infinity's
+
+template <int LANES>
+__device__ __forceinline__ float lanes_total(float v) {
+#pragma unroll
+  for (int d = 1; d < LANES; d <<= 1) v += __shfl_xor(v, d, LANES);
+  return v;
+}
+
+template <int LANES>
+__device__ __forceinline__ float lanes_most(float v) {
+#pragma unroll
+  for (int d = 1; d < LANES; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, LANES));
+  return v;
+}
+
+// This lane's logits; minus infinity behind the last one.
+template <int PER, typename T>
+__device__ __forceinline__ void load_logits(const T* p, int n, float* v) {
+#pragma unroll
+  for (int i = 0; i < PER; i += 8) {
+    if (n >= i + 8) {
+      load_n<8>(p + i, v + i);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i + j] = i + j < n ? to_f(p[i + j]) : -INFINITY;
+    }
+  }
+}
+
+template <typename T, int LANES, int PER>
+__global__ __launch_bounds__(kThreads) void k_router(RouterArgs a) {
+  const uint64_t line = ((uint64_t)a.first + blockIdx.x) * (kThreads / LANES) + threadIdx.x / LANES;
+  if (line >= a.lines) return;   // all of a group's lanes at once
+  const uint32_t w = (uint32_t)(line / a.tokens), t = (uint32_t)(line % a.tokens);
+  const int lane = threadIdx.x % LANES, first = lane * PER;
+  float v[PER];
+  load_logits<PER>((const T*)a.logits.p + (int64_t)w * a.logits.worker + (int64_t)t * a.logits.row + first, (int)a.experts - first, v);
+  uint32_t rank[PER];
+  int place[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    rank[i] = rank_of(v[i]);
+    if (rank[i] == kRankOfNone) rank[i] = 0;   // never chosen
+    place[i] = -1;
+  }
+  float most = 0.f, total = 0.f;
+  uint32_t k = 0;
+  for (; k < a.top; ++k) {
+    uint64_t best = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint64_t it = (uint64_t)rank[i] << 32 | (uint32_t)~(first + i);
+      best = rank[i] && it > best ? it : best;
+    }
+#pragma unroll
+    for (int d = 1; d < LANES; d <<= 1) {
+      const uint64_t other = __shfl_xor((unsigned long long)best, d, LANES);
+      best = other > best ? other : best;
+    }
+    if (!best) break;   // none is left
+    const int e = (int)~(uint32_t)best;
+    const uint32_t r = (uint32_t)(best >> 32);
+    const float value = r == 0xFFFFFFFFu ? NAN : __uint_as_float(r & 0x80000000u ? r & 0x7FFFFFFFu : ~r);
+    if (k == 0) most = value;
+    total += expf(value - most);
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (first + i == e) {
+        place[i] = (int)k;
+        rank[i] = 0;
+      }
+  }
+  if (!a.over_chosen) {
+    total = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) total += expf(v[i] - most);
+    total = lanes_total<LANES>(total);
+  }
+  int32_t* const chosen = a.chosen + line * a.top;
+  float* const weights = a.weights + line * a.top;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (place[i] >= 0) {
+      chosen[place[i]] = first + i;
+      weights[place[i]] = expf(v[i] - most) / total;
+    }
+  for (uint32_t j = k + lane; j < a.top; j += LANES) {
+    chosen[j] = -1;
+    weights[j] = 0.f;
+  }
+}
+
+template <typename T, int LANES, int PER>
+__global__ __launch_bounds__(kThreads) void k_router_backward(RouterArgs a) {
+  const uint64_t line = ((uint64_t)a.first + blockIdx.x) * (kThreads / LANES) + threadIdx.x / LANES;
+  if (line >= a.lines) return;
+  const uint32_t w = (uint32_t)(line / a.tokens), t = (uint32_t)(line % a.tokens);
+  const int lane = threadIdx.x % LANES, first = lane * PER;
+  const T* const logits = (const T*)a.logits.p + (int64_t)w * a.logits.worker + (int64_t)t * a.logits.row;
+  const int32_t* const chosen = a.chosen + line * a.top;
+  const float* const dw = a.weights + line * a.top;
+  float v[PER], d[PER];
+  load_logits<PER>(logits + first, (int)a.experts - first, v);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) d[i] = 0.f;
+  uint32_t mine[PER];   // is it chosen?
+#pragma unroll
+  for (int i = 0; i < PER; ++i) mine[i] = 0;
+  for (uint32_t k = 0; k < a.top; ++k) {
+    const int e = chosen[k];
+    const float g = (uint32_t)e < a.experts ? dw[k] : 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (first + i == e) {
+        d[i] = g;
+        mine[i] = 1;
+      }
+  }
+  // The softmax over what counts; all that is chosen, or all.
+  float most = -INFINITY, total = 0.f, inner = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (a.over_chosen && !mine[i]) v[i] = -INFINITY;
+    most = fmaxf(most, v[i]);
+  }
+  most = lanes_most<LANES>(most);
+  if (most == -INFINITY) most = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    v[i] = expf(v[i] - most);
+    total += v[i];
+  }
+  total = lanes_total<LANES>(total);
+  const float part = total > 0.f || total != total ? 1.f / total : 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    v[i] *= part;
+    inner += mine[i] ? v[i] * d[i] : 0.f;
+  }
+  inner = lanes_total<LANES>(inner);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) d[i] = a.over_chosen && !mine[i] ? 0.f : v[i] * (d[i] - inner);
+  T* const out = (T*)a.d_logits.p + (int64_t)w * a.d_logits.worker + (int64_t)t * a.d_logits.row + first;
+#pragma unroll
+  for (int i = 0; i < PER; i += 8) store_upto<8>(out + i, (int)a.experts - first - i, d + i);
+}
+
+template <typename T, int LANES, int PER>
+hipError_t launch_lanes(RouterArgs a, bool backward, hipStream_t s) {
+  const uint64_t per = kThreads / LANES, groups = (a.lines + per - 1) / per;
+  if (groups > 0x7FFFFFFFull) return hipErrorInvalidValue;
+  launch_pieces(groups, kThreads, [&](uint32_t first, uint32_t grid) {
+    a.first = first;
+    if (backward) k_router_backward<T, LANES, PER><<<grid, kThreads, 0, s>>>(a);
+    else k_router<T, LANES, PER><<<grid, kThreads, 0, s>>>(a);
+  });
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_router(const RouterArgs& a, bool backward, hipStream_t s) {
+  if (a.experts <= 8) return launch_lanes<T, 1, 8>(a, backward, s);
+  if (a.experts <= 16) return launch_lanes<T, 2, 8>(a, backward, s);
+  if (a.experts <= 32) return launch_lanes<T, 4, 8>(a, backward, s);
+  if (a.experts <= 64) return launch_lanes<T, 8, 8>(a, backward, s);
+  if (a.experts <= 128) return launch_lanes<T, 16, 8>(a, backward, s);
+  if (a.experts <= 256) return launch_lanes<T, 32, 8>(a, backward, s);
+  if (a.experts <= 512) return launch_lanes<T, 64, 8>(a, backward, s);
+  return launch_lanes<T, 64, 16>(a, backward, s);
+}
+
+}  // namespace
+}  // namespace evg
+
+using namespace evg;
+
+struct evg_router {
+  evg_router_config cfg{};
+  hipStream_t stream = nullptr;
+};
+
+namespace {
+
+hipError_t launch_any(const evg_router* c, RouterArgs& a, uint32_t tokens, bool backward) {
+  const evg_router_config& g = c->cfg;
+  a.lines = (uint64_t)g.workers * tokens;
+  a.tokens = tokens, a.experts = g.experts, a.top = g.top, a.over_chosen = g.over_chosen;
+  for (evg_mat* m : {&a.logits, &a.d_logits}) {
+    if (g.workers <= 1) m->worker = 0;
+    if (tokens <= 1) m->row = 0;
+  }
+  if (g.type == EVG_F32) return launch_router<float>(a, backward, c->stream);
+  if (g.type == EVG_F16) return launch_router<half_t>(a, backward, c->stream);
+  return launch_router<bf16_t>(a, backward, c->stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+evg_status evg_router_init(evg_router** out, const evg_router_config* cfg, void* hip_stream) {
+  if (!out || !cfg) return fail(EVG_ERR_INVALID, "out and cfg must be non-NULL");
+  *out = nullptr;
+  if (cfg->workers < 1) return fail(EVG_ERR_INVALID, "workers must be at least 1");
+  if (cfg->experts < 1 || cfg->experts > EVG_ROUTER_MAX_EXPERTS) return fail(EVG_ERR_INVALID, "experts must be 1 .. %u", EVG_ROUTER_MAX_EXPERTS);
+  if (cfg->top < 1 || cfg->top > cfg->experts) return fail(EVG_ERR_INVALID, "top must be 1 .. experts");
+  if ((uint64_t)cfg->workers * cfg->max_tokens > 0x7FFFFFFFull) return fail(EVG_ERR_INVALID, "workers and max_tokens together are out of range");
+  evg_status st;
+  if ((st = check_type(cfg->type, "type")) != EVG_OK) return st;
+  evg_router* c = new (std::nothrow) evg_router();
+  if (!c) return fail(EVG_ERR_OOM, "host allocation failed");
+  c->cfg = *cfg;
+  c->stream = static_cast<hipStream_t>(hip_stream);
+  *out = c;
+  return EVG_OK;
+}
+
+evg_status evg_router_forward(evg_router* c, uint32_t tokens, const evg_mat* logits, int32_t* chosen, float* weights) {
+  if (!c) return fail(EVG_ERR_INVALID, "context must be non-NULL");
+  const evg_router_config& g = c->cfg;
+  if (tokens > g.max_tokens) return fail(EVG_ERR_INVALID, "tokens exceeds the context's max_tokens");
+  const uint64_t n = (uint64_t)g.workers * tokens * g.top;
+  evg_status st;
+  if ((st = check_mat(logits, g.workers, tokens, g.experts, g.type, false, "logits")) != EVG_OK) return st;
+  if ((st = check_array(chosen, n, "chosen")) != EVG_OK || (st = check_array(weights, n, "weights")) != EVG_OK) return st;
+  const Span ins[] = {mat_span(logits, g.workers, tokens, g.experts, g.type, "logits")};
+  const Span outs[] = {array_span(chosen, n, "chosen"), array_span(weights, n, "weights")};
+  if ((st = check_apart(outs, 2, ins, 1)) != EVG_OK) return st;
+  if (!n) return EVG_OK;
+  RouterArgs a{};
+  a.logits = *logits;
+  a.chosen = chosen;
+  a.weights = weights;
+  HIP_TRY(launch_any(c, a, tokens, false));
+  return EVG_OK;
+}
+
+evg_status evg_router_backward(evg_router* c, uint32_t tokens, const float* d_weights, const evg_mat* logits, const int32_t* chosen,
+                               const evg_mat* d_logits) {
+  if (!c) return fail(EVG_ERR_INVALID, "context must be non-NULL");
+  const evg_router_config& g = c->cfg;
+  if (tokens > g.max_tokens) return fail(EVG_ERR_INVALID, "tokens exceeds the context's max_tokens");
+  const uint64_t n = (uint64_t)g.workers * tokens * g.top;
+  evg_status st;
+  if ((st = check_array(d_weights, n, "d_weights")) != EVG_OK || (st = check_array(chosen, n, "chosen")) != EVG_OK) return st;
+  if ((st = check_mat(logits, g.workers, tokens, g.experts, g.type, false, "logits")) != EVG_OK) return st;
+  if ((st = check_mat(d_logits, g.workers, tokens, g.experts, g.type, true, "d_logits")) != EVG_OK) return st;
+  const Span ins[] = {mat_span(logits, g.workers, tokens, g.experts, g.type, "logits"), array_span(d_weights, n, "d_weights"), array_span(chosen, n, "chosen")};
+  const Span outs[] = {mat_span(d_logits, g.workers, tokens, g.experts, g.type, "d_logits")};
+  if ((st = check_apart(outs, 1, ins, 3, 0, 0)) != EVG_OK) return st;
+  if (!n) return EVG_OK;
+  RouterArgs a{};
+  a.logits = *logits;
+  a.d_logits = *d_logits;
+  a.chosen = const_cast<int32_t*>(chosen);
+  a.weights = const_cast<float*>(d_weights);
+  HIP_TRY(launch_any(c, a, tokens, true));
+  return EVG_OK;
+}
+
+evg_status evg_router_destroy(evg_router* c) {
+  delete c;
+  return EVG_OK;
+}
+
+}  // extern "C"

@@ -2,7 +2,9 @@
 
 ``BlockNorm`` (the norms on both sides of a block, with its gate and residual scale), ``GatedFFN`` (the gated feed-forward
 block), both with their backward passes, and ``GradClip`` (clipping by each worker's global gradient norm, into the arena
-that ``evg.Ring.step`` takes).  Tensors have the worker as their first axis; one model alone is one worker.
+that ``evg.Ring.step`` takes).  ``Embedding`` (tokens to rows), ``Router`` (which experts a token goes to) and ``ExpertSort`` (tokens in
+the experts' order and back), with their backward passes, are what stands around blocks of several experts; ``Orthogonal`` makes the gradients of
+matrices orthogonal updates.  Tensors have the worker as their first axis; one model alone is one worker.
 
 Argument marshalling only, as in ``evg``: every operation runs in the library's HIP kernels, there is no fallback.  An
 operator is bound to one stream (the current one when it is made, or the one given) and its calls only enqueue work there.
@@ -16,6 +18,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+from typing import NamedTuple
 
 import torch
 
@@ -28,7 +31,11 @@ NONFINITE_PASS, NONFINITE_ZERO = 0, 1
 
 EXPORTS = ("evg_clip_init", "evg_clip_run", "evg_clip_destroy",
            "evg_blocknorm_init", "evg_blocknorm_forward", "evg_blocknorm_backward", "evg_blocknorm_destroy",
-           "evg_ffn_init", "evg_ffn_saved_bytes", "evg_ffn_forward", "evg_ffn_backward", "evg_ffn_destroy")
+           "evg_ffn_init", "evg_ffn_saved_bytes", "evg_ffn_forward", "evg_ffn_backward", "evg_ffn_destroy",
+           "evg_embed_init", "evg_embed_forward", "evg_embed_backward", "evg_embed_destroy",
+           "evg_router_init", "evg_router_forward", "evg_router_backward", "evg_router_destroy",
+           "evg_experts_init", "evg_experts_slots", "evg_experts_dispatch", "evg_experts_combine", "evg_experts_combine_backward",
+           "evg_experts_destroy", "evg_ortho_init", "evg_ortho_update", "evg_ortho_destroy")
 
 _NOTHING = 256     # the address of a tensor without elements: given, but never read
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -65,12 +72,44 @@ class FFNConfig(C.Structure):
                 ("type", C.c_uint32), ("activation", C.c_uint32), ("train", C.c_uint32)]
 
 
+class EmbedConfig(C.Structure):
+    _fields_ = [("workers", C.c_uint32), ("vocab", C.c_uint32), ("width", C.c_uint32), ("max_tokens", C.c_uint32),
+                ("type", C.c_uint32), ("scale", C.c_float), ("train", C.c_uint32)]
+
+
+class Ids(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("worker", C.c_int64), ("wide", C.c_uint32)]
+
+
+class RouterConfig(C.Structure):
+    _fields_ = [("workers", C.c_uint32), ("experts", C.c_uint32), ("top", C.c_uint32), ("max_tokens", C.c_uint32),
+                ("type", C.c_uint32), ("over_chosen", C.c_uint32)]
+
+
+class ExpertsConfig(C.Structure):
+    _fields_ = [("workers", C.c_uint32), ("experts", C.c_uint32), ("top", C.c_uint32), ("width", C.c_uint32),
+                ("max_tokens", C.c_uint32), ("capacity", C.c_uint32), ("type", C.c_uint32)]
+
+
+class ExpertsPlan(C.Structure):
+    _fields_ = [("slot", C.c_void_p), ("source", C.c_void_p), ("counts", C.c_void_p)]
+
+
+class OrthoConfig(C.Structure):
+    _fields_ = [("matrices", C.c_uint32), ("rows", C.c_uint32), ("cols", C.c_uint32), ("type", C.c_uint32), ("out_type", C.c_uint32),
+                ("steps", C.c_uint32), ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("momentum", C.c_float),
+                ("nesterov", C.c_uint32), ("eps", C.c_float), ("scale", C.c_float)]
+
+
 # Arguments that are structures go as packed bytes, which costs a call less than filling ctypes structures: evg_mat,
-# evg_blocknorm_in and evg_blocknorm_grads.
+# evg_blocknorm_in, evg_blocknorm_grads, evg_ids and evg_experts_plan.
 _MAT = struct.Struct("3q").pack
 _IN = struct.Struct("2I21q").pack
 _GRADS = struct.Struct("21q").pack
+_IDS = struct.Struct("2qIxxxx").pack
+_PLAN = struct.Struct("3q").pack
 assert struct.calcsize("3q") == C.sizeof(Mat) and struct.calcsize("2I21q") == C.sizeof(BlockNormIn)
+assert struct.calcsize("2qIxxxx") == C.sizeof(Ids) and struct.calcsize("3q") == C.sizeof(ExpertsPlan)
 _ABSENT = (0, 0, 0)
 
 _lib = None
@@ -91,14 +130,28 @@ def lib():
         l.evg_ffn_saved_bytes.restype = C.c_uint64
         l.evg_ffn_forward.argtypes = [vp, u32] + [mp] * 5 + [vp]
         l.evg_ffn_backward.argtypes = [vp, u32] + [mp] * 5 + [vp] + [mp] * 4
-        for name in ("clip", "blocknorm", "ffn"):
+        l.evg_embed_init.argtypes = [C.POINTER(vp), C.POINTER(EmbedConfig), vp]
+        l.evg_embed_forward.argtypes = [vp, u32, mp, mp, mp]
+        l.evg_embed_backward.argtypes = [vp, u32, mp, mp, mp, u32]
+        l.evg_router_init.argtypes = [C.POINTER(vp), C.POINTER(RouterConfig), vp]
+        l.evg_router_forward.argtypes = [vp, u32, mp, vp, vp]
+        l.evg_router_backward.argtypes = [vp, u32, vp, mp, vp, mp]
+        l.evg_experts_init.argtypes = [C.POINTER(vp), C.POINTER(ExpertsConfig), vp]
+        l.evg_experts_slots.argtypes = [vp, u32]
+        l.evg_experts_slots.restype = C.c_uint64
+        l.evg_experts_dispatch.argtypes = [vp, u32, mp, vp, mp, mp]
+        l.evg_experts_combine.argtypes = [vp, u32, mp, vp, mp, mp]
+        l.evg_experts_combine_backward.argtypes = [vp, u32, mp, mp, vp, mp, mp, vp]
+        l.evg_ortho_init.argtypes = [C.POINTER(vp), C.POINTER(OrthoConfig), vp]
+        l.evg_ortho_update.argtypes = [vp, mp, mp, mp, mp]
+        for name in ("clip", "blocknorm", "ffn", "embed", "router", "experts", "ortho"):
             getattr(l, f"evg_{name}_destroy").argtypes = [vp]
         _lib = l
     return _lib
 
 
 class _Operator:
-    """What the three have in common: a handle of the library, its stream and the checks of tensors."""
+    """What they have in common: a handle of the library, its stream and the checks of tensors."""
 
     _destroy = None
 
@@ -135,10 +188,11 @@ class _Operator:
             return torch.empty_like(t)
         return self._empty(t.shape)
 
-    def _at(self, t, shape, what):
+    def _at(self, t, shape, what, dtype=None):
         """Address and strides of a tensor of the given shape, [workers, rows, columns] or [workers, columns]."""
-        if t.dtype is not self.dtype or t.get_device() != self._index:
-            raise ValueError(f"{what} must be {self.dtype} on {self.device}, is {t.dtype} on {t.device}")
+        dtype = dtype or self.dtype
+        if t.dtype is not dtype or t.get_device() != self._index:
+            raise ValueError(f"{what} must be {dtype} on {self.device}, is {t.dtype} on {t.device}")
         if t.shape != shape:
             raise ValueError(f"{what} must have the shape {tuple(shape)}, has {tuple(t.shape)}")
         stride = t.stride()
@@ -146,8 +200,14 @@ class _Operator:
             raise ValueError(f"{what}: the last axis must have stride 1")
         return t.data_ptr() or _NOTHING, stride[0], stride[1] if len(stride) == 3 else 0
 
-    def _mat(self, t, shape, what):
-        return _MAT(*self._at(t, shape, what))
+    def _mat(self, t, shape, what, dtype=None):
+        return _MAT(*self._at(t, shape, what, dtype))
+
+    def _array(self, t, shape, what, dtype=torch.int32):
+        """The address of a contiguous tensor."""
+        if t.dtype is not dtype or t.get_device() != self._index or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}")
+        return t.data_ptr() or _NOTHING
 
     def _rows(self, t, width, what):
         if t.dim() != 3 or t.shape[0] != self.workers or t.shape[2] != width:
@@ -325,3 +385,217 @@ class GatedFFN(_Operator):
             *(None if d is None else self._mat(d, w.shape, what)
               for d, w, what in zip(grads, (w_gate, w_up, w_down), ("dw_gate", "dw_up", "dw_down")))))
         return (dx, *grads)
+
+
+class Embedding(_Operator):
+    """``y[t] = scale * table[token[t]]`` for each worker, and the table's gradient (with ``train``).
+
+    tokens: [workers, tokens], int32 or int64; a number outside 0 .. vocab-1 is padding: a row of zeros, no part in the gradient.
+    table: [workers, vocab, width]; y: [workers, tokens, width].
+    """
+
+    _destroy = "evg_embed_destroy"
+
+    def __init__(self, vocab, width, *, workers=1, max_tokens, dtype=torch.bfloat16, scale=1.0, train=False, device="cuda", stream=None):
+        self._open(dtype, device, stream)
+        self.vocab, self.width, self.workers, self.max_rows = int(vocab), int(width), int(workers), int(max_tokens)
+        self._make(lib().evg_embed_init, EmbedConfig(self.workers, self.vocab, self.width, self.max_rows, _TYPES[dtype], scale, bool(train)))
+
+    def _ids(self, tokens):
+        if tokens.dtype not in (torch.int32, torch.int64) or tokens.get_device() != self._index:
+            raise ValueError(f"tokens must be int32 or int64 on {self.device}, is {tokens.dtype} on {tokens.device}")
+        if tokens.dim() != 2 or tokens.shape[0] != self.workers:
+            raise ValueError(f"tokens must have the shape ({self.workers}, tokens), has {tuple(tokens.shape)}")
+        count = tokens.shape[1]
+        if count > self.max_rows:
+            raise ValueError(f"tokens has {count} of a worker, at most {self.max_rows} were asked for")
+        if count > 1 and tokens.stride(1) != 1:
+            raise ValueError("tokens: the last axis must have stride 1")
+        return count, _IDS(tokens.data_ptr() or _NOTHING, tokens.stride(0), tokens.dtype is torch.int64)
+
+    def forward(self, tokens, table, *, out=None):
+        """``y``."""
+        count, ids = self._ids(tokens)
+        shape = (self.workers, count, self.width)
+        if out is None:
+            out = self._empty(shape)
+        evg._check(lib().evg_embed_forward(self._h, count, ids, self._mat(table, (self.workers, self.vocab, self.width), "table"),
+                                           self._mat(out, shape, "out")))
+        return out
+
+    def backward(self, d_out, tokens, *, d_table=None, accumulate=False):
+        """``d_table``.  ``accumulate``: added to what ``d_table`` holds, as where a table has a second use or a batch several parts."""
+        count, ids = self._ids(tokens)
+        shape = (self.workers, self.vocab, self.width)
+        if d_table is None:
+            if accumulate:
+                raise ValueError("accumulate needs the d_table to add to")
+            d_table = self._empty(shape)
+        evg._check(lib().evg_embed_backward(self._h, count, ids, self._mat(d_out, (self.workers, count, self.width), "d_out"),
+                                            self._mat(d_table, shape, "d_table"), bool(accumulate)))
+        return d_table
+
+
+class Router(_Operator):
+    """The ``top`` experts of each token's largest logits, and their weights: the softmax over all logits, or with ``over_chosen`` over the
+    chosen ones.
+
+    logits: [workers, tokens, experts]; chosen (int32) and weights (float32): [workers, tokens, top], the largest first, equal
+    ones in the experts' order.  Experts at minus infinity are never chosen; where too few are left, -1 with weight 0.
+    """
+
+    _destroy = "evg_router_destroy"
+
+    def __init__(self, experts, top, *, workers=1, max_tokens, dtype=torch.float32, over_chosen=True, device="cuda", stream=None):
+        self._open(dtype, device, stream)
+        self.experts, self.top, self.workers, self.max_rows = int(experts), int(top), int(workers), int(max_tokens)
+        self._make(lib().evg_router_init, RouterConfig(self.workers, self.experts, self.top, self.max_rows, _TYPES[dtype], bool(over_chosen)))
+
+    def forward(self, logits, *, chosen=None, weights=None):
+        """``(chosen, weights)``."""
+        count = self._rows(logits, self.experts, "logits")
+        shape = (self.workers, count, self.top)
+        if chosen is None:
+            chosen = self._empty(shape, torch.int32)
+        if weights is None:
+            weights = self._empty(shape, torch.float32)
+        evg._check(lib().evg_router_forward(self._h, count, self._mat(logits, logits.shape, "logits"), self._array(chosen, shape, "chosen"),
+                                            self._array(weights, shape, "weights", torch.float32)))
+        return chosen, weights
+
+    def backward(self, d_weights, logits, chosen, *, out=None):
+        """The logits' gradient from that of the weights and what ``forward`` chose.  ``out`` may be ``logits`` itself."""
+        count = self._rows(logits, self.experts, "logits")
+        shape = (self.workers, count, self.top)
+        if out is None:
+            out = self._like(logits)
+        evg._check(lib().evg_router_backward(self._h, count, self._array(d_weights, shape, "d_weights", torch.float32),
+                                             self._mat(logits, logits.shape, "logits"), self._array(chosen, shape, "chosen"),
+                                             self._mat(out, logits.shape, "out")))
+        return out
+
+
+class ExpertPlan(NamedTuple):
+    """Where ``ExpertSort.dispatch`` sent a batch's entries, all int32: ``slot`` [workers, tokens, top], -1 where left out; ``source``
+    [workers, slots], the entry ``token * top + k`` of a slot or -1; ``counts`` [workers, experts], with those that found no room."""
+
+    slot: torch.Tensor
+    source: torch.Tensor
+    counts: torch.Tensor
+
+
+class ExpertSort(_Operator):
+    """Tokens in the order of their experts, and back with weights applied.
+
+    x, y: [workers, tokens, width]; chosen: [workers, tokens, top], int32, -1 for none; rows: [workers, slots, width].  Without ``capacity`` a worker has
+    tokens * top slots, one expert's after the other's; with it, experts * capacity, of which expert e has those from e * capacity on, so that
+    ``rows.view(workers * experts, capacity, width)`` is what a ``GatedFFN`` with as many workers takes; an expert's later entries
+    that find no room are left out.  Empty slots hold zeros.
+    """
+
+    _destroy = "evg_experts_destroy"
+
+    def __init__(self, experts, top, width, *, workers=1, max_tokens, capacity=0, dtype=torch.bfloat16, device="cuda", stream=None):
+        self._open(dtype, device, stream)
+        self.experts, self.top, self.width, self.workers = int(experts), int(top), int(width), int(workers)
+        self.max_rows, self.capacity = int(max_tokens), int(capacity)
+        self._make(lib().evg_experts_init, ExpertsConfig(self.workers, self.experts, self.top, self.width, self.max_rows, self.capacity,
+                                                         _TYPES[dtype]))
+
+    def slots(self, tokens):
+        """Slots of each worker for so many tokens."""
+        return self.experts * self.capacity if self.capacity else tokens * self.top
+
+    def _sizes(self, count):
+        slots = self.slots(count)
+        return (self.workers, slots, self.width), (self.workers, count, self.top), (self.workers, slots), (self.workers, self.experts)
+
+    def _plan(self, plan, count):
+        _, entry, slots, counts = self._sizes(count)
+        return _PLAN(self._array(plan.slot, entry, "slot"), self._array(plan.source, slots, "source"), self._array(plan.counts, counts, "counts"))
+
+    def _count(self, plan):
+        count = plan.slot.shape[1] if plan.slot.dim() == 3 else -1
+        if not 0 <= count <= self.max_rows:
+            raise ValueError(f"the plan must be one of this operator's, of at most {self.max_rows} tokens")
+        return count
+
+    def dispatch(self, x, chosen, *, rows=None, plan=None):
+        """``(rows, plan)``; a plan that is given is written again."""
+        count = self._rows(x, self.width, "x")
+        row, entry, slots, counts = self._sizes(count)
+        if rows is None:
+            rows = self._empty(row)
+        if plan is None:
+            plan = ExpertPlan(self._empty(entry, torch.int32), self._empty(slots, torch.int32), self._empty(counts, torch.int32))
+        evg._check(lib().evg_experts_dispatch(self._h, count, self._mat(x, x.shape, "x"), self._array(chosen, entry, "chosen"),
+                                              self._mat(rows, row, "rows"), self._plan(plan, count)))
+        return rows, plan
+
+    def dispatch_backward(self, d_rows, plan, *, dx=None):
+        """``dx[t]``: the sum of the gradients of the rows that token t was sent to."""
+        return self.combine(d_rows, None, plan, out=dx)
+
+    def combine(self, rows, weights, plan, *, out=None):
+        """``y[t] = sum_k weights[t, k] * rows[slot[t, k]]``; weights: [workers, tokens, top], float32, or None: all 1."""
+        count = self._count(plan)
+        row, entry, _, _ = self._sizes(count)
+        shape = (self.workers, count, self.width)
+        if out is None:
+            out = self._empty(shape)
+        evg._check(lib().evg_experts_combine(self._h, count, self._mat(rows, row, "rows"),
+                                             None if weights is None else self._array(weights, entry, "weights", torch.float32),
+                                             self._plan(plan, count), self._mat(out, shape, "out")))
+        return out
+
+    def combine_backward(self, dy, rows, weights, plan, *, d_rows=None, d_weights=None, row_gradients=True, weight_gradients=True):
+        """``(d_rows, d_weights)``.  One that is neither given nor asked for is None and not computed; ``rows`` is read for
+        ``d_weights`` only."""
+        count = self._count(plan)
+        row, entry, _, _ = self._sizes(count)
+        if d_rows is None and row_gradients:
+            d_rows = self._empty(row)
+        if d_weights is None and weight_gradients:
+            d_weights = self._empty(entry, torch.float32)
+        evg._check(lib().evg_experts_combine_backward(
+            self._h, count, self._mat(dy, (self.workers, count, self.width), "dy"), None if d_weights is None else self._mat(rows, row, "rows"),
+            self._array(weights, entry, "weights", torch.float32), self._plan(plan, count),
+            None if d_rows is None else self._mat(d_rows, row, "d_rows"),
+            None if d_weights is None else self._array(d_weights, entry, "d_weights", torch.float32)))
+        return d_rows, d_weights
+
+
+class Orthogonal(_Operator):
+    """Orthogonal updates of matrices by Newton-Schulz products, with the momentum ahead of them.
+
+    ``m' = momentum * m + grad``, ``u = grad + momentum * m'`` (``nesterov``) or ``m'``; ``X = u / (|u| + eps)``; ``steps`` times
+    ``X <- a X + (b S + c S S) X`` with ``S = X X^T`` and ``polynomial = (a, b, c)``; the update is ``scale * X``.  grad and the update:
+    [matrices, rows, cols], the latter of ``out_dtype``, which is ``dtype`` or float32; m: float32.
+    """
+
+    _destroy = "evg_ortho_destroy"
+
+    def __init__(self, rows, cols, *, matrices=1, dtype=torch.float32, out_dtype=None, steps=5, polynomial=(3.4445, -4.7750, 2.0315),
+                 momentum=0.95, nesterov=True, eps=1e-7, scale=1.0, device="cuda", stream=None):
+        self._open(dtype, device, stream)
+        self.out_dtype = dtype if out_dtype is None else out_dtype
+        if self.out_dtype not in (dtype, torch.float32):
+            raise ValueError("out_dtype must be dtype or float32")
+        self.rows, self.cols, self.matrices = int(rows), int(cols), int(matrices)
+        self._make(lib().evg_ortho_init, OrthoConfig(self.matrices, self.rows, self.cols, _TYPES[dtype], _TYPES[self.out_dtype], steps,
+                                                     *polynomial, momentum, bool(nesterov), eps, scale))
+
+    def update(self, grad, *, momentum=None, momentum_out=None, out=None):
+        """The update.  ``momentum``: m, which becomes m', or stays as it is where ``momentum_out`` is given for m'; None: u is the gradient.
+        ``out`` may be ``grad`` itself."""
+        shape = (self.matrices, self.rows, self.cols)
+        if momentum is None and momentum_out is not None:
+            raise ValueError("momentum_out is given, but no momentum")
+        if out is None:
+            out = self._empty(shape, self.out_dtype)
+        old = new = None
+        if momentum is not None:
+            old = self._mat(momentum, shape, "momentum", torch.float32)
+            new = old if momentum_out is None else self._mat(momentum_out, shape, "momentum_out", torch.float32)
+        evg._check(lib().evg_ortho_update(self._h, self._mat(grad, shape, "grad"), old, new, self._mat(out, shape, "out", self.out_dtype)))
+        return out
