@@ -5,9 +5,9 @@
 // Forward: a wavefront takes 64 vectors of 16 bytes of one token's row.  Bound by memory, rows of the table in any order.
 //
 // Backward: the tokens are sorted by their number, those of one number stay in their order; then a wavefront adds up the rows of a
-// chunk of 32 sorted tokens, 64 vectors wide, and writes a sum where the number changes.  Numbers that go on in the next chunk leave partial sums in 32 bits,
+// chunk of 16 sorted tokens, 64 vectors wide, and writes a sum where the number changes.  Numbers that go on in the next chunk leave partial sums in 32 bits,
 // which a launch behind adds in the chunks' order: no atomics, so the same tokens give the same bits, and a number that half of all
-// tokens have costs no more than others.  The rows that no token names are zeroed by the same launch; a bit for each number says which.
+// tokens have costs no more than others.  The rows that no token names are zeroed by the same launch; a mark for each number says which.
 // Bound by memory: dy once, the gradient's table once.
 #include <hip/hip_runtime.h>
 
@@ -22,17 +22,19 @@ namespace evg {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr uint32_t kChunk = 32;          // sorted tokens that a wavefront adds up
+constexpr uint32_t kChunk = 16;          // sorted tokens that a wavefront adds up (16384 tokens 2048 wide: 8 / 16 / 32 take 63 / 54 / 67 us with the joining)
 constexpr int kOneWaves = 16;            // of the workgroup that sorts alone
-constexpr uint32_t kOneSort = 4096;      // most tokens of a worker that one workgroup sorts
-constexpr uint32_t kZeroRows = 4;        // rows that a wavefront may have to zero
+constexpr int kPer = 4;                  // keys of a thread in a round
+// Most tokens of a worker that one workgroup sorts.  Ranking keeps a CU's vector units busy: 16384 tokens took one workgroup 57 us, sixteen 24.
+constexpr uint32_t kOneSort = kOneWaves * 64 * kPer;
+constexpr uint32_t kZeroRows = 4;        // rows that a wavefront may have to zero: a word of marks
 
 struct EmbedArgs {
   const void* ids;
   int64_t ids_worker;
   uint32_t wide;
   evg_mat table, rows;         // rows: y or dy
-  uint32_t workers, tokens, vocab, width, blocks;   // blocks: of 64 vectors across a row
+  uint32_t workers, tokens, vocab, width, blocks, lines;   // blocks: of 64 vectors across a row; lines: workers * tokens
   float scale;
   uint32_t accumulate;
   uint32_t first;              // workgroup of a launch in pieces
@@ -40,154 +42,166 @@ struct EmbedArgs {
   uint32_t *key[2], *pos[2];   // [workers][tokens]
   uint32_t *counts;            // [workers][runs][bins]
   uint32_t *real;              // [workers]: sorted tokens
-  uint32_t *seen;              // [workers][ceil(vocab / 32)]
+  uint8_t *seen;               // [workers][vocab, up to a multiple of 4]: is a number some token's?
   float *partial;              // [workers][chunks][2][width]
   uint32_t run, runs, bins, bits, shift, last;   // of a sorting pass
   uint32_t chunks, sum_groups;
 };
 
+constexpr uint32_t kNoToken = 0xFFFFFFFFu;
+
 __device__ __forceinline__ uint32_t token_id(const EmbedArgs& a, uint32_t w, uint32_t t) {
   const int64_t at = (int64_t)w * a.ids_worker + t;
   const int64_t id = a.wide ? ((const int64_t*)a.ids)[at] : (int64_t)((const int32_t*)a.ids)[at];
-  return id >= 0 && id < (int64_t)a.vocab ? (uint32_t)id : 0xFFFFFFFFu;
+  return id >= 0 && id < (int64_t)a.vocab ? (uint32_t)id : kNoToken;
 }
 
-template <typename T>
+// U neighbouring units of 64 vectors to a wavefront, all their loads under way at once.
+template <typename T, int U>
 __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedArgs a) {
   constexpr int E = 16 / sizeof(T);
-  const uint64_t job = ((uint64_t)a.first + blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t line = job / a.blocks;
-  if (line >= (uint64_t)a.workers * a.tokens) return;
-  const uint32_t w = (uint32_t)(line / a.tokens), t = (uint32_t)(line % a.tokens);
-  const uint32_t col = (uint32_t)(job % a.blocks) * 64 * E + (threadIdx.x & 63) * E;
-  const int n = (int)a.width - (int)col;
-  if (n <= 0) return;
-  const uint32_t id = token_id(a, w, t);
-  float v[E] = {};
-  if (id != 0xFFFFFFFFu) load_upto<E>((const T*)a.table.p + (int64_t)w * a.table.worker + (int64_t)id * a.table.row + col, n, v);
+  const uint32_t unit = ((a.first + blockIdx.x) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * U;
+  uint32_t line = unit / a.blocks, block = unit % a.blocks;
+  float v[U][E] = {};
+  T* out[U];
+  int n[U];
 #pragma unroll
-  for (int i = 0; i < E; ++i) v[i] *= a.scale;
-  store_upto<E>((T*)a.rows.p + (int64_t)w * a.rows.worker + (int64_t)t * a.rows.row + col, n, v);
+  for (int u = 0; u < U; ++u) {
+    const uint32_t w = line / a.tokens, t = line % a.tokens, col = block * 64 * E + (threadIdx.x & 63) * E;
+    n[u] = line < a.lines ? (int)a.width - (int)col : 0;
+    const uint32_t id = line < a.lines ? token_id(a, w, t) : kNoToken;
+    if (id != kNoToken) load_upto<E>((const T*)a.table.p + (int64_t)w * a.table.worker + (int64_t)id * a.table.row + col, n[u], v[u]);
+    out[u] = (T*)a.rows.p + (int64_t)w * a.rows.worker + (int64_t)t * a.rows.row + col;
+    if (++block == a.blocks) block = 0, ++line;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[u][i] *= a.scale;
+    store_upto<E>(out[u], n[u], v[u]);
+  }
 }
 
 // ---- sorting -----------------------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ uint32_t seen_words(uint32_t vocab) { return (vocab + 31) / 32; }
+// Bytes, not bits: what thousands of tokens set takes no atomic operations, which would meet at a few addresses (100 us of 16384 tokens).
+__device__ __forceinline__ uint32_t seen_words(uint32_t vocab) { return (vocab + 3) / 4; }
+__device__ __forceinline__ uint8_t* seen_of(const EmbedArgs& a, uint32_t w) { return a.seen + (uint64_t)w * seen_words(a.vocab) * 4; }
 
-// A worker's tokens by one workgroup, digits of 8 bits from the lowest up, all in LDS.
+// A worker's tokens by one workgroup, digits of 8 bits from the lowest up: keys and places stay in registers and change threads through LDS.
+template <int PER>
 __global__ __launch_bounds__(kOneWaves * 64) void k_embed_sort_alone(EmbedArgs a, int bits) {
-  constexpr uint32_t BINS = 256;
-  __shared__ uint32_t key[2][kOneSort], pos[2][kOneSort], counts[kOneWaves * BINS], first[BINS], part[kOneWaves];
-  const uint32_t w = a.first + blockIdx.x, threads = kOneWaves * 64;
-  uint32_t* const seen = a.seen + (uint64_t)w * seen_words(a.vocab);
-  for (uint32_t i = threadIdx.x; i < seen_words(a.vocab); i += threads) seen[i] = 0;
-  __threadfence();   // before other threads' bits
-  uint32_t n = a.tokens;
-  int from = 0;
-  for (int shift = 0; shift == 0 || shift < bits; shift += 8, from ^= 1) {
-    for (uint32_t i = threadIdx.x; i < kOneWaves * BINS; i += threads) counts[i] = 0;
-    if (shift == 0)
-      for (uint32_t i = threadIdx.x; i < n; i += threads) {
-        key[0][i] = token_id(a, w, i);
-        pos[0][i] = i;
-      }
-    __syncthreads();
+  constexpr uint32_t BINS = 256, THREADS = kOneWaves * 64;
+  __shared__ uint32_t keys[THREADS * PER];
+  __shared__ uint16_t poss[THREADS * PER];
+  __shared__ uint32_t counts[kOneWaves * BINS], first[BINS], part[kOneWaves];
+  const uint32_t w = a.first + blockIdx.x;
+  uint8_t* const seen = seen_of(a, w);
+  uint32_t key[PER], pos[PER], rank[PER], n = a.tokens;
+  each_key<PER>(n, [&](int j, uint32_t i, bool real) {
+    key[j] = real ? token_id(a, w, i) : kNoToken;
+    pos[j] = i;
+  });
+  for (uint32_t i = threadIdx.x; i < seen_words(a.vocab); i += THREADS) ((uint32_t*)seen)[i] = 0;
+  __threadfence();   // before other threads' marks
+  for (int shift = 0; shift == 0 || shift < bits; shift += 8) {
+    for (uint32_t i = threadIdx.x; i < kOneWaves * BINS; i += THREADS) counts[i] = 0;
     // Tokens outside the table are left out by the first pass.
-    auto digit = [&](uint32_t i) { return key[from][i] == 0xFFFFFFFFu ? BINS : key[from][i] >> shift & (BINS - 1); };
-    count_keys<kOneWaves>(counts + threadIdx.x / 64 * BINS, BINS, n, digit);
+    auto digit = [&](int j) { return key[j] == kNoToken ? BINS : key[j] >> shift & (BINS - 1); };
     __syncthreads();
-    for (uint32_t b = threadIdx.x; b < BINS; b += threads) {
+    uint32_t* const own = counts + threadIdx.x / 64 * BINS;
+    rank_keys<PER>(digit, rank, own, BINS, 8);
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < BINS; b += THREADS) {
       uint32_t sum = 0;
+#pragma unroll
       for (int v = 0; v < kOneWaves; ++v) sum += counts[v * BINS + b];
       first[b] = sum;
     }
     __syncthreads();
-    const uint32_t left = scan_bins<kOneWaves>(first, BINS, part);
+    n = scan_bins<kOneWaves>(first, BINS, part);
     places_of_waves<kOneWaves>(counts, first, BINS);
     __syncthreads();
-    place_keys<kOneWaves>(counts + threadIdx.x / 64 * BINS, BINS, 8, n, digit, [&](uint32_t i, uint32_t, uint32_t at) {
-      key[from ^ 1][at] = key[from][i];
-      pos[from ^ 1][at] = pos[from][i];
-    });
-    n = left;
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (key[j] != kNoToken) {
+        const uint32_t at = own[digit(j)] + rank[j];
+        keys[at] = key[j];
+        poss[at] = (uint16_t)pos[j];
+      }
     __syncthreads();
+    each_key<PER>(n, [&](int j, uint32_t i, bool real) {
+      key[j] = real ? keys[i] : kNoToken;
+      pos[j] = real ? poss[i] : 0;
+    });
   }
-  for (uint32_t i = threadIdx.x; i < n; i += threads) {
-    const uint32_t k = key[from][i];
-    a.key[0][(uint64_t)w * a.tokens + i] = k;
-    a.pos[0][(uint64_t)w * a.tokens + i] = pos[from][i];
-    if (i == 0 || key[from][i - 1] != k) atomicOr(&seen[k >> 5], 1u << (k & 31));
-  }
+  each_key<PER>(n, [&](int j, uint32_t i, bool real) {
+    if (!real) return;
+    a.key[0][(uint64_t)w * a.tokens + i] = key[j];
+    a.pos[0][(uint64_t)w * a.tokens + i] = pos[j];
+    seen[key[j]] = 1;
+  });
   if (threadIdx.x == 0) a.real[w] = n;
 }
 
-// Many tokens: a pass over one digit is two launches, counting and placing.  Pass p goes from buffer p & 1 to the other; the first reads the
-// tokens themselves.
-__device__ __forceinline__ uint32_t sort_digit(const EmbedArgs& a, const uint32_t* keys, uint32_t w, uint32_t i) {
-  const uint32_t k = keys ? keys[i] : token_id(a, w, i);
-  return k == 0xFFFFFFFFu ? a.bins : k >> a.shift & (a.bins - 1);
+// Many tokens: a pass over one digit is two launches, counting and placing.  The first pass reads the tokens themselves.
+__device__ __forceinline__ void load_keys(const EmbedArgs& a, const uint32_t* keys, uint32_t w, uint32_t begin, uint32_t n, uint32_t* key) {
+  each_key<kPer>(n, [&](int j, uint32_t i, bool real) { key[j] = !real ? kNoToken : keys ? keys[begin + i] : token_id(a, w, begin + i); });
 }
+
+__device__ __forceinline__ uint32_t sort_digit(const EmbedArgs& a, uint32_t k) { return k == kNoToken ? a.bins : k >> a.shift & (a.bins - 1); }
 
 __global__ __launch_bounds__(kThreads) void k_embed_count(EmbedArgs a, const uint32_t* keys) {
   __shared__ uint32_t counts[kMostBins];
-  const uint32_t block = a.first + blockIdx.x, w = block / a.runs, r = block % a.runs, begin = r * a.run;
-  const uint32_t n = keys ? a.real[w] : a.tokens;
+  const uint32_t block = a.first + blockIdx.x, w = block / a.runs, r = block % a.runs;
+  const uint32_t n = keys ? a.real[w] : a.tokens, end = min(n, (r + 1) * a.run);
   for (uint32_t i = threadIdx.x; i < a.bins; i += kThreads) counts[i] = 0;
   if (!keys) {   // numbers are marked by the last pass
-    uint32_t* const seen = a.seen + (uint64_t)w * seen_words(a.vocab);
-    for (uint32_t i = r * kThreads + threadIdx.x; i < seen_words(a.vocab); i += a.runs * kThreads) seen[i] = 0;
+    uint8_t* const seen = seen_of(a, w);
+    for (uint32_t i = r * kThreads + threadIdx.x; i < seen_words(a.vocab); i += a.runs * kThreads) ((uint32_t*)seen)[i] = 0;
   }
   __syncthreads();
   const uint32_t* const own = keys ? keys + (uint64_t)w * a.tokens : nullptr;
-  if (begin < n)
-    count_keys<kWaves>(counts, a.bins, min(a.run, n - begin), [&](uint32_t i) { return sort_digit(a, own, w, begin + i); });
+  for (uint32_t begin = r * a.run; begin < end; begin += kThreads * kPer) {
+    uint32_t key[kPer], rank[kPer];
+    load_keys(a, own, w, begin, end - begin, key);
+    rank_keys<kPer>([&](int j) { return sort_digit(a, key[j]); }, rank, counts, a.bins, (int)a.bits);
+  }
   __syncthreads();
   for (uint32_t i = threadIdx.x; i < a.bins; i += kThreads) a.counts[((uint64_t)w * a.runs + r) * a.bins + i] = counts[i];
 }
 
 __global__ __launch_bounds__(kThreads) void k_embed_place(EmbedArgs a, const uint32_t* keys, const uint32_t* poss, uint32_t* key_out, uint32_t* pos_out) {
-  __shared__ uint32_t counts[kWaves * kMostBins], first[kMostBins], part[kWaves];
-  const uint32_t block = a.first + blockIdx.x, w = block / a.runs, r = block % a.runs, begin = r * a.run;
-  const uint32_t n = keys ? a.real[w] : a.tokens;
-  const uint32_t* const all = a.counts + (uint64_t)w * a.runs * a.bins;
-  constexpr uint32_t EACH = kMostBins / kThreads;
-  uint32_t ahead[EACH];   // keys of a bin in the runs ahead of this one
-#pragma unroll
-  for (uint32_t j = 0; j < EACH; ++j) {
-    const uint32_t b = j * kThreads + threadIdx.x;
-    ahead[j] = 0;
-    if (b < a.bins) {
-      uint32_t sum = 0;
-      for (uint32_t q = 0; q < a.runs; ++q) {
-        const uint32_t c = all[(uint64_t)q * a.bins + b];
-        if (q == r) ahead[j] = sum;
-        sum += c;
-      }
-      first[b] = sum;
-    }
-  }
-  for (uint32_t i = threadIdx.x; i < kWaves * a.bins; i += kThreads) counts[i] = 0;
-  __syncthreads();
+  __shared__ uint32_t counts[kWaves * kMostBins], first[kMostBins], ahead[kMostBins], part[kWaves];
+  const uint32_t block = a.first + blockIdx.x, w = block / a.runs, r = block % a.runs;
+  const uint32_t n = keys ? a.real[w] : a.tokens, end = min(n, (r + 1) * a.run);
+  sum_runs<kWaves>(a.counts + (uint64_t)w * a.runs * a.bins, a.runs, r, a.bins, first, ahead);
   const uint32_t left = scan_bins<kWaves>(first, a.bins, part);
-#pragma unroll
-  for (uint32_t j = 0; j < EACH; ++j) {
-    const uint32_t b = j * kThreads + threadIdx.x;
-    if (b < a.bins) first[b] += ahead[j];
-  }
+  for (uint32_t b = threadIdx.x; b < a.bins; b += kThreads) first[b] += ahead[b];
   const uint32_t* const own = keys ? keys + (uint64_t)w * a.tokens : nullptr;
-  const uint32_t here = begin < n ? min(a.run, n - begin) : 0;
-  auto digit = [&](uint32_t i) { return sort_digit(a, own, w, begin + i); };
-  count_keys<kWaves>(counts + threadIdx.x / 64 * a.bins, a.bins, here, digit);
-  __syncthreads();
-  places_of_waves<kWaves>(counts, first, a.bins);
-  __syncthreads();
-  uint32_t* const seen = a.seen + (uint64_t)w * seen_words(a.vocab);
-  place_keys<kWaves>(counts + threadIdx.x / 64 * a.bins, a.bins, (int)a.bits, here, digit, [&](uint32_t i, uint32_t, uint32_t at) {
-    const uint32_t k = own ? own[begin + i] : token_id(a, w, begin + i);
-    key_out[(uint64_t)w * a.tokens + at] = k;
-    pos_out[(uint64_t)w * a.tokens + at] = own ? poss[(uint64_t)w * a.tokens + begin + i] : begin + i;
-    if (a.last) atomicOr(&seen[k >> 5], 1u << (k & 31));
-  });
+  uint8_t* const seen = seen_of(a, w);
+  uint32_t* const mine = counts + threadIdx.x / 64 * a.bins;
+  for (uint32_t begin = r * a.run; begin < end; begin += kThreads * kPer) {
+    uint32_t key[kPer], rank[kPer], pos[kPer];
+    load_keys(a, own, w, begin, end - begin, key);
+    auto digit = [&](int j) { return sort_digit(a, key[j]); };
+    each_key<kPer>(end - begin, [&](int j, uint32_t i, bool real) { pos[j] = !real ? 0 : own ? poss[(uint64_t)w * a.tokens + begin + i] : begin + i; });
+    for (uint32_t i = threadIdx.x; i < kWaves * a.bins; i += kThreads) counts[i] = 0;
+    __syncthreads();
+    rank_keys<kPer>(digit, rank, mine, a.bins, (int)a.bits);
+    __syncthreads();
+    places_of_waves<kWaves>(counts, first, a.bins);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (key[j] != kNoToken) {
+        const uint64_t at = (uint64_t)w * a.tokens + mine[digit(j)] + rank[j];
+        key_out[at] = key[j];
+        pos_out[at] = pos[j];
+        if (a.last) seen[key[j]] = 1;
+      }
+    __syncthreads();
+  }
   // All passes place the same tokens, so that what the first finds holds for the others.
   if (!keys && r == 0 && threadIdx.x == 0) a.real[w] = left;
 }
@@ -204,31 +218,31 @@ __device__ __forceinline__ void leave_sum(const EmbedArgs& a, uint32_t w, uint32
   store_upto<E>(p, n, v);
 }
 
-template <typename T>
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_embed_sum(EmbedArgs a) {
   constexpr int E = 16 / sizeof(T);
   constexpr uint32_t AHEAD = 8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t group = (uint64_t)a.first + blockIdx.x;
+  const uint32_t group = a.first + blockIdx.x;
   if (group >= a.sum_groups) {   // rows that no token names
-    const uint64_t sets = (a.vocab + kZeroRows - 1) / kZeroRows, job = (group - a.sum_groups) * kWaves + wave;
-    const uint32_t w = (uint32_t)(job / sets), v0 = (uint32_t)(job % sets) * kZeroRows;
+    const uint32_t sets = (a.vocab + kZeroRows - 1) / kZeroRows, job = (group - a.sum_groups) * kWaves + wave;
+    const uint32_t w = job / sets, v0 = job % sets * kZeroRows;
     if (w >= a.workers) return;
-    const uint32_t word = a.seen[(uint64_t)w * seen_words(a.vocab) + (v0 >> 5)] >> (v0 & 31);
-    const float zero[E] = {};
+    const uint32_t marks = *(const uint32_t*)(seen_of(a, w) + v0);   // of four rows
+    const Pack<T, E> zero = {};
     for (uint32_t v = v0; v < min(v0 + kZeroRows, a.vocab); ++v) {
-      if (word >> (v - v0) & 1) continue;
+      if (marks >> (v - v0) * 8 & 1) continue;
       T* const p = (T*)a.table.p + (int64_t)w * a.table.worker + (int64_t)v * a.table.row;
-      for (uint32_t col = lane * E; col < a.width; col += 64 * E) store_upto<E>(p + col, (int)(a.width - col), zero);
+      for (uint32_t col = lane * E; col < a.width; col += 64 * E) store_pack<E, ONCE>(p + col, (int)(a.width - col), zero);
     }
     return;
   }
-  const uint64_t job = group * kWaves + wave, line = job / a.blocks;
-  const uint32_t w = (uint32_t)(line / a.chunks), c = (uint32_t)(line % a.chunks);
+  const uint32_t job = group * kWaves + wave, line = job / a.blocks;
+  const uint32_t w = line / a.chunks, c = line % a.chunks;
   if (w >= a.workers) return;
   const uint32_t real = a.real[w], begin = c * kChunk;
   if (begin >= real) return;
-  const uint32_t m = min(kChunk, real - begin), col = (uint32_t)(job % a.blocks) * 64 * E + lane * E;
+  const uint32_t m = min(kChunk, real - begin), col = job % a.blocks * 64 * E + lane * E;
   const int n = (int)a.width - (int)col;
   const uint32_t* const keys = a.key[0] + (uint64_t)w * a.tokens;
   const uint32_t* const poss = a.pos[0] + (uint64_t)w * a.tokens;
@@ -246,13 +260,19 @@ __global__ __launch_bounds__(kThreads) void k_embed_sum(EmbedArgs a) {
       else leave_sum<E, T>(a, w, now, col, n, acc);
     }
   };
-  for (uint32_t i = 0; i < m; i += AHEAD) {
-    float v[AHEAD][E];
+  Pack<T, E> v[2][AHEAD];   // the next rows are under way while these are added
+  auto ask = [&](uint32_t i, int to) {
 #pragma unroll
     for (uint32_t j = 0; j < AHEAD; ++j) {
       const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)my_pos, (int)min(i + j, m - 1));
-      load_upto<E>(dy + (int64_t)at * a.rows.row, n, v[j]);
+      if (i < m) v[to][j] = load_pack<E, ONCE>(dy + (int64_t)at * a.rows.row, n);
     }
+  };
+  ask(0, 0);
+#pragma unroll
+  for (uint32_t i = 0; i < kChunk; i += AHEAD) {
+    if (i >= m) break;
+    ask(i + AHEAD, (i / AHEAD + 1) & 1);
 #pragma unroll
     for (uint32_t j = 0; j < AHEAD; ++j) {
       if (i + j >= m) break;
@@ -265,40 +285,50 @@ __global__ __launch_bounds__(kThreads) void k_embed_sum(EmbedArgs a) {
         for (int e = 0; e < E; ++e) acc[e] = 0.f;
       }
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += v[j][e];
+      for (int e = 0; e < E; ++e) acc[e] += to_f(v[(i / AHEAD) & 1][j].v[e]);
     }
   }
   leave(true);
 }
 
-// The numbers that go on from chunk c, where they begin, into the next ones.
+// The numbers that go on from chunk c, where they begin, into the next ones.  A wavefront has 256 columns, sixteen partial sums under way at once: a number that
+// every sixteenth of 16384 tokens has goes through 64 chunks.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_embed_join(EmbedArgs a) {
-  constexpr int E = 16 / sizeof(T);
+  constexpr int E = 4, AT_ONCE = 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t job = ((uint64_t)a.first + blockIdx.x) * kWaves + wave, line = job / a.blocks;
-  const uint32_t w = (uint32_t)(line / a.chunks), c = (uint32_t)(line % a.chunks);
+  const uint32_t job = (a.first + blockIdx.x) * kWaves + wave, across = (a.width + 64 * E - 1) / (64 * E), line = job / across;
+  const uint32_t w = line / a.chunks, c = line % a.chunks;
   if (w >= a.workers) return;
   const uint32_t real = a.real[w], begin = c * kChunk;
   if (begin + kChunk >= real) return;
   const uint32_t* const keys = a.key[0] + (uint64_t)w * a.tokens;
-  const uint32_t k = keys[begin + kChunk - 1];
-  if (keys[begin + kChunk] != k) return;
-  if (begin && keys[begin] == k && keys[begin - 1] == k) return;   // begins further ahead
-  const uint32_t col = (uint32_t)(job % a.blocks) * 64 * E + lane * E;
+  const uint32_t k = keys[begin + kChunk - 1], next = keys[begin + kChunk], head = keys[begin], before = begin ? keys[begin - 1] : kNoToken;
+  if (next != k || (head == k && before == k)) return;   // ends here, or begins further ahead
+  const uint32_t col = (job % across * 64 + lane) * E;
   const int n = (int)a.width - (int)col;
-  if (n <= 0) return;
   const float* p = a.partial + ((uint64_t)w * a.chunks + c) * 2 * a.width + col;
   float acc[E];
   load_upto<E>(p + a.width, n, acc);
-  for (uint32_t at = begin + kChunk; at < real && keys[at] == k; at += kChunk) {
-    p += 2 * (uint64_t)a.width;
-    float v[E];
-    load_upto<E>(p, n, v);
+  for (uint32_t at = begin + kChunk;;) {
+    // In how many of the next 64 chunks does it go on?
+    const uint64_t there = at + (uint64_t)lane * kChunk;
+    const uint64_t not_on = ~__ballot(there < real && keys[there] == k);
+    const int on = not_on ? __ffsll((unsigned long long)not_on) - 1 : 64;
+    for (int i = 0; i < on; i += AT_ONCE) {
+      float v[AT_ONCE][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] += v[e];
+      for (int j = 0; j < AT_ONCE; ++j) load_upto<E>(p + (uint64_t)(min(i + j, on - 1) + 1) * 2 * a.width, n, v[j]);
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += i + j < on ? v[j][e] : 0.f;
+    }
+    if (on < 64) break;
+    p += 64 * 2 * (uint64_t)a.width;
+    at += 64 * kChunk;
   }
-  leave_sum<E, T>(a, w, k, col, n, acc);
+  if (n > 0) leave_sum<E, T>(a, w, k, col, n, acc);
 }
 
 }  // namespace
@@ -362,7 +392,7 @@ EmbedArgs embed_args(const evg_embed* c, uint32_t tokens, const evg_ids* ids, co
   if (g.workers <= 1) a.table.worker = a.rows.worker = 0;
   if (tokens <= 1) a.rows.row = 0;
   if (g.vocab <= 1) a.table.row = 0;
-  a.workers = g.workers, a.tokens = tokens, a.vocab = g.vocab, a.width = g.width;
+  a.workers = g.workers, a.lines = g.workers * tokens, a.tokens = tokens, a.vocab = g.vocab, a.width = g.width;
   const uint32_t across = 64 * 16 / type_bytes(g.type);
   a.blocks = (g.width + across - 1) / across;
   a.scale = g.scale;
@@ -370,13 +400,37 @@ EmbedArgs embed_args(const evg_embed* c, uint32_t tokens, const evg_ids* ids, co
 }
 
 template <typename T>
+hipError_t embed_forward(const evg_embed* c, EmbedArgs& a) {
+  const uint64_t units = (uint64_t)a.lines * a.blocks;
+  // Few units go to a wavefront each: the chip has room for 8192 of them.
+  const uint32_t each = units <= 8192 ? 1 : 4;
+  const uint64_t groups = (units + each * kWaves - 1) / (each * kWaves);
+  return launch(groups, kThreads, c->stream, a, each == 1 ? k_embed_rows<T, 1> : k_embed_rows<T, 4>);
+}
+
+template <typename T>
+hipError_t embed_sums(const evg_embed* c, EmbedArgs& a) {
+  a.chunks = (a.tokens + kChunk - 1) / kChunk;
+  const uint64_t groups = ((uint64_t)a.workers * a.chunks * a.blocks + kWaves - 1) / kWaves;
+  const uint64_t zero = a.accumulate ? 0 : ((uint64_t)a.workers * ((a.vocab + kZeroRows - 1) / kZeroRows) + kWaves - 1) / kWaves;
+  a.sum_groups = (uint32_t)groups;
+  const bool once = (uint64_t)a.workers * a.vocab * a.width * sizeof(T) > (128u << 20);   // half of the last-level cache
+  const hipError_t e = launch(groups + zero, kThreads, c->stream, a, once ? k_embed_sum<T, true> : k_embed_sum<T, false>);
+  if (e != hipSuccess || a.chunks <= 1) return e;
+  const uint64_t joins = (uint64_t)a.workers * a.chunks * ((a.width + 255) / 256);
+  return launch((joins + kWaves - 1) / kWaves, kThreads, c->stream, a, k_embed_join<T>);
+}
+
+template <typename T>
 hipError_t embed_backward(const evg_embed* c, EmbedArgs& a) {
   hipStream_t s = c->stream;
   hipError_t e;
   if (a.tokens <= kOneSort) {
-    if ((e = launch(a.workers, kOneWaves * 64, s, a, k_embed_sort_alone, c->bits)) != hipSuccess) return e;
+    const uint32_t per = (a.tokens + kOneWaves * 64 - 1) / (kOneWaves * 64);
+    if ((e = launch(a.workers, kOneWaves * 64, s, a, per <= 1 ? k_embed_sort_alone<1> : k_embed_sort_alone<kPer>, c->bits)) != hipSuccess)
+      return e;
   } else {
-    const Runs runs = cut_runs(a.tokens);
+    const Runs runs = cut_runs(a.tokens, kThreads * kPer);
     a.run = runs.each, a.runs = runs.count;
     a.bits = (c->bits + c->passes - 1) / c->passes;
     a.bins = 1u << a.bits;
@@ -390,12 +444,7 @@ hipError_t embed_backward(const evg_embed* c, EmbedArgs& a) {
       if ((e = launch((uint64_t)a.workers * a.runs, kThreads, s, a, k_embed_place, keys, (const uint32_t*)a.pos[to ^ 1], a.key[to], a.pos[to])) != hipSuccess) return e;
     }
   }
-  a.chunks = (a.tokens + kChunk - 1) / kChunk;
-  const uint64_t jobs = (uint64_t)a.workers * a.chunks * a.blocks, groups = (jobs + kWaves - 1) / kWaves;
-  const uint64_t zero = a.accumulate ? 0 : ((uint64_t)a.workers * ((a.vocab + kZeroRows - 1) / kZeroRows) + kWaves - 1) / kWaves;
-  a.sum_groups = (uint32_t)groups;
-  if ((e = launch(groups + zero, kThreads, s, a, k_embed_sum<T>)) != hipSuccess) return e;
-  return a.chunks > 1 ? launch(groups, kThreads, s, a, k_embed_join<T>) : hipSuccess;
+  return embed_sums<T>(c, a);
 }
 
 }  // namespace
@@ -411,6 +460,10 @@ evg_status evg_embed_init(evg_embed** out, const evg_embed_config* cfg, void* hi
   if (cfg->max_tokens > (1u << 26)) return fail(EVG_ERR_INVALID, "max_tokens must be at most 2^26");
   evg_status st;
   if ((st = check_type(cfg->type, "type")) != EVG_OK) return st;
+  // Kernels count units of 64 vectors, and sets of rows, in 32 bits.
+  const uint64_t across = ((uint64_t)cfg->width * type_bytes(cfg->type) + 1023) / 1024;
+  if (cfg->workers * (uint64_t)cfg->max_tokens * across > 0x7FFFFFFFull || cfg->workers * (uint64_t)cfg->vocab > 0x7FFFFFFFull)
+    return fail(EVG_ERR_INVALID, "workers, width and max_tokens or vocab together are out of range");
   if (!std::isfinite(cfg->scale)) return fail(EVG_ERR_INVALID, "scale must be finite");
   evg_embed* c = new (std::nothrow) evg_embed();
   if (!c) return fail(EVG_ERR_OOM, "host allocation failed");
@@ -422,10 +475,10 @@ evg_status evg_embed_init(evg_embed** out, const evg_embed_config* cfg, void* hi
     const uint64_t W = cfg->workers, T = cfg->max_tokens;
     const bool many = T > kOneSort;
     // Fewer tokens may be cut into as many runs.
-    const uint32_t bins = 1u << ((c->bits + c->passes - 1) / c->passes), runs = many ? 128 : 0;
+    const uint32_t bins = 1u << ((c->bits + c->passes - 1) / c->passes), runs = many ? kMostRuns : 0;
     const uint64_t chunks = (T + kChunk - 1) / kChunk;
     const uint64_t words[] = {W * T, W * T, many && c->passes > 1 ? W * T : 0, many && c->passes > 1 ? W * T : 0, W * runs * bins, W,
-                              W * ((cfg->vocab + 31) / 32), chunks > 1 ? W * chunks * 2 * cfg->width : 0};
+                              W * ((cfg->vocab + 3) / 4), chunks > 1 ? W * chunks * 2 * cfg->width : 0};
     uint64_t total = 0;
     for (uint64_t n : words) total += (n + 63) / 64 * 64;
     const hipError_t e = total >> 46 ? hipErrorOutOfMemory : hipMalloc(&c->owned, total * 4);
@@ -435,7 +488,7 @@ evg_status evg_embed_init(evg_embed** out, const evg_embed_config* cfg, void* hi
       return fail(e == hipErrorOutOfMemory ? EVG_ERR_OOM : EVG_ERR_HIP, "workspace: %s", hipGetErrorString(e));
     }
     uint32_t* p = (uint32_t*)c->owned;
-    uint32_t** const to[] = {&c->at.key[0], &c->at.pos[0], &c->at.key[1], &c->at.pos[1], &c->at.counts, &c->at.real, &c->at.seen, (uint32_t**)&c->at.partial};
+    uint32_t** const to[] = {&c->at.key[0], &c->at.pos[0], &c->at.key[1], &c->at.pos[1], &c->at.counts, &c->at.real, (uint32_t**)&c->at.seen, (uint32_t**)&c->at.partial};
     for (int i = 0; i < 8; ++i) {
       *to[i] = p;
       p += (words[i] + 63) / 64 * 64;
@@ -458,11 +511,7 @@ evg_status evg_embed_forward(evg_embed* c, uint32_t tokens, const evg_ids* ids, 
   if ((st = check_apart(outs, 1, ins, 2)) != EVG_OK) return st;
   if (!tokens) return EVG_OK;
   EmbedArgs a = embed_args(c, tokens, ids, table, y);
-  const uint64_t groups = ((uint64_t)g.workers * tokens * a.blocks + kWaves - 1) / kWaves;
-  if (groups > 0x7FFFFFFFull) return fail(EVG_ERR_INVALID, "tokens is out of range");
-  HIP_TRY(g.type == EVG_F32   ? launch(groups, kThreads, c->stream, a, k_embed_rows<float>)
-          : g.type == EVG_F16 ? launch(groups, kThreads, c->stream, a, k_embed_rows<half_t>)
-                              : launch(groups, kThreads, c->stream, a, k_embed_rows<bf16_t>));
+  HIP_TRY(g.type == EVG_F32 ? embed_forward<float>(c, a) : g.type == EVG_F16 ? embed_forward<half_t>(c, a) : embed_forward<bf16_t>(c, a));
   return EVG_OK;
 }
 
@@ -480,8 +529,6 @@ evg_status evg_embed_backward(evg_embed* c, uint32_t tokens, const evg_ids* ids,
   if ((st = check_apart(outs, 1, ins, 2)) != EVG_OK) return st;
   EmbedArgs a = embed_args(c, tokens, ids, d_table, dy);
   a.accumulate = accumulate != 0;
-  const uint64_t rows = (uint64_t)g.workers * g.vocab, sums = (uint64_t)g.workers * ((tokens + kChunk - 1) / kChunk) * a.blocks;
-  if ((rows / kZeroRows + g.workers + sums) / kWaves > 0x7FFF0000ull) return fail(EVG_ERR_INVALID, "vocab or tokens is out of range");
   HIP_TRY(g.type == EVG_F32 ? embed_backward<float>(c, a) : g.type == EVG_F16 ? embed_backward<half_t>(c, a) : embed_backward<bf16_t>(c, a));
   return EVG_OK;
 }

@@ -19,8 +19,9 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kOneWaves = 16;
-constexpr uint32_t kOneSort = 8192;     // most entries of a worker that one workgroup places
-constexpr uint32_t kEmptySlots = 64;    // slots that a wavefront looks through
+constexpr int kOnePer = 8, kPer = 4;    // entries of a thread in a round
+constexpr uint32_t kOneSort = kOneWaves * 64 * kOnePer;   // most entries of a worker that one workgroup places
+constexpr uint32_t kEmptySlots = 8;     // slots that a wavefront looks through
 
 struct ExpertsArgs {
   evg_mat x, rows, d_rows;     // tokens' rows (x, y, dy) and slots' rows
@@ -31,8 +32,8 @@ struct ExpertsArgs {
   uint32_t workers, tokens, experts, top, width, capacity, slots, first;
   uint32_t run, runs, bits;
   uint32_t* run_counts;        // [workers][runs][experts]
-  uint32_t blocks;             // column blocks of a token's row
-  uint64_t token_groups;       // workgroups ahead of those that look for empty slots
+  uint32_t blocks, lines;      // blocks: of 64 vectors across a row; lines: workers * tokens
+  uint32_t token_groups;       // workgroups ahead of those that look for empty slots
 };
 
 // ---- the plan ------------------------------------------------------------------------------------------------------------------
@@ -44,59 +45,67 @@ __device__ __forceinline__ uint32_t expert_of(const ExpertsArgs& a, uint32_t w, 
 
 __global__ __launch_bounds__(kThreads) void k_experts_count(ExpertsArgs a) {
   __shared__ uint32_t counts[kMostBins];
-  const uint32_t block = a.first + blockIdx.x, w = block / a.runs, r = block % a.runs, n = a.tokens * a.top, begin = r * a.run;
+  const uint32_t block = a.first + blockIdx.x, w = block / a.runs, r = block % a.runs, end = min(a.tokens * a.top, (r + 1) * a.run);
   for (uint32_t i = threadIdx.x; i < a.experts; i += kThreads) counts[i] = 0;
   __syncthreads();
-  count_keys<kWaves>(counts, a.experts, min(a.run, n - begin), [&](uint32_t i) { return expert_of(a, w, begin + i); });
+  for (uint32_t begin = r * a.run; begin < end; begin += kThreads * kPer) {
+    uint32_t key[kPer], rank[kPer];
+    each_key<kPer>(end - begin, [&](int j, uint32_t i, bool real) { key[j] = real ? expert_of(a, w, begin + i) : a.experts; });
+    rank_keys<kPer>([&](int j) { return key[j]; }, rank, counts, a.experts, (int)a.bits);
+  }
   __syncthreads();
   for (uint32_t i = threadIdx.x; i < a.experts; i += kThreads) a.run_counts[((uint64_t)w * a.runs + r) * a.experts + i] = counts[i];
 }
 
-// ALONE: the workgroup has all of a worker's entries.
-template <bool ALONE, int WAVES>
+// ALONE: the workgroup has all of a worker's entries, one round of them.
+template <bool ALONE, int WAVES, int PER>
 __global__ __launch_bounds__(WAVES * 64) void k_experts_place(ExpertsArgs a) {
-  constexpr uint32_t THREADS = WAVES * 64, EACH = (kMostBins + THREADS - 1) / THREADS;
+  constexpr uint32_t THREADS = WAVES * 64;
   __shared__ uint32_t counts[WAVES * kMostBins], first[kMostBins], ahead[kMostBins], part[WAVES];
   const uint32_t block = a.first + blockIdx.x, w = ALONE ? block : block / a.runs, r = ALONE ? 0 : block % a.runs;
-  const uint32_t n = a.tokens * a.top, begin = ALONE ? 0 : r * a.run, here = ALONE ? n : min(a.run, n - begin), E = a.experts;
+  const uint32_t n = a.tokens * a.top, E = a.experts, end = ALONE ? n : min(n, (r + 1) * a.run);
   int32_t* const slot = a.slot + (uint64_t)w * n;
   int32_t* const source = a.source + (uint64_t)w * a.slots;
-  for (uint32_t i = threadIdx.x; i < WAVES * E; i += THREADS) counts[i] = 0;
-  __syncthreads();
-  auto key = [&](uint32_t i) { return expert_of(a, w, begin + i); };
-  count_keys<WAVES>(counts + threadIdx.x / 64 * E, E, here, key);
-  __syncthreads();
-#pragma unroll
-  for (uint32_t j = 0; j < EACH; ++j) {
-    const uint32_t e = j * THREADS + threadIdx.x;
-    if (e < E) {
-      uint32_t sum = 0, before = 0;
-      if constexpr (ALONE) {
-        for (int v = 0; v < WAVES; ++v) sum += counts[v * E + e];
-      } else {
-        const uint32_t* c = a.run_counts + (uint64_t)w * a.runs * E + e;
-        for (uint32_t q = 0; q < a.runs; ++q, c += E) {
-          if (q == r) before = sum;
-          sum += *c;
-        }
-      }
-      first[e] = sum;
-      ahead[e] = before;
-      if (r == 0) a.counts[(uint64_t)w * E + e] = (int32_t)sum;
-    }
+  uint32_t* const mine = counts + threadIdx.x / 64 * E;
+  if constexpr (!ALONE) {
+    sum_runs<WAVES>(a.run_counts + (uint64_t)w * a.runs * E, a.runs, r, E, first, ahead);
+    if (r == 0)
+      for (uint32_t e = threadIdx.x; e < E; e += THREADS) a.counts[(uint64_t)w * E + e] = (int32_t)first[e];
+    if (!a.capacity) scan_bins<WAVES>(first, E, part);
   }
-  __syncthreads();
-  if (!a.capacity) scan_bins<WAVES>(first, E, part);
-  places_of_waves<WAVES>(counts, ahead, E);   // ranks among the expert's entries
-  __syncthreads();
-  place_keys<WAVES>(counts + threadIdx.x / 64 * E, E, (int)a.bits, here, key, [&](uint32_t i, uint32_t e, uint32_t rank) {
-    const bool fits = !a.capacity || rank < a.capacity;
-    const uint32_t at = a.capacity ? e * a.capacity + rank : first[e] + rank;
-    slot[begin + i] = fits ? (int32_t)at : -1;
-    if (fits) source[at] = (int32_t)(begin + i);
-  });
-  for (uint32_t i = threadIdx.x; i < here; i += THREADS)
-    if (key(i) >= E) slot[begin + i] = -1;
+  uint32_t begin = ALONE ? 0 : r * a.run;
+  do {
+    uint32_t key[PER], rank[PER];
+    each_key<PER>(end - begin, [&](int j, uint32_t i, bool real) { key[j] = real ? expert_of(a, w, begin + i) : E; });
+    for (uint32_t i = threadIdx.x; i < WAVES * E; i += THREADS) counts[i] = 0;
+    __syncthreads();
+    rank_keys<PER>([&](int j) { return key[j]; }, rank, mine, E, (int)a.bits);
+    __syncthreads();
+    if constexpr (ALONE) {
+      for (uint32_t e = threadIdx.x; e < E; e += THREADS) {
+        uint32_t sum = 0;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) sum += counts[v * E + e];
+        first[e] = sum;
+        ahead[e] = 0;
+        a.counts[(uint64_t)w * E + e] = (int32_t)sum;
+      }
+      __syncthreads();
+      if (!a.capacity) scan_bins<WAVES>(first, E, part);
+    }
+    places_of_waves<WAVES>(counts, ahead, E);   // ranks among the expert's entries
+    __syncthreads();
+    each_key<PER>(end - begin, [&](int j, uint32_t i, bool real) {
+      if (!real) return;
+      const uint32_t e = key[j], at_expert = e < E ? mine[e] + rank[j] : 0;
+      const bool fits = e < E && (!a.capacity || at_expert < a.capacity);
+      const uint32_t at = !fits ? 0 : a.capacity ? e * a.capacity + at_expert : first[e] + at_expert;
+      slot[begin + i] = fits ? (int32_t)at : -1;
+      if (fits) source[at] = (int32_t)(begin + i);
+    });
+    begin += THREADS * PER;
+    if constexpr (!ALONE) __syncthreads();
+  } while (begin < end);
 }
 
 // ---- rows ----------------------------------------------------------------------------------------------------------------------
@@ -104,15 +113,15 @@ __global__ __launch_bounds__(WAVES * 64) void k_experts_place(ExpertsArgs a) {
 // A slot that the tensors have, whatever the plan holds.
 __device__ __forceinline__ bool real_slot(const ExpertsArgs& a, int32_t s) { return (uint32_t)s < a.slots; }
 
-// Zeroes the rows of the empty ones among 64 slots.  PLANNED: the plan's sources tell which they are; else the counts do, and the sources are written.
+// Zeroes the rows of the empty ones among a few slots.  PLANNED: the plan's sources tell which they are; else the counts do, and the sources are written.
 template <typename T, bool PLANNED>
-__device__ __forceinline__ void zero_empty(const ExpertsArgs& a, const evg_mat& rows, uint64_t job, int lane) {
+__device__ __forceinline__ void zero_empty(const ExpertsArgs& a, const evg_mat& rows, uint32_t job, int lane) {
   constexpr int E = 16 / sizeof(T);
-  const uint32_t sets = (a.slots + kEmptySlots - 1) / kEmptySlots, w = (uint32_t)(job / sets), s0 = (uint32_t)(job % sets) * kEmptySlots;
+  const uint32_t sets = (a.slots + kEmptySlots - 1) / kEmptySlots, w = job / sets, s0 = job % sets * kEmptySlots;
   if (w >= a.workers) return;
   const uint32_t mine = s0 + lane;
   int32_t* const source = a.source + (uint64_t)w * a.slots;
-  bool empty = mine < a.slots;
+  bool empty = lane < (int)kEmptySlots && mine < a.slots;
   if constexpr (PLANNED) {
     empty = empty && source[mine] < 0;
   } else {
@@ -135,119 +144,143 @@ __device__ __forceinline__ void zero_empty(const ExpertsArgs& a, const evg_mat& 
   }
 }
 
-// rows[slot] = x[t].  A wavefront has 64 vectors of a token's row.
-template <typename T>
+// A unit is 64 vectors of a token's row; a wavefront has U neighbouring ones.
+struct Unit { uint32_t line, block; };
+
+__device__ __forceinline__ void next_unit(const ExpertsArgs& a, Unit& u) {
+  if (++u.block == a.blocks) u.block = 0, ++u.line;
+}
+
+// rows[slot] = x[t].
+template <typename T, int U, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_experts_dispatch(ExpertsArgs a) {
   constexpr int E = 16 / sizeof(T);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t group = (uint64_t)a.first + blockIdx.x;
+  const uint32_t group = a.first + blockIdx.x;
   if (group >= a.token_groups) {
     zero_empty<T, false>(a, a.rows, (group - a.token_groups) * kWaves + wave, lane);
     return;
   }
-  const uint64_t job = group * kWaves + wave, line = job / a.blocks;
-  if (line >= (uint64_t)a.workers * a.tokens) return;
-  const uint32_t w = (uint32_t)(line / a.tokens), t = (uint32_t)(line % a.tokens), col = (uint32_t)(job % a.blocks) * 64 * E + lane * E;
-  const int n = (int)a.width - (int)col;
-  if (n <= 0) return;
-  const T* const p = (const T*)a.x.p + (int64_t)w * a.x.worker + (int64_t)t * a.x.row + col;
-  T* const out = (T*)a.rows.p + (int64_t)w * a.rows.worker + col;
-  const int32_t* const slot = a.slot + line * a.top;
-  float v[E];
-  load_upto<E>(p, n, v);
+  const uint32_t first = (group * kWaves + wave) * U;
+  const Unit start{first / a.blocks, first % a.blocks};
+  Pack<T, E> v[U];
+  Unit at = start;
+#pragma unroll
+  for (int u = 0; u < U; ++u, next_unit(a, at)) {
+    const uint32_t w = at.line / a.tokens, t = at.line % a.tokens, col = (at.block * 64 + lane) * E;
+    if (at.line < a.lines) v[u] = load_pack<E>((const T*)a.x.p + (int64_t)w * a.x.worker + (int64_t)t * a.x.row + col, (int)a.width - (int)col);
+  }
+  // A slot's units one after the other: whole rows where a wavefront has them.
   for (uint32_t k = 0; k < a.top; ++k) {
-    const int32_t s = slot[k];
-    if (real_slot(a, s)) store_upto<E>(out + (int64_t)s * a.rows.row, n, v);
+    at = start;
+#pragma unroll
+    for (int u = 0; u < U; ++u, next_unit(a, at)) {
+      if (at.line >= a.lines) break;
+      const uint32_t w = at.line / a.tokens, col = (at.block * 64 + lane) * E;
+      const int32_t s = a.slot[(uint64_t)at.line * a.top + k];
+      T* const out = (T*)a.rows.p + (int64_t)w * a.rows.worker + col;
+      if (real_slot(a, s)) store_pack<E, ONCE>(out + (int64_t)s * a.rows.row, (int)a.width - (int)col, v[u]);
+    }
   }
 }
 
-// y[t] = sum over k of weights[i] rows[slot[i]].
-template <typename T>
+// y[t] = sum over k of weights[i] rows[slot[i]], KS rows under way at once.
+template <typename T, uint32_t KS, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_experts_combine(ExpertsArgs a) {
   constexpr int E = 16 / sizeof(T);
-  constexpr uint32_t AHEAD = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t job = ((uint64_t)a.first + blockIdx.x) * kWaves + wave, line = job / a.blocks;
-  if (line >= (uint64_t)a.workers * a.tokens) return;
-  const uint32_t w = (uint32_t)(line / a.tokens), t = (uint32_t)(line % a.tokens), col = (uint32_t)(job % a.blocks) * 64 * E + lane * E;
+  const uint32_t job = (a.first + blockIdx.x) * kWaves + wave, line = job / a.blocks;
+  if (line >= a.lines) return;
+  const uint32_t w = line / a.tokens, t = line % a.tokens, col = (job % a.blocks * 64 + lane) * E;
   const int n = (int)a.width - (int)col;
-  if (n <= 0) return;
   const T* const p = (const T*)a.rows.p + (int64_t)w * a.rows.worker + col;
-  const int32_t* const slot = a.slot + line * a.top;
-  const float* const weights = a.weights + line * a.top;
+  const int32_t* const slot = a.slot + (uint64_t)line * a.top;
+  const float* const weights = a.weights + (uint64_t)line * a.top;
   float acc[E] = {};
-  for (uint32_t k = 0; k < a.top; k += AHEAD) {
-    float v[AHEAD][E], f[AHEAD];
+  for (uint32_t k = 0; k < a.top; k += KS) {
+    Pack<T, E> v[KS];
+    float f[KS];
 #pragma unroll
-    for (uint32_t j = 0; j < AHEAD; ++j) {
+    for (uint32_t j = 0; j < KS; ++j) {
       const int32_t s = k + j < a.top ? slot[k + j] : -1;
       const bool real = real_slot(a, s);
       f[j] = real ? (a.weights ? weights[k + j] : 1.f) : 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[j][e] = 0.f;
-      if (real) load_upto<E>(p + (int64_t)s * a.rows.row, n, v[j]);
+      v[j] = load_pack<E, ONCE>(p + (real ? (int64_t)s * a.rows.row : 0), real ? n : 0);
     }
 #pragma unroll
-    for (uint32_t j = 0; j < AHEAD; ++j)
+    for (uint32_t j = 0; j < KS; ++j)
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = fmaf(f[j], v[j][e], acc[e]);
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(f[j], to_f(v[j].v[e]), acc[e]);
   }
   store_upto<E>((T*)a.x.p + (int64_t)w * a.x.worker + (int64_t)t * a.x.row + col, n, acc);
 }
 
-// d_rows[slot] = weights[i] dy[t], d_weights[i] = <dy[t], rows[slot]>.  A wavefront has a token's whole row, four experts at a time.
-template <typename T>
+// d_rows[slot] = weights[i] dy[t], d_weights[i] = <dy[t], rows[slot]>.  A wavefront has a token, BLOCKS units of its row at a time: those of dy stay, the
+// experts' go by, the next one's asked for ahead.
+template <typename T, int BLOCKS, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_experts_combine_backward(ExpertsArgs a) {
   constexpr int E = 16 / sizeof(T);
-  constexpr uint32_t AT_ONCE = 4;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint64_t group = (uint64_t)a.first + blockIdx.x;
+  const uint32_t group = a.first + blockIdx.x;
   if (group >= a.token_groups) {
     zero_empty<T, true>(a, a.d_rows, (group - a.token_groups) * kWaves + wave, lane);
     return;
   }
-  const uint64_t line = group * kWaves + wave;
-  if (line >= (uint64_t)a.workers * a.tokens) return;
-  const uint32_t w = (uint32_t)(line / a.tokens), t = (uint32_t)(line % a.tokens);
+  const uint32_t line = group * kWaves + wave;
+  if (line >= a.lines) return;
+  const uint32_t w = line / a.tokens, t = line % a.tokens;
   const T* const dy = (const T*)a.x.p + (int64_t)w * a.x.worker + (int64_t)t * a.x.row;
   const T* const rows = (const T*)a.rows.p + (int64_t)w * a.rows.worker;
   T* const d_rows = (T*)a.d_rows.p + (int64_t)w * a.d_rows.worker;
-  for (uint32_t k = 0; k < a.top; k += AT_ONCE) {
-    int32_t s[AT_ONCE];
-    float f[AT_ONCE], sum[AT_ONCE];
-    bool real[AT_ONCE];
+  const int32_t* const slot = a.slot + (uint64_t)line * a.top;
+  const float* const weights = a.weights + (uint64_t)line * a.top;
+  for (uint32_t first = 0; first < a.width; first += BLOCKS * 64 * E) {
+    Pack<T, E> g[BLOCKS], v[2][BLOCKS];
+    int n[BLOCKS];
+    uint32_t col[BLOCKS];
 #pragma unroll
-    for (uint32_t j = 0; j < AT_ONCE; ++j) {
-      s[j] = k + j < a.top ? a.slot[line * a.top + k + j] : -1;
-      real[j] = real_slot(a, s[j]);
-      f[j] = real[j] ? a.weights[line * a.top + k + j] : 0.f;
-      sum[j] = 0.f;
+    for (int u = 0; u < BLOCKS; ++u) {
+      col[u] = first + (u * 64 + lane) * E;
+      n[u] = (int)a.width - (int)col[u];
+      g[u] = load_pack<E>(dy + col[u], n[u]);
     }
-    for (uint32_t col = lane * E; col < a.width; col += 64 * E) {
-      const int n = (int)(a.width - col);
-      float g[E];
-      load_upto<E>(dy + col, n, g);
+    auto ask = [&](uint32_t k, int to) {
+      const int32_t s = k < a.top ? slot[k] : -1;
+      if (!a.d_weights || !real_slot(a, s)) return;
 #pragma unroll
-      for (uint32_t j = 0; j < AT_ONCE; ++j) {
-        if (!real[j]) continue;
-        float v[E];
+      for (int u = 0; u < BLOCKS; ++u) v[to][u] = load_pack<E, ONCE>(rows + (int64_t)s * a.rows.row + col[u], n[u]);
+    };
+    ask(0, 0);
+    for (uint32_t k0 = 0; k0 < a.top; k0 += 2) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t k = k0 + half;
+        if (k >= a.top) break;
+        ask(k + 1, half ^ 1);
+        const int32_t s = slot[k];
+        const bool real = real_slot(a, s);
+        if (real && a.d_rows.p) {
+          const float f = weights[k];
+#pragma unroll
+          for (int u = 0; u < BLOCKS; ++u) {
+            Pack<T, E> d;
+#pragma unroll
+            for (int e = 0; e < E; ++e) d.v[e] = from_f<T>(f * to_f(g[u].v[e]));
+            store_pack<E, ONCE>(d_rows + (int64_t)s * a.d_rows.row + col[u], n[u], d);
+          }
+        }
         if (a.d_weights) {
-          load_upto<E>(rows + (int64_t)s[j] * a.rows.row + col, n, v);
+          float sum = 0.f;
+          if (real) {
 #pragma unroll
-          for (int e = 0; e < E; ++e) sum[j] = fmaf(g[e], v[e], sum[j]);
+            for (int u = 0; u < BLOCKS; ++u)
+#pragma unroll
+              for (int e = 0; e < E; ++e) sum = fmaf(to_f(g[u].v[e]), to_f(v[half][u].v[e]), sum);
+            sum = wave_sum_uniform(sum);
+          }
+          float* const out = a.d_weights + (uint64_t)line * a.top + k;
+          if (lane == 0) *out = first ? *out + sum : sum;
         }
-        if (a.d_rows.p) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) v[e] = f[j] * g[e];
-          store_upto<E>(d_rows + (int64_t)s[j] * a.d_rows.row + col, n, v);
-        }
-      }
-    }
-    if (a.d_weights) {
-#pragma unroll
-      for (uint32_t j = 0; j < AT_ONCE; ++j) {
-        const float all = wave_sum_uniform(sum[j]);
-        if (k + j < a.top && lane == 0) a.d_weights[line * a.top + k + j] = all;
       }
     }
   }
@@ -285,7 +318,7 @@ Sizes sizes_of(const evg_experts* c, uint32_t tokens) {
 ExpertsArgs experts_args(const evg_experts* c, uint32_t tokens, const evg_mat* x, const evg_mat* rows, const evg_mat* d_rows) {
   const evg_experts_config& g = c->cfg;
   ExpertsArgs a{};
-  a.workers = g.workers, a.tokens = tokens, a.experts = g.experts, a.top = g.top, a.width = g.width, a.capacity = g.capacity;
+  a.workers = g.workers, a.lines = g.workers * tokens, a.tokens = tokens, a.experts = g.experts, a.top = g.top, a.width = g.width, a.capacity = g.capacity;
   a.slots = (uint32_t)evg_experts_slots(c, tokens);
   const evg_mat none{};
   a.x = *x;
@@ -303,33 +336,54 @@ uint64_t empty_groups(const ExpertsArgs& a) {
   return ((uint64_t)a.workers * ((a.slots + kEmptySlots - 1) / kEmptySlots) + kWaves - 1) / kWaves;
 }
 
+// Do the slots' rows go past the caches, as they do not fit them?
+template <typename T>
+bool past_caches(const ExpertsArgs& a) { return (uint64_t)a.workers * a.slots * a.width * sizeof(T) > (128u << 20); }
+
 template <typename T>
 hipError_t dispatch(const evg_experts* c, ExpertsArgs& a) {
   const uint32_t n = a.tokens * a.top;
   hipError_t e;
   while ((1u << a.bits) < a.experts) ++a.bits;
   if (n <= kOneSort) {
-    if ((e = launch(a.workers, kOneWaves * 64, c->stream, a, k_experts_place<true, kOneWaves>)) != hipSuccess) return e;
+    if ((e = launch(a.workers, kOneWaves * 64, c->stream, a, n <= kOneWaves * 64 ? k_experts_place<true, kOneWaves, 1> : k_experts_place<true, kOneWaves, kOnePer>)) != hipSuccess) return e;
   } else {
-    const Runs runs = cut_runs(n);
+    const Runs runs = cut_runs(n, kThreads * kPer);
     a.run = runs.each, a.runs = runs.count;
     const uint64_t groups = (uint64_t)a.workers * a.runs;
     if ((e = launch(groups, kThreads, c->stream, a, k_experts_count)) != hipSuccess) return e;
-    if ((e = launch(groups, kThreads, c->stream, a, k_experts_place<false, kWaves>)) != hipSuccess) return e;
+    if ((e = launch(groups, kThreads, c->stream, a, k_experts_place<false, kWaves, kPer>)) != hipSuccess) return e;
   }
-  a.token_groups = ((uint64_t)a.workers * a.tokens * a.blocks + kWaves - 1) / kWaves;
-  return launch(a.token_groups + empty_groups(a), kThreads, c->stream, a, k_experts_dispatch<T>);
+  // Few units go to a wavefront each: the chip has room for 8192 of them.
+  const uint32_t units = a.lines * a.blocks, each = units <= 8192 ? 1 : 4;
+  a.token_groups = (units + each * kWaves - 1) / (each * kWaves);
+  const uint64_t groups = a.token_groups + empty_groups(a);
+  if (each == 1) return launch(groups, kThreads, c->stream, a, k_experts_dispatch<T, 1, false>);
+  return launch(groups, kThreads, c->stream, a, past_caches<T>(a) ? k_experts_dispatch<T, 4, true> : k_experts_dispatch<T, 4, false>);
+}
+
+template <typename T, bool ONCE>
+hipError_t combine_by(const evg_experts* c, ExpertsArgs& a) {
+  const uint64_t groups = ((uint64_t)a.lines * a.blocks + kWaves - 1) / kWaves;
+  return launch(groups, kThreads, c->stream, a,
+                a.top <= 2 ? k_experts_combine<T, 2, ONCE> : a.top <= 4 ? k_experts_combine<T, 4, ONCE> : k_experts_combine<T, 8, ONCE>);
 }
 
 template <typename T>
 hipError_t combine(const evg_experts* c, ExpertsArgs& a) {
-  return launch(((uint64_t)a.workers * a.tokens * a.blocks + kWaves - 1) / kWaves, kThreads, c->stream, a, k_experts_combine<T>);
+  return past_caches<T>(a) ? combine_by<T, true>(c, a) : combine_by<T, false>(c, a);
+}
+
+template <typename T, bool ONCE>
+hipError_t combine_backward_by(const evg_experts* c, ExpertsArgs& a) {
+  a.token_groups = (a.lines + kWaves - 1) / kWaves;
+  const uint64_t groups = a.token_groups + (a.d_rows.p ? empty_groups(a) : 0);
+  return launch(groups, kThreads, c->stream, a, a.blocks <= 1 ? k_experts_combine_backward<T, 1, ONCE> : a.blocks <= 2 ? k_experts_combine_backward<T, 2, ONCE> : k_experts_combine_backward<T, 4, ONCE>);
 }
 
 template <typename T>
 hipError_t combine_backward(const evg_experts* c, ExpertsArgs& a) {
-  a.token_groups = ((uint64_t)a.workers * a.tokens + kWaves - 1) / kWaves;
-  return launch(a.token_groups + (a.d_rows.p ? empty_groups(a) : 0), kThreads, c->stream, a, k_experts_combine_backward<T>);
+  return past_caches<T>(a) ? combine_backward_by<T, true>(c, a) : combine_backward_by<T, false>(c, a);
 }
 
 evg_status check_plan(const evg_experts* c, uint32_t tokens, const evg_experts_plan* plan, bool source, bool counts) {
@@ -356,8 +410,9 @@ evg_status evg_experts_init(evg_experts** out, const evg_experts_config* cfg, vo
   if ((uint64_t)cfg->max_tokens * cfg->top >> 28) return fail(EVG_ERR_INVALID, "max_tokens and top together must be below 2^28");
   if ((uint64_t)cfg->experts * cfg->capacity >> 31) return fail(EVG_ERR_INVALID, "experts and capacity together must be below 2^31");
   const uint64_t slots = cfg->capacity ? (uint64_t)cfg->experts * cfg->capacity : (uint64_t)cfg->max_tokens * cfg->top;
-  const uint64_t blocks = ((uint64_t)cfg->width * 4 + 1023) / 1024;
-  if (cfg->workers * ((uint64_t)cfg->max_tokens * blocks + slots / kEmptySlots + 1) / kWaves > 0x7FFF0000ull)
+  const uint64_t blocks = ((uint64_t)cfg->width * type_bytes(cfg->type) + 1023) / 1024;
+  // Kernels count units of 64 vectors, and slots, in 32 bits.
+  if (cfg->workers * (uint64_t)cfg->max_tokens * blocks > 0x7FFFFFFFull || cfg->workers * (slots + kEmptySlots) > 0x7FFFFFFFull)
     return fail(EVG_ERR_INVALID, "workers, max_tokens, width and capacity together are out of range");
   evg_status st;
   if ((st = check_type(cfg->type, "type")) != EVG_OK) return st;
@@ -366,7 +421,7 @@ evg_status evg_experts_init(evg_experts** out, const evg_experts_config* cfg, vo
   c->cfg = *cfg;
   c->stream = static_cast<hipStream_t>(hip_stream);
   if ((uint64_t)cfg->max_tokens * cfg->top > kOneSort) {
-    const hipError_t e = hipMalloc((void**)&c->run_counts, (uint64_t)cfg->workers * 128 * cfg->experts * 4);
+    const hipError_t e = hipMalloc((void**)&c->run_counts, (uint64_t)cfg->workers * kMostRuns * cfg->experts * 4);
     if (e != hipSuccess) {
       (void)hipGetLastError();
       delete c;

@@ -1,9 +1,9 @@
 // Stable counting sort of small whole numbers, as tokens and experts have.
 //
-// A workgroup takes a run of keys; each of its wavefronts a contiguous part of the run.  The wavefronts count their keys, a scan over the bins
-// gives each wavefront the place of its first key of each bin, and 64 keys at a time find their places from there: the lanes
-// with the same key are found by one ballot for each bit, the first of them moves the bin's place on.  No result depends on the
-// order in which wavefronts run.
+// A workgroup takes a run of keys, WAVES * 64 * PER at a time in registers; each of its wavefronts has a contiguous part, all of whose loads are under way at once.
+// The wavefronts rank and count their keys, 64 at a time: the lanes with the same key are found by one ballot for each bit, the first of them moves the bin's count
+// on.  A scan over the bins then gives each wavefront the place of its first key of each bin.
+// No result depends on the order in which wavefronts run.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -12,37 +12,33 @@ namespace evg {
 
 constexpr uint32_t kMostBins = 1024;
 
-// Keys of a wavefront's part of n: whole groups of 64.
-template <int WAVES>
-__device__ __forceinline__ uint32_t part_keys(uint32_t n) { return (n + WAVES * 64 - 1) / (WAVES * 64) * 64; }
-
-// Adds the keys of this wavefront's part to counts[bin]; keys of `bins` and above do not count.  key(i): that of the run's i-th.
-template <int WAVES, typename Key>
-__device__ __forceinline__ void count_keys(uint32_t* counts, uint32_t bins, uint32_t n, Key key) {
-  const uint32_t part = part_keys<WAVES>(n), begin = threadIdx.x / 64 * part, end = min(n, begin + part);
-  for (uint32_t i = begin + threadIdx.x % 64; i < end; i += 64) {
-    const uint32_t k = key(i);
-    if (k < bins) atomicAdd(&counts[k], 1u);
-  }
+// Calls f(j, i) for this thread's keys of a run of n: the i-th of the run is its j-th.
+template <int PER, typename F>
+__device__ __forceinline__ void each_key(uint32_t n, F f) {
+  const uint32_t begin = threadIdx.x / 64 * (64 * PER) + threadIdx.x % 64;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) f(j, begin + j * 64, begin + j * 64 < n);
 }
 
-// The places of this wavefront's keys: next[bin] is that of its first, and is moved on.  emit(i, key, place) for each key below `bins` < 2^bits.
-template <int WAVES, typename Key, typename Emit>
-__device__ __forceinline__ void place_keys(uint32_t* next, uint32_t bins, int bits, uint32_t n, Key key, Emit emit) {
-  const uint32_t part = part_keys<WAVES>(n), begin = threadIdx.x / 64 * part, end = min(n, begin + part);
+// Counts this wavefront's keys, key(j), in counts[bin]; what was there before each key is its rank.  Keys of `bins` <= 2^bits and above do not count.  (Counting by an
+// LDS operation of each lane costs one of a lane after the other where many keys are the same: 60 us for 16384 tokens of which half had the same upper byte.)
+template <int PER, typename Key>
+__device__ __forceinline__ void rank_keys(Key key, uint32_t* rank, uint32_t* counts, uint32_t bins, int bits) {
   const int lane = threadIdx.x % 64;
-  for (uint32_t base = begin; base < end; base += 64) {
-    const uint32_t i = base + lane, k = i < end ? key(i) : bins;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const uint32_t k = key(j);
     uint64_t same = __ballot(k < bins);
+    rank[j] = 0;
+    if (!same) continue;
     for (int b = 0; b < bits; ++b) {
       const uint64_t set = __ballot(k >> b & 1);
       same &= k >> b & 1 ? set : ~set;
     }
     uint32_t at = 0;
     const int leader = same ? __ffsll((unsigned long long)same) - 1 : lane;
-    if (k < bins && lane == leader) at = atomicAdd(&next[k], (uint32_t)__popcll(same));
-    at = __shfl(at, leader, 64) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-    if (k < bins) emit(i, k, at);
+    if (k < bins && lane == leader) at = atomicAdd(&counts[k], (uint32_t)__popcll(same));
+    rank[j] = __shfl(at, leader, 64) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
   }
 }
 
@@ -69,9 +65,9 @@ __device__ __forceinline__ uint32_t sum_ahead(uint32_t v, uint32_t* part, uint32
   return before + sum - v;
 }
 
-// counts[wave][bin] of a workgroup, on top of first[bin]: the place of each wavefront's first key of each bin.
+// counts[wave][bin] of a workgroup, on top of first[bin]: the place of each wavefront's first key of each bin; first[bin] goes on behind the last one's.
 template <int WAVES>
-__device__ __forceinline__ void places_of_waves(uint32_t* counts, const uint32_t* first, uint32_t bins) {
+__device__ __forceinline__ void places_of_waves(uint32_t* counts, uint32_t* first, uint32_t bins) {
   for (uint32_t b = threadIdx.x; b < bins; b += WAVES * 64) {
     uint32_t at = first[b];
 #pragma unroll
@@ -80,6 +76,7 @@ __device__ __forceinline__ void places_of_waves(uint32_t* counts, const uint32_t
       counts[w * bins + b] = at;
       at += c;
     }
+    first[b] = at;
   }
 }
 
@@ -105,12 +102,36 @@ __device__ __forceinline__ uint32_t scan_bins(uint32_t* values, uint32_t bins, u
   return total;
 }
 
-// How a worker's n keys are cut into runs of a workgroup each: few enough that every workgroup can add up what the runs ahead of its own counted.
+// What all runs counted, all[run][bin], added up: total[bin] over all of them, ahead[bin] over those ahead of run r.  Both in LDS.  Threads beyond the bins
+// take runs of their own.
+template <int WAVES>
+__device__ __forceinline__ void sum_runs(const uint32_t* all, uint32_t runs, uint32_t r, uint32_t bins, uint32_t* total, uint32_t* ahead) {
+  constexpr uint32_t THREADS = WAVES * 64;
+  for (uint32_t b = threadIdx.x; b < bins; b += THREADS) total[b] = ahead[b] = 0;
+  __syncthreads();
+  const uint32_t shares = bins >= THREADS ? 1 : THREADS / bins, share = bins >= THREADS ? 0 : threadIdx.x / bins;
+  if (share < shares) {
+    for (uint32_t b = bins >= THREADS ? threadIdx.x : threadIdx.x % bins; b < bins; b += THREADS) {
+      uint32_t sum = 0, before = 0;
+#pragma unroll 8
+      for (uint32_t q = share; q < runs; q += shares) {
+        const uint32_t c = all[(uint64_t)q * bins + b];
+        sum += c;
+        before += q < r ? c : 0;
+      }
+      if (sum) atomicAdd(&total[b], sum);
+      if (before) atomicAdd(&ahead[b], before);
+    }
+  }
+  __syncthreads();
+}
+
+// How a worker's n keys are cut into runs of a workgroup each, whole rounds of `round` keys: few enough that every workgroup can add up what the runs counted.
 struct Runs { uint32_t each, count; };
-inline Runs cut_runs(uint32_t n) {
-  const uint64_t least = 2048, by = ((uint64_t)n + 127) / 128;
-  const uint32_t each = (uint32_t)(by <= least ? least : (by + 1023) / 1024 * 1024);
-  return {each, n ? (n + each - 1) / each : 0};
+constexpr uint32_t kMostRuns = 128;
+inline Runs cut_runs(uint32_t n, uint32_t round) {
+  const uint32_t rounds = (uint32_t)(((uint64_t)n + round - 1) / round), each = (rounds + kMostRuns - 1) / kMostRuns * round;
+  return {each, n ? (uint32_t)(((uint64_t)n + each - 1) / each) : 0};
 }
 
 }  // namespace evg

@@ -71,6 +71,33 @@ __device__ __forceinline__ void store_upto(T* p, int n, const float* v) {
   }
 }
 
+// The first n of N elements as they are; the others are 0.  ONCE: past the caches.
+template <int N, bool ONCE = false, typename T>
+__device__ __forceinline__ Pack<T, N> load_pack(const T* p, int n) {
+  typedef uint32_t words __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T))));
+  if (n >= N) {
+    if constexpr (ONCE) return __builtin_bit_cast(Pack<T, N>, __builtin_nontemporal_load(reinterpret_cast<const words*>(p)));
+    return *reinterpret_cast<const Pack<T, N>*>(p);
+  }
+  Pack<T, N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.v[i] = i < n ? p[i] : (T)0.f;
+  return r;
+}
+
+template <int N, bool ONCE = false, typename T>
+__device__ __forceinline__ void store_pack(T* p, int n, const Pack<T, N>& r) {
+  typedef uint32_t words __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T))));
+  if (n >= N) {
+    if constexpr (ONCE) __builtin_nontemporal_store(__builtin_bit_cast(words, r), reinterpret_cast<words*>(p));
+    else *reinterpret_cast<Pack<T, N>*>(p) = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = r.v[i];
+  }
+}
+
 // The sum over a wavefront, in every lane; the order is fixed.
 template <typename F>
 __device__ __forceinline__ F wave_sum(F v) {

@@ -3,8 +3,9 @@
 // A token's logits lie in the registers of 1 to 64 lanes, eight to a lane (sixteen above 512 experts).  K times the lanes find the largest
 // among those not chosen yet: a lane its own, then the group by exchanges, of one word that has the logit's rank above and
 // the expert's number, turned round, below.  So equal logits go to the lowest number, and the order of the lanes is of no matter.
+// A logit of 16 bits and its number fit a word of 32 bits, one of 32 needs 64.
 //
-// Bound by memory where tokens are many (E values in, K pairs out); a choice is about sixty instructions.
+// Bound by memory where tokens are many (E values in, K pairs out) and by the choices' instructions: 128 experts, top 8 of 32768 tokens.
 #include <hip/hip_runtime.h>
 
 #include <new>
@@ -25,13 +26,52 @@ struct RouterArgs {
   uint32_t tokens, experts, top, over_chosen, first;
 };
 
-// Ranks of floats as whole numbers: minus infinity lowest but 0, a NaN of any kind highest; both zeros are one.
-__device__ __forceinline__ uint32_t rank_of(float v) {
-  if (v != v) return 0xFFFFFFFFu;
-  const uint32_t b = __float_as_uint(v + 0.f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+// A logit and its expert as a whole number, ordered as they are chosen: a NaN highest, then by value, both zeros one, then the lowest number.  0 for minus
+// infinity, which is never chosen.
+template <typename T> struct Word {
+  typedef uint32_t type;
+  static __device__ __forceinline__ type of(float v, int e) {   // exact in T
+    const uint32_t b = __builtin_bit_cast(uint16_t, from_f<T>(v + 0.f));
+    const uint32_t r = v != v ? 0xFFFFu : b & 0x8000u ? ~b & 0xFFFFu : b | 0x8000u;
+    return v == -INFINITY ? 0 : r << 16 | (0xFFFFu - e);
+  }
+  static __device__ __forceinline__ int expert(type w) { return (int)(0xFFFFu - (w & 0xFFFFu)); }
+  static __device__ __forceinline__ float value(type w) {
+    const uint32_t r = w >> 16;
+    return r == 0xFFFFu ? NAN : to_f(__builtin_bit_cast(T, (uint16_t)(r & 0x8000u ? r & 0x7FFFu : ~r)));
+  }
+};
+template <> struct Word<float> {
+  typedef uint64_t type;
+  static __device__ __forceinline__ type of(float v, int e) {
+    const uint32_t b = __float_as_uint(v + 0.f);
+    const uint32_t r = v != v ? 0xFFFFFFFFu : b & 0x80000000u ? ~b : b | 0x80000000u;
+    return v == -INFINITY ? 0 : (uint64_t)r << 32 | (0xFFFFFFFFu - (uint32_t)e);
+  }
+  static __device__ __forceinline__ int expert(type w) { return (int)(0xFFFFFFFFu - (uint32_t)w); }
+  static __device__ __forceinline__ float value(type w) {
+    const uint32_t r = (uint32_t)(w >> 32);
+    return r == 0xFFFFFFFFu ? NAN : __uint_as_float(r & 0x80000000u ? r & 0x7FFFFFFFu : ~r);
+  }
+};
+
+// The same of another lane, by data-parallel moves within 16 lanes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved_word(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false); }
+template <int CTRL>
+__device__ __forceinline__ uint64_t moved_word(uint64_t v) { return (uint64_t)moved_word<CTRL>((uint32_t)(v >> 32)) << 32 | moved_word<CTRL>((uint32_t)v); }
+
+// The largest of a group's words, in all of its lanes.
+template <int LANES, typename W>
+__device__ __forceinline__ W lanes_largest(W v) {
+  if constexpr (LANES >= 2) v = max(v, moved_word<0xB1>(v));    // lanes 1 0 3 2
+  if constexpr (LANES >= 4) v = max(v, moved_word<0x4E>(v));    // lanes 2 3 0 1
+  if constexpr (LANES >= 8) v = max(v, moved_word<0x141>(v));   // mirrored within 8
+  if constexpr (LANES >= 16) v = max(v, moved_word<0x140>(v));  // mirrored within 16
+  if constexpr (LANES >= 32) v = max(v, (W)__shfl_xor(v, 16, 64));
+  if constexpr (LANES >= 64) v = max(v, (W)__shfl_xor(v, 32, 64));
+  return v;
 }
-constexpr uint32_t kRankOfNone = 0x007FFFFFu;   // minus infinity's
 
 template <int LANES>
 __device__ __forceinline__ float lanes_total(float v) {
@@ -63,60 +103,51 @@ __device__ __forceinline__ void load_logits(const T* p, int n, float* v) {
 
 template <typename T, int LANES, int PER>
 __global__ __launch_bounds__(kThreads) void k_router(RouterArgs a) {
-  const uint64_t line = ((uint64_t)a.first + blockIdx.x) * (kThreads / LANES) + threadIdx.x / LANES;
-  if (line >= a.lines) return;   // all of a group's lanes at once
-  const uint32_t w = (uint32_t)(line / a.tokens), t = (uint32_t)(line % a.tokens);
+  const uint32_t row = (a.first + blockIdx.x) * (kThreads / LANES) + threadIdx.x / LANES;
+  if (row >= a.lines) return;   // all of a group's lanes at once
+  const uint32_t w = row / a.tokens, t = row % a.tokens;
+  const uint64_t line = row;
   const int lane = threadIdx.x % LANES, first = lane * PER;
   float v[PER];
   load_logits<PER>((const T*)a.logits.p + (int64_t)w * a.logits.worker + (int64_t)t * a.logits.row + first, (int)a.experts - first, v);
-  uint32_t rank[PER];
-  int place[PER];
+  typedef typename Word<T>::type W;
+  W word[PER];
+  uint32_t place[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    rank[i] = rank_of(v[i]);
-    if (rank[i] == kRankOfNone) rank[i] = 0;   // never chosen
-    place[i] = -1;
+    word[i] = Word<T>::of(v[i], first + i);
+    place[i] = a.top;
   }
-  float most = 0.f, total = 0.f;
+  float most = 0.f;
   uint32_t k = 0;
   for (; k < a.top; ++k) {
-    uint64_t best = 0;
+    W best = word[0];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const uint64_t it = (uint64_t)rank[i] << 32 | (uint32_t)~(first + i);
-      best = rank[i] && it > best ? it : best;
-    }
-#pragma unroll
-    for (int d = 1; d < LANES; d <<= 1) {
-      const uint64_t other = __shfl_xor((unsigned long long)best, d, LANES);
-      best = other > best ? other : best;
-    }
+    for (int i = 1; i < PER; ++i) best = max(best, word[i]);
+    best = lanes_largest<LANES>(best);
     if (!best) break;   // none is left
-    const int e = (int)~(uint32_t)best;
-    const uint32_t r = (uint32_t)(best >> 32);
-    const float value = r == 0xFFFFFFFFu ? NAN : __uint_as_float(r & 0x80000000u ? r & 0x7FFFFFFFu : ~r);
-    if (k == 0) most = value;
-    total += expf(value - most);
+    if (k == 0) most = Word<T>::value(best);
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      if (first + i == e) {
-        place[i] = (int)k;
-        rank[i] = 0;
+      if (word[i] == best) {   // words differ
+        place[i] = k;
+        word[i] = 0;
       }
   }
-  if (!a.over_chosen) {
-    total = 0.f;
+  float total = 0.f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) total += expf(v[i] - most);
-    total = lanes_total<LANES>(total);
+  for (int i = 0; i < PER; ++i) {
+    v[i] = expf(v[i] - most);
+    total += place[i] < a.top || !a.over_chosen ? v[i] : 0.f;
   }
+  total = lanes_total<LANES>(total);
   int32_t* const chosen = a.chosen + line * a.top;
   float* const weights = a.weights + line * a.top;
 #pragma unroll
   for (int i = 0; i < PER; ++i)
-    if (place[i] >= 0) {
+    if (place[i] < a.top) {
       chosen[place[i]] = first + i;
-      weights[place[i]] = expf(v[i] - most) / total;
+      weights[place[i]] = v[i] / total;
     }
   for (uint32_t j = k + lane; j < a.top; j += LANES) {
     chosen[j] = -1;
@@ -126,9 +157,10 @@ __global__ __launch_bounds__(kThreads) void k_router(RouterArgs a) {
 
 template <typename T, int LANES, int PER>
 __global__ __launch_bounds__(kThreads) void k_router_backward(RouterArgs a) {
-  const uint64_t line = ((uint64_t)a.first + blockIdx.x) * (kThreads / LANES) + threadIdx.x / LANES;
-  if (line >= a.lines) return;
-  const uint32_t w = (uint32_t)(line / a.tokens), t = (uint32_t)(line % a.tokens);
+  const uint32_t row = (a.first + blockIdx.x) * (kThreads / LANES) + threadIdx.x / LANES;
+  if (row >= a.lines) return;
+  const uint32_t w = row / a.tokens, t = row % a.tokens;
+  const uint64_t line = row;
   const int lane = threadIdx.x % LANES, first = lane * PER;
   const T* const logits = (const T*)a.logits.p + (int64_t)w * a.logits.worker + (int64_t)t * a.logits.row;
   const int32_t* const chosen = a.chosen + line * a.top;
