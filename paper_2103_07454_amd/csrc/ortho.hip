@@ -19,13 +19,14 @@
 
 #include "nn_device.h"
 #include "nn_host.h"
+#include "ortho_choose.h"
 #include "ortho_internal.h"
 
 namespace evg {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr uint32_t kBlocks = 512;   // of a matrix, at most: each of the second pass adds up what those of the first left
+constexpr uint32_t kBlocks = 2048;  // of a matrix, at most: each of the second pass adds up what those of the first left
 constexpr int kVector = 8;          // elements of a lane
 
 struct UpdateArgs {
@@ -105,9 +106,9 @@ __global__ __launch_bounds__(kThreads) void k_ortho_start(UpdateArgs a) {
     for (int i = 0; i < kVector; ++i) {
       halves_of(i < n ? u[i] * f : 0.f, &hi.v[i], &lo.v[i]);
     }
-    const int64_t at = (int64_t)w * a.x.worker + (int64_t)row * a.x.ld + col;
-    *reinterpret_cast<Pack<half_t, kVector>*>(a.x.hi + at) = hi;
-    *reinterpret_cast<Pack<half_t, kVector>*>(a.x.lo + at) = lo;
+    uint16_t* const p = a.x.p + (int64_t)w * a.x.worker + (int64_t)row * a.x.ld + halves_col(a.x.paired, col);
+    *reinterpret_cast<Pack<half_t, kVector>*>(p) = hi;
+    *reinterpret_cast<Pack<half_t, kVector>*>(p + a.x.apart) = lo;
   }
 }
 
@@ -128,7 +129,7 @@ hipError_t launch_start(UpdateArgs a, uint32_t matrices, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_ortho(OrthoOp op, bool tall, bool split, bool last, OrthoArgs a, hipStream_t s) {
+hipError_t launch_ortho(OrthoOp op, bool tall, bool split, bool last, const OrthoArgs& a, hipStream_t s) {
   return split ? launch_ortho_parts<true>(op, tall, last, a, s) : launch_ortho_parts<false>(op, tall, last, a, s);
 }
 
@@ -141,7 +142,9 @@ struct evg_ortho {
   hipStream_t stream = nullptr;
   void* owned = nullptr;
   double* partials = nullptr;
-  Halves x[2]{}, s{}, p{};
+  uint16_t *x[2]{}, *s = nullptr, *p = nullptr;   // each with room for both parts
+  float* sums = nullptr;   // partial sums of products
+  uint64_t room = 0;       // how many
   uint32_t blocks = 1;
   uint32_t split_from = 0;   // the first step whose products are of both parts
   float scale_x = 1.f, scale_s = 1.f, scale_p = 1.f;
@@ -183,6 +186,19 @@ float scale_for(double most) {
   return std::ldexp(1.f, 15 - e);
 }
 
+// Rows of a matrix's parts are whole 128 bytes apart.
+uint64_t pitch_of(uint32_t cols) { return ((uint64_t)cols + 63) / 64 * 64; }
+
+// A matrix for products of both parts, or of hi alone; with or without a lo.
+Halves halves(uint16_t* p, uint32_t matrices, uint32_t rows, uint32_t cols, bool split, bool lo) {
+  const int64_t pitch = (int64_t)pitch_of(cols), plane = (int64_t)rows * pitch;
+  if (split) return {p, 32, 2 * plane, 2 * pitch, 1};
+  return {p, lo ? (int64_t)matrices * plane : 0, plane, pitch, 0};
+}
+
+// Floats that partial sums may take at most; no product that is better in parts has been seen to need half of it.
+constexpr uint64_t kMostSums = 1ull << 26;
+
 }  // namespace
 
 extern "C" {
@@ -213,31 +229,33 @@ evg_status evg_ortho_init(evg_ortho** out, const evg_ortho_config* cfg, void* hi
   c->scale_s = scale_for(bound * bound);
   c->scale_p = scale_for(1.01 * most_quadratic(cfg->b, cfg->c, bound * bound));
   c->split_from = cfg->type == EVG_F32 ? 0 : cfg->type == EVG_BF16 ? cfg->steps : cfg->steps > 2 ? cfg->steps - 2 : 0;
-  const bool split = c->split_from < cfg->steps;
   const uint64_t across = ((uint64_t)cfg->cols + 64 * kVector - 1) / (64 * kVector), jobs = (cfg->rows * across + kWaves - 1) / kWaves;
   c->blocks = (uint32_t)(jobs < kBlocks ? jobs : kBlocks);
-  const uint64_t W = cfg->matrices, ldx = ((uint64_t)cfg->cols + 63) / 64 * 64, lds = ((uint64_t)n + 63) / 64 * 64;
-  const uint64_t x = W * cfg->rows * ldx, s = W * n * lds;
-  struct { uint16_t** to; uint64_t count; } parts[] = {{&c->x[0].hi, x}, {&c->x[0].lo, x}, {&c->x[1].hi, x}, {&c->x[1].lo, x}, {&c->s.hi, s}, {&c->p.hi, s},
-                                                       {&c->s.lo, split ? s : 0}, {&c->p.lo, split ? s : 0}};
-  uint64_t total = W * c->blocks * sizeof(double);
-  total = (total + 255) / 256 * 256;
-  const uint64_t sums = total;
-  for (auto& q : parts) total += (q.count * 2 + 255) / 256 * 256;
+  const uint64_t W = cfg->matrices, x = W * cfg->rows * pitch_of(cfg->cols) * 2 * sizeof(uint16_t), s = W * n * pitch_of(n) * 2 * sizeof(uint16_t);
+  const uint32_t k = cfg->rows < cfg->cols ? cfg->cols : cfg->rows;
+  for (int split = 0; split < 2; ++split) {
+    const OrthoShape gram{n, n, k, cfg->matrices, kMostSums}, square{n, n, n, cfg->matrices, kMostSums}, apply{cfg->rows, cfg->cols, n, cfg->matrices, kMostSums};
+    if (split ? c->split_from >= cfg->steps : c->split_from == 0) continue;   // no such step
+    for (const uint64_t need : {ortho_partial(gram, true, choose_ortho(gram, true, split)), ortho_partial(square, true, choose_ortho(square, true, split)),
+                                ortho_partial(apply, false, choose_ortho(apply, false, split))})
+      if (need > c->room) c->room = need;
+  }
+  auto whole = [](uint64_t bytes) { return (bytes + 255) / 256 * 256; };
+  struct { void** to; uint64_t bytes; } parts[] = {{(void**)&c->partials, W * c->blocks * sizeof(double)}, {(void**)&c->x[0], x}, {(void**)&c->x[1], x},
+                                                   {(void**)&c->s, s}, {(void**)&c->p, s}, {(void**)&c->sums, c->room * sizeof(float)}};
+  uint64_t total = 0;
+  for (auto& q : parts) total += whole(q.bytes);
   const hipError_t e = total >> 46 ? hipErrorOutOfMemory : hipMalloc(&c->owned, total);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     delete c;
     return fail(e == hipErrorOutOfMemory ? EVG_ERR_OOM : EVG_ERR_HIP, "workspace: %s", hipGetErrorString(e));
   }
-  c->partials = (double*)c->owned;
-  char* at = (char*)c->owned + sums;
+  char* at = (char*)c->owned;
   for (auto& q : parts) {
-    *q.to = (uint16_t*)at;
-    at += (q.count * 2 + 255) / 256 * 256;
+    *q.to = at;
+    at += whole(q.bytes);
   }
-  for (Halves* h : {&c->x[0], &c->x[1]}) h->worker = (int64_t)(cfg->rows * ldx), h->ld = (int64_t)ldx;
-  for (Halves* h : {&c->s, &c->p}) h->worker = (int64_t)(n * lds), h->ld = (int64_t)lds;
   *out = c;
   return EVG_OK;
 }
@@ -270,35 +288,38 @@ evg_status evg_ortho_update(evg_ortho* c, const evg_mat* grad, const evg_mat* mo
   u.rows = R, u.cols = C, u.nesterov = g.nesterov, u.blocks = c->blocks;
   u.mu = g.momentum, u.eps = g.eps, u.scale_x = c->scale_x;
   u.partials = c->partials;
-  u.x = c->x[0];
+  const bool tall = R > C;
+  const uint32_t n = tall ? C : R, k = tall ? R : C;
+  auto split_at = [&](uint32_t step) { return step >= c->split_from; };
+  auto x_at = [&](uint32_t step) { return halves(c->x[step & 1], W, R, C, split_at(step), true); };   // as the step's products take it
+  u.x = x_at(0);
   HIP_TRY(g.type == EVG_F32   ? launch_start<float>(u, W, c->stream)
           : g.type == EVG_F16 ? launch_start<half_t>(u, W, c->stream)
                               : launch_start<bf16_t>(u, W, c->stream));
 
-  const bool tall = R > C;
-  const uint32_t n = tall ? C : R, k = tall ? R : C;
   const float sx = c->scale_x, ss = c->scale_s, sp = c->scale_p;
   for (uint32_t i = 0; i < g.steps; ++i) {
-    const Halves &x = c->x[i & 1], &next_x = c->x[~i & 1];
-    const bool last = i + 1 == g.steps, split = i >= c->split_from;
+    const bool last = i + 1 == g.steps, split = split_at(i);
+    const Halves x = x_at(i), S = halves(c->s, W, n, n, split, false), P = halves(c->p, W, n, n, split, false);
     OrthoArgs a{};
     a.matrices = W;
+    a.partial = c->sums, a.room = c->room;
     a.a = a.b = x;
-    a.to = c->s;
+    a.to = S;
     a.M = a.N = n, a.K = k;
     a.f_acc = ss / (sx * sx);
     HIP_TRY(launch_ortho(ORTHO_GRAM, tall, split, false, a, c->stream));
 
-    a.a = a.b = a.own = c->s;
-    a.to = c->p;
+    a.a = a.b = a.own = S;
+    a.to = P;
     a.K = n;
     a.f_acc = g.c * sp / (ss * ss), a.f_own = g.b * sp / ss;
     HIP_TRY(launch_ortho(ORTHO_SQUARE, tall, split, false, a, c->stream));
 
-    a.a = tall ? x : c->p;
-    a.b = tall ? c->p : x;
+    a.a = tall ? x : P;
+    a.b = tall ? P : x;
     a.own = x;
-    a.to = next_x;
+    a.to = x_at(i + 1);
     a.M = R, a.N = C;
     a.f_acc = 1.f / sp, a.f_own = g.a;
     if (last) {
