@@ -42,10 +42,45 @@ __device__ __forceinline__ void tile_of(const OrthoArgs& g, uint32_t id, uint32_
   }
 }
 
+// An operand's tile in LDS, in units of 16 bytes, permuted for LDS as this chip reads it: 64 banks, 256 bytes at a time.  K-contiguous: row m has 8 units, unit c at
+// m * 8 + (c ^ (m >> 1 & 7)), so that the 16 lanes that read one unit each of 16 neighbouring rows meet all banks (by
+// m & 7 half of LDS's cycles were conflicts, now none are; the products' time, which is not LDS's, stayed as it was).  M/N-contiguous: row k has BD / 8 units; 32 lanes of a transposing read take 4 units of each of 4 neighbouring rows.
+template <int BD, bool KC>
+struct HalvesTile {
+  static constexpr int kUnits = BD * 8, kPerRow = KC ? 8 : BD / 8;
+  static __device__ __forceinline__ int swizzle(int row) {
+    if constexpr (KC) return row >> 1 & 7;
+    else if constexpr (BD >= 128) return (row & 3) << 2;
+    else return (row >> 1 & 1) << 2;
+  }
+};
+
+// Fragment `ks` (0 .. 3: 32 bytes of k) of the 32 rows from d0 on, of a tile `from` units into a buffer.
+template <int BD, bool KC>
+__device__ __forceinline__ Frag<half_t> read_halves(const u32x4* s, int from, int d0, int ks, int lane) {
+  using L = HalvesTile<BD, KC>;
+  Frag<half_t> f;
+  if constexpr (KC) {
+    const int row = d0 + (lane & 31);
+    f.v = s[from + row * 8 + ((ks * 2 + (lane >> 5)) ^ L::swizzle(row))];
+  } else {
+    const int q = lane >> 4, i = lane & 15;
+    const int k = ks * 16 + (q >> 1) * 8 + (i >> 2);
+    const int unit = (d0 >> 3) + (q & 1) * 2 + ((i & 3) >> 1);
+    const int byte = (from + k * L::kPerRow + (unit ^ L::swizzle(k))) * 16 + (i & 1) * 8;
+    using P = __attribute__((address_space(3))) s16x4*;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)((const char*)s + byte));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)((const char*)s + (byte + 4 * L::kPerRow * 16)));   // 4 rows on, which are permuted alike
+    struct { s16x4 a, b; } both{lo, hi};
+    f.v = __builtin_bit_cast(u32x4, both);
+  }
+  return f;
+}
+
 // One operand's way into LDS.
 template <int BD, bool KC, int WAVES, bool SPLIT>
 struct HalvesLoader {
-  using L = Tile<half_t, BD, KC>;
+  using L = HalvesTile<BD, KC>;
   static constexpr int N = L::kUnits / 64 / WAVES;            // loads of a wavefront in a step
   static constexpr int kApart = KC ? 8 : 64 / L::kPerRow;     // rows between them
   static constexpr int BK = SPLIT ? 32 : 64;
@@ -67,7 +102,7 @@ struct HalvesLoader {
       const int row = place / L::kPerRow + j * kApart, unit = (place % L::kPerRow) ^ L::swizzle(row);
       if constexpr (KC) {
         off[j] = (uint32_t)(row * ld) + unit * 16;   // rows beyond the last one lie beyond `left`
-        if (j == 0) k = SPLIT ? (unit & 3) * 8 : unit * 8;   // the others' too: rows 8 apart are permuted alike
+        if (j == 0) k = SPLIT ? (unit & 3) * 8 : unit * 8;
       } else {
         const uint32_t d = unit * 8, kr = SPLIT ? row & 31 : row;
         off[j] = lead + d < dim ? (uint32_t)(kr * ld) + (SPLIT ? ((d & ~31u) * 2 + (d & 31) + (row & 32)) : d) * 2 : kOut;
@@ -78,7 +113,7 @@ struct HalvesLoader {
 
   // Does unit j lie behind the last k?
   __device__ __forceinline__ bool behind(int j, int k_left) const {
-    if constexpr (KC) return (int)k >= k_left;
+    if constexpr (KC) return (int)(SPLIT ? k : k ^ (j & 1) * 32) >= k_left;   // in rows 8 apart unit c is where c ^ 4 is
     else return (int)(SPLIT ? (k + j * kApart) & 31 : k + j * kApart) >= k_left;
   }
 
@@ -245,9 +280,9 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, 2) void k_ortho_gemm(OrthoA
   auto multiply = [&](const u32x4* lds) {
     auto read = [&](int ks, int to) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) b[to][j] = read_frag<T, BM, BKC>(lds, A_UNITS, wn + j * 32, ks, lane);
+      for (int j = 0; j < TN; ++j) b[to][j] = read_halves<BM, BKC>(lds, A_UNITS, wn + j * 32, ks, lane);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) a[to][i] = read_frag<T, BM, AKC>(lds, 0, wm + i * 32, ks, lane);
+      for (int i = 0; i < TM; ++i) a[to][i] = read_halves<BM, AKC>(lds, 0, wm + i * 32, ks, lane);
     };
     auto product = [&](int of_a, int of_b) {
 #pragma unroll
