@@ -415,7 +415,7 @@ hipError_t launch_ortho_tile(OrthoArgs a, uint32_t parts, hipStream_t s) {
     a.first = first;
     k_ortho_gemm<OP, TALL, SPLIT, LAST, BM, WAVES_M, WAVES_N><<<grid, WAVES_M * WAVES_N * 64, 0, s>>>(a);
   });
-  if (a.parts > 1) {
+  if constexpr (BM < 256 || OP != ORTHO_APPLY) if (a.parts > 1) {
     const uint64_t joins = (cells * a.matrices * (BM / 32) * WAVES_N + 3) / 4;
     launch_pieces(joins, 256, [&](uint32_t first, uint32_t grid) {
       a.first = first;
@@ -430,7 +430,8 @@ hipError_t launch_ortho_op(const OrthoArgs& a, hipStream_t s) {
   const OrthoChoice c = choose_ortho({a.M, a.N, a.K, a.matrices, a.room}, OP != ORTHO_APPLY, SPLIT);
   if (c.tile == 64) return launch_ortho_tile<OP, TALL, SPLIT, LAST, 64, 2, 2>(a, c.parts, s);
   if (c.tile == 128) return launch_ortho_tile<OP, TALL, SPLIT, LAST, 128, 2, 2>(a, c.parts, s);
-  return launch_ortho_tile<OP, TALL, SPLIT, LAST, 256, 2, 4>(a, c.parts, s);
+  if constexpr (SPLIT) return hipErrorInvalidValue;
+  else return launch_ortho_tile<OP, TALL, SPLIT, LAST, 256, 2, 4>(a, c.parts, s);
 }
 
 template <bool SPLIT>

@@ -6,6 +6,7 @@ import torch
 
 import nn_experts_reference as ref
 import nn_reference
+from ortho_sizes import SIZES as EVERY_TILE
 
 pytestmark = pytest.mark.gpu
 
@@ -67,6 +68,47 @@ def test_larger_tiles(nn, types, size):
         want, bound = ref.orthogonal(grad[w].double(), dtype, steps=2, polynomial=GENTLE[0])
         bound += float(nn_reference.rounding(want.abs() + 1e-3, out_dtype).norm())
         assert float((out[w].double().cpu() - want).norm()) <= bound
+
+
+def one_step(u, dtype, polynomial):
+    """A step's result and a bound of each element.  With X of norm 1, r its rows' norms and c its columns' (wide; tall the other way round), p those of P's rows,
+    o an operand's rounding, and sums of absolute products at most the products of norms:
+        |dS_ij| <= E r_i r_j,  E = 3 o + k 2^-24                                       (two operands, the result, the sum)
+        |dP_ij| <= Q r_i r_j + o |P_ij|,  Q = |b| E + |c| (2 E + 2 o + n 2^-24)
+        |dX'_ij| <= |a| (2^-22 + 2^-24) |X_ij| + c_j (Q r_i + (2 o + n 2^-24) p_i)
+    and what the start is off, d = 4 * 2^-24 + 2^-22 of each element, comes to d (|a X_ij| + (3 |b| + 5 |c|) r_i c_j) at most.
+    """
+    a, b, c = polynomial
+    o, d = 2 * ref.KEPT if dtype == torch.float32 else ref.HALF, 4 * ref.U32 + ref.KEPT
+    x = u / (u.norm() + 1e-7)
+    if x.shape[0] > x.shape[1]:
+        out, bound = one_step(u.T, dtype, polynomial)
+        return out.T, bound.T
+    n, k = x.shape
+    S = x @ x.T
+    P = b * S + c * S @ S
+    E = 3 * o + k * ref.U32
+    Q = abs(b) * E + abs(c) * (2 * E + 2 * o + n * ref.U32)
+    r, cols, p = x.norm(dim=1)[:, None], x.norm(dim=0)[None], P.norm(dim=1)[:, None]
+    bound = abs(a) * (ref.KEPT + ref.U32) * x.abs() + cols * (Q * r + (2 * o + n * ref.U32) * p) + d * (abs(a) * x.abs() + (3 * abs(b) + 5 * abs(c)) * r * cols)
+    return a * x + P @ x, 1.05 * bound
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", EVERY_TILE, ids=lambda s: "x".join(map(str, s)))
+def test_every_tile(nn, dtype, size):
+    """Products of hi alone (bfloat16) and of both parts (float32), of every tile, whole and in parts of k."""
+    W, R, C = size
+    gen = torch.Generator(device="cuda").manual_seed(R)
+    k = max(1, min(R, C) // 8)
+    grad = (torch.bmm(torch.randn(W, R, k, generator=gen, device="cuda"), torch.randn(W, k, C, generator=gen, device="cuda")) / k ** 0.5
+            + 0.3 * torch.randn(W, R, C, generator=gen, device="cuda")).to(dtype)
+    out = nn.Orthogonal(R, C, matrices=W, dtype=dtype, out_dtype=torch.float32, steps=1).update(grad)
+    for w in range(W):
+        want, bound = one_step(grad[w].double(), dtype, ref.POLYNOMIAL)
+        off = (out[w].double() - want).abs()
+        print(f"[ortho] {size} {dtype}: off by {float((off / bound).max()):.3f} of the bound, which is {float((bound / want.abs()).median()):.1e} of an element", flush=True)
+        assert bool((off <= bound + nn_reference.rounding(want, torch.float32)).all())
 
 
 @pytest.mark.parametrize("types", TYPES, ids=IDS)
