@@ -208,7 +208,7 @@ typedef struct {
 evg_status evg_router_init(evg_router** out, const evg_router_config* cfg, void* hip_stream);
 /* logits: tokens x E for each worker.  chosen, weights: DEVICE, [workers][tokens][K]. */
 evg_status evg_router_forward(evg_router* c, uint32_t tokens, const evg_mat* logits, int32_t* chosen, float* weights);
-/* chosen: what forward wrote.  What d_weights has where chosen is -1 does not count. */
+/* chosen: what forward wrote.  What d_weights has where chosen is -1 does not count.  d_logits may be logits itself. */
 evg_status evg_router_backward(evg_router* c, uint32_t tokens, const float* d_weights, const evg_mat* logits, const int32_t* chosen,
                                const evg_mat* d_logits);
 evg_status evg_router_destroy(evg_router* c);
