@@ -160,7 +160,7 @@ evg_status evg_ffn_destroy(evg_ffn* c);
  * For each worker, a table of V x D (V = vocab, D = width) and T tokens:
  *     y[t] = scale * table[id[t]],    d_table[v] = scale * sum of dy[t] over the tokens t with id[t] = v
  * A token whose number is not in 0 .. V-1 (padding) has a row of zeros and no part in the gradient.  Sums are in 32 bits, over a number's tokens
- * in their order. */
+ * in their order.  W V, and W T times the KB of a row, are below 2^31. */
 typedef struct evg_embed evg_embed;
 
 typedef struct {

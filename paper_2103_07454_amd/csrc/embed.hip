@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr uint32_t kChunk = 16;          // sorted tokens that a wavefront adds up (16384 tokens 2048 wide: 8 / 16 / 32 take 63 / 54 / 67 us with the joining)
+constexpr uint32_t kFewTokens = 512;     // most tokens of a worker that are sorted by comparing each with all (eight times 333: 7.0 us instead of 8.8)
 constexpr int kOneWaves = 16;            // of the workgroup that sorts alone
 constexpr int kPer = 4;                  // keys of a thread in a round
 // Most tokens of a worker that one workgroup sorts.  Ranking keeps a CU's vector units busy: 16384 tokens took one workgroup 57 us, sixteen 24.
@@ -88,6 +89,34 @@ __global__ __launch_bounds__(kThreads) void k_embed_rows(EmbedArgs a) {
 __device__ __forceinline__ uint32_t seen_words(uint32_t vocab) { return (vocab + 3) / 4; }
 __device__ __forceinline__ uint8_t* seen_of(const EmbedArgs& a, uint32_t w) { return a.seen + (uint64_t)w * seen_words(a.vocab) * 4; }
 
+// Few tokens: each thread compares its token with all others.  A number and its place are one word, so that a comparison tells both.
+__global__ __launch_bounds__(kFewTokens) void k_embed_sort_few(EmbedArgs a, int place_bits) {
+  __shared__ __attribute__((aligned(16))) uint32_t words[kFewTokens];
+  __shared__ uint32_t part[kFewTokens / 64];
+  const uint32_t w = a.first + blockIdx.x, i = threadIdx.x;
+  uint8_t* const seen = seen_of(a, w);
+  const uint32_t key = i < a.tokens ? token_id(a, w, i) : kNoToken, word = key == kNoToken ? kNoToken : key << place_bits | i;
+  words[i] = word;   // of 31 bits where there is a token
+  for (uint32_t v = i; v < seen_words(a.vocab); v += kFewTokens) ((uint32_t*)seen)[v] = 0;
+  __syncthreads();   // marks come behind
+  uint32_t rank = 0;
+  for (uint32_t j = 0; j < a.tokens; j += 32) {
+    uint4 q[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) q[u] = *reinterpret_cast<const uint4*>(words + j + u * 4);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) rank += (q[u].x < word) + (q[u].y < word) + (q[u].z < word) + (q[u].w < word);
+  }
+  uint32_t real;
+  (void)sum_ahead<kFewTokens / 64>(key != kNoToken, part, &real);
+  if (key != kNoToken) {
+    a.key[0][(uint64_t)w * a.tokens + rank] = key;
+    a.pos[0][(uint64_t)w * a.tokens + rank] = i;
+    seen[key] = 1;
+  }
+  if (i == 0) a.real[w] = real;
+}
+
 // A worker's tokens by one workgroup, digits of 8 bits from the lowest up: keys and places stay in registers and change threads through LDS.
 template <int PER>
 __global__ __launch_bounds__(kOneWaves * 64) void k_embed_sort_alone(EmbedArgs a, int bits) {
@@ -102,8 +131,7 @@ __global__ __launch_bounds__(kOneWaves * 64) void k_embed_sort_alone(EmbedArgs a
     key[j] = real ? token_id(a, w, i) : kNoToken;
     pos[j] = i;
   });
-  for (uint32_t i = threadIdx.x; i < seen_words(a.vocab); i += THREADS) ((uint32_t*)seen)[i] = 0;
-  __threadfence();   // before other threads' marks
+  for (uint32_t i = threadIdx.x; i < seen_words(a.vocab); i += THREADS) ((uint32_t*)seen)[i] = 0;   // marks come behind barriers
   for (int shift = 0; shift == 0 || shift < bits; shift += 8) {
     for (uint32_t i = threadIdx.x; i < kOneWaves * BINS; i += THREADS) counts[i] = 0;
     // Tokens outside the table are left out by the first pass.
@@ -425,7 +453,11 @@ template <typename T>
 hipError_t embed_backward(const evg_embed* c, EmbedArgs& a) {
   hipStream_t s = c->stream;
   hipError_t e;
-  if (a.tokens <= kOneSort) {
+  int place_bits = 1;
+  while (a.tokens > 1u << place_bits) ++place_bits;
+  if (a.tokens <= kFewTokens && c->bits + place_bits < 32) {
+    if ((e = launch(a.workers, kFewTokens, s, a, k_embed_sort_few, place_bits)) != hipSuccess) return e;
+  } else if (a.tokens <= kOneSort) {
     const uint32_t per = (a.tokens + kOneWaves * 64 - 1) / (kOneWaves * 64);
     if ((e = launch(a.workers, kOneWaves * 64, s, a, per <= 1 ? k_embed_sort_alone<1> : k_embed_sort_alone<kPer>, c->bits)) != hipSuccess)
       return e;

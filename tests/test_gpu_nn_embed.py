@@ -26,10 +26,11 @@ def check(got, want, what):
     assert bool((off <= bound).all()), f"{what}: {float((off - bound).max())} beyond the bound"
 
 
-#: workers, tokens, vocab, width: one token; fewer and more tokens than numbers; several chunks; odd widths; a vocabulary of one; both ways of sorting,
-#: with one, two and three digits
+#: workers, tokens, vocab, width: one token; fewer and more tokens than numbers; several chunks; odd widths; a vocabulary of one; every way of
+#: sorting, with one, two and three digits
 SIZES = [(1, 1, 5, 8), (1, 1, 1, 1), (3, 7, 11, 33), (2, 33, 4, 64), (1, 200, 1, 129), (2, 257, 1000, 515), (1, 4096, 300, 16), (1, 4097, 300, 16), (2, 5000, 1024, 7),
-         (1, 9001, 70_000, 24), (1, 6000, 1_100_000, 3), (5, 0, 9, 40)]
+         (1, 9001, 70_000, 24), (1, 6000, 1_100_000, 3), (5, 0, 9, 40), (1, 300, 1 << 24, 1), (2, 512, 90, 12),
+         (2, 700, 5000, 20)]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=IDS)
