@@ -149,21 +149,35 @@ __device__ __forceinline__ void finish_rows(const OrthoArgs& g, uint32_t w, uint
   constexpr int PER = TN * 4;   // 16-byte units of a row
   const uint32_t m = rows0 + (lane & 31), limit = (g.N + 7) & ~7u;   // columns up to a whole unit are 0
   Pack<T, 4> hi[TN][4], lo[TN][4], own[TN][4], own_lo[TN][4];
-  auto col_of = [&](int j, int q) { return cols0 + j * 32 + 8 * q + 4 * (lane >> 5); };
+  // A lane's four columns of 32 j + 8 q in `room`, of which the wavefront moves whole units.
+  auto place = [&](int j, int q) { return (Pack<T, 4>*)((char*)(room + (lane & 31) * PER + ((j * 4 + q) ^ (lane & (PER - 1)))) + (lane >> 5) * 8); };
   if constexpr (OP != ORTHO_GRAM) {
-    const uint16_t* const p = g.own.p + (int64_t)w * g.own.worker + (int64_t)m * g.own.ld;
+    u32x4 unit[2][PER / 2];
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t n = col_of(j, q);
-        own[j][q] = own_lo[j][q] = Pack<T, 4>{};
-        if (m < g.M && n < limit) {
-          const uint16_t* const at = p + halves_col(g.own.paired, n);
-          own[j][q] = *reinterpret_cast<const Pack<T, 4>*>(at);
-          if (g.own.apart) own_lo[j][q] = *reinterpret_cast<const Pack<T, 4>*>(at + g.own.apart);
-        }
+    for (int r = 0; r < PER / 2; ++r) {
+      const uint32_t at = r * 64 + lane, row = rows0 + at / PER, n = cols0 + at % PER * 8;
+      unit[0][r] = unit[1][r] = u32x4{0, 0, 0, 0};
+      if (row < g.M && n < limit) {
+        const uint16_t* const p = g.own.p + (int64_t)w * g.own.worker + (int64_t)row * g.own.ld + halves_col(g.own.paired, n);
+        unit[0][r] = *(const u32x4*)p;
+        if (g.own.apart) unit[1][r] = *(const u32x4*)(p + g.own.apart);
       }
+    }
+    auto spread = [&](const u32x4* v, Pack<T, 4> (&to)[TN][4]) {
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int r = 0; r < PER / 2; ++r) {
+        const int at = r * 64 + lane, row = at / PER;
+        room[row * PER + (at % PER ^ (row & (PER - 1)))] = v[r];
+      }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) to[j][q] = *place(j, q);
+    };
+    spread(unit[0], own);
+    spread(unit[1], own_lo);
   }
   auto value = [&](int j, int q, int e) {
     const float p = acc(j, q)[e] * g.f_acc;
@@ -171,19 +185,42 @@ __device__ __forceinline__ void finish_rows(const OrthoArgs& g, uint32_t w, uint
     else return fmaf(to_f(own[j][q].v[e]) + to_f(own_lo[j][q].v[e]), g.f_own, p);
   };
   if constexpr (LAST) {
-    if (m >= g.M) return;
-    const int64_t row = (int64_t)w * g.out.worker + (int64_t)m * g.out.row;
+    if (g.out_type == EVG_F32) {
+      if (m >= g.M) return;
+      float* const p = (float*)g.out.p + (int64_t)w * g.out.worker + (int64_t)m * g.out.row;
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+      for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint32_t n = col_of(j, q);
-        const float x[4] = {value(j, q, 0), value(j, q, 1), value(j, q, 2), value(j, q, 3)};
-        const int count = n < g.N ? (int)(g.N - n) : 0;
-        if (g.out_type == EVG_F32) store_upto<4>((float*)g.out.p + row + n, count, x);
-        else if (g.out_type == EVG_F16) store_upto<4>((half_t*)g.out.p + row + n, count, x);
-        else store_upto<4>((bf16_t*)g.out.p + row + n, count, x);
-      }
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t n = cols0 + j * 32 + 8 * q + 4 * (lane >> 5);
+          const float x[4] = {value(j, q, 0), value(j, q, 1), value(j, q, 2), value(j, q, 3)};
+          store_upto<4>(p + n, n < g.N ? (int)(g.N - n) : 0, x);
+        }
+    } else {
+      auto leave_as = [&](auto type) {
+        typedef decltype(type) U;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            Pack<U, 4> x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x.v[e] = from_f<U>(value(j, q, e));
+            *place(j, q) = __builtin_bit_cast(Pack<T, 4>, x);
+          }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int r = 0; r < PER / 2; ++r) {
+          const int at = r * 64 + lane, row = at / PER, unit = at % PER;
+          const Pack<U, 8> x = __builtin_bit_cast(Pack<U, 8>, room[row * PER + (unit ^ (row & (PER - 1)))]);
+          const uint32_t n = cols0 + unit * 8;
+          if (rows0 + row < g.M) store_pack<8>((U*)g.out.p + (int64_t)w * g.out.worker + (int64_t)(rows0 + row) * g.out.row + n, n < g.N ? (int)(g.N - n) : 0, x);
+        }
+      };
+      if (g.out_type == EVG_F16) leave_as(half_t{});
+      else leave_as(bf16_t{});
+    }
   } else {
 #pragma unroll
     for (int j = 0; j < TN; ++j)
@@ -197,10 +234,7 @@ __device__ __forceinline__ void finish_rows(const OrthoArgs& g, uint32_t w, uint
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int row = lane & 31;
-          *reinterpret_cast<Pack<T, 4>*>((char*)(room + row * PER + ((j * 4 + q) ^ (row & (PER - 1)))) + (lane >> 5) * 8) = v[j][q];
-        }
+        for (int q = 0; q < 4; ++q) *place(j, q) = v[j][q];
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int r = 0; r < PER / 2; ++r) {
