@@ -29,7 +29,7 @@ inline uint64_t ortho_partial(const OrthoShape& g, bool symmetric, OrthoChoice c
 //   128 x 128    2             0.72 / 1.05                          0.8 / 1.4                     9          5
 //    64 x  64    2             0.42 / 0.5                           0.45 / 0.65                   3.5        3
 // and adding up the parts 4 and 0.19 a MB, 0.55 where the caches do not hold them.  Measured, tile and parts: S of 4096 x 11264, hi alone, 256 268, 256 in three parts 211 + 24,
-// 128 in two 232 + 17, 64 356; X' of the same 256 425, 128 440, 64 700; both parts, S of 2048 x 5632 256 316, 256 in four 102 + 11, 128 139, 128 in three 89 + 11, 64 151, P 128 59, in three
+// 128 in two 232 + 17, 64 356; X' of the same 256 386, 128 440, 64 700; both parts, S of 2048 x 5632 256 316, 256 in four 102 + 11, 128 139, 128 in three 89 + 11, 64 151, P 128 59, in three
 // 37 + 16, X' 256 158, 128 153, 64 210; S of four 128 x 784 64 12.8, in four parts 5.5 + 4.0.
 inline OrthoChoice choose_ortho(const OrthoShape& g, bool symmetric, bool split) {
   struct { uint32_t tile, slots; double few[2], busy[2], out, part_out; } const kinds[] = {
