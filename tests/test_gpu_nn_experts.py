@@ -157,3 +157,36 @@ def test_refusals(nn):
                  lambda: nn.ExpertSort(4, 3, 0, max_tokens=5), lambda: nn.ExpertSort(4, 4, 4, max_tokens=1 << 26)):
         with pytest.raises(evg.EvgError):
             call()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("width", [2048, 1100])
+def test_rows_that_the_caches_do_not_hold(nn, dtype, width):
+    """More than 128 MB of rows, with room for some: every kernel that moves them past the caches."""
+    T, E, K = 40_003, 6, 2
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    op = nn.ExpertSort(E, K, width, max_tokens=T, capacity=12_000, dtype=dtype)
+    make = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(dtype)  # noqa: E731
+    x, dy, done = make(1, T, width), make(1, T, width), make(1, E * 12_000, width)
+    weights = torch.randn(1, T, K, generator=gen, device="cuda")
+    chosen = torch.rand(1, T, E, generator=gen, device="cuda").argsort(-1)[..., :K].int()
+    rows, plan = op.dispatch(x, chosen)
+    slot, source, counts = ref.plan(chosen[0].cpu(), E, 12_000)
+    assert torch.equal(plan.slot[0].cpu(), slot) and torch.equal(plan.source[0].cpu(), source) and int(counts.max()) > 12_000 > int(counts.min()) - 2_000
+    y, (d_done, d_weights) = op.combine(done, weights, plan), op.combine_backward(dy, done, weights, plan)
+    some = torch.cat([torch.arange(50), torch.randint(0, T, (400,)), torch.arange(T - 50, T)])
+    at = slot[some]
+    within(y[0, some.cuda()], ref.combine(done[0].cpu().double(), weights[0, some.cuda()].cpu().double(), at, dtype), "y")
+    real = (source >= 0).cuda()
+    token = source.cuda().long().clamp(min=0) // K
+    assert torch.equal(rows[0], torch.where(real[:, None], x[0, token], torch.zeros((), dtype=dtype, device="cuda")))
+    w = weights.view(-1)[source.cuda().long().clamp(min=0)]
+    # The product of 24 and at most 24 bits is exact in 64.  It is rounded to 32 bits and then to the type, or to the type at once (float16 products have an
+    # instruction for that): U32 and a rounding of the type cover both, where bits need not be the same, as a value that the first rounding takes to the middle
+    # between two neighbours may go either way in the second.
+    want = torch.where(real[:, None], w[:, None].double() * dy[0, token].double(), 0.0)
+    off = (d_done[0].double() - want).abs()
+    assert bool((off <= ref.U32 * want.abs() + ref.rounding(want, dtype)).all())
+    del want, off
+    terms = torch.where((at >= 0)[..., None], dy[0].cpu().double()[some][:, None] * done[0].cpu().double()[at.long().clamp(min=0)], 0.0)
+    within(d_weights[0, some.cuda()], (terms.sum(-1), (width + 1) * ref.U32 * terms.abs().sum(-1)), "d_weights")
