@@ -9,6 +9,9 @@
 // which a launch behind adds in the chunks' order: no atomics, so the same tokens give the same bits, and a number that half of all
 // tokens have costs no more than others.  The rows that no token names are zeroed by the same launch; a mark for each number says which.
 // Bound by memory: dy once, the gradient's table once.
+//
+// 16384 tokens, 50257 x 2048 in bfloat16, half of the tokens of 224 numbers: rows 20 us (87 MB, 4.4 TB/s), sorting 2 x (5 + 11), sums and zeros 45 (273 MB, 6.1 TB/s; 82
+// with zeros through the caches and rows not asked for ahead), join 9 (22 with a load at a time).
 #include <hip/hip_runtime.h>
 
 #include <cmath>

@@ -10,6 +10,9 @@
 // Results of float16 (2e-4) have both parts of all operands multiplied in the last two steps, 1e-4, those of 32 bits in all, 1e-6 beside the sums' own: three
 // products for one.
 //
+// The elementwise passes are bound by memory: 4096 x 11264 with its momentum 93 and 86 us, 460 MB each, 4.9 and 5.3 TB/s.  The norm is known only behind the first, so the
+// second reads gradient and momentum again.
+//
 // X, S and P are kept times powers of two, so that the largest elements that they can have come near float16's 65504 and the small ones
 // stay clear of its subnormals: an element is at most the largest singular value, which p(s) = a s + b s^3 + c s^5 bounds.
 #include <hip/hip_runtime.h>
