@@ -92,7 +92,9 @@ __global__ __launch_bounds__(kThreads) void k_ortho_start(UpdateArgs a) {
   double sum = 0.0;
   for (uint32_t i = threadIdx.x; i < a.blocks; i += kThreads) sum += a.partials[(uint64_t)w * a.blocks + i];
   const double norm = sqrt(group_sum(sum, part));
-  const float f = norm == 0.0 ? 0.f : (float)((double)a.scale_x / (norm + (double)a.eps));
+  // The factor as a fraction and a power of two: that of a tiny norm is beyond 32 bits, what it makes of the update's elements is not.
+  int power = 0;
+  const float f = norm == 0.0 ? 0.f : (float)frexp((double)a.scale_x / (norm + (double)a.eps), &power);
   const uint32_t across = (a.cols + 64 * kVector - 1) / (64 * kVector);
   const uint64_t jobs = (uint64_t)a.rows * across;
   const int lane = threadIdx.x & 63;
@@ -107,7 +109,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_start(UpdateArgs a) {
     Pack<half_t, kVector> hi, lo;
 #pragma unroll
     for (int i = 0; i < kVector; ++i) {
-      halves_of(i < n ? u[i] * f : 0.f, &hi.v[i], &lo.v[i]);
+      halves_of(i < n ? ldexpf(u[i], power) * f : 0.f, &hi.v[i], &lo.v[i]);
     }
     uint16_t* const p = a.x.p + (int64_t)w * a.x.worker + (int64_t)row * a.x.ld + halves_col(a.x.paired, col);
     *reinterpret_cast<Pack<half_t, kVector>*>(p) = hi;
