@@ -3,12 +3,12 @@
 //     m' = mu m + G,  u = G + mu m' or m',  X = u / (|u| + eps);  steps times  S = X X^T,  P = b S + c S S,  X <- a X + P X
 //
 // With n the smaller side and k the larger, a step is n^2 k (S, half of it), n^3 (S S, half of it) and 2 n^2 k operations, all on the matrix cores,
-// three launches.  What the steps cost in precision was looked at with each value rounded by itself (gradients of a few large directions and many small ones, sides
-// 64 to 1365).  Rounding X to float16 between steps leaves an error of 1e-3 to 1e-2 of the result, as the small singular values grow up to 485-fold and what is
-// rounded off the large ones' part grows with them; rounding S, P or the products' operands 1e-4 to 7e-4, most of it from the last steps. So X is kept in two
-// parts, 22 bits, of which products read the first; the second costs a read and a write a step.  That is 1e-3, below what bfloat16 rounds off a result (1.7e-3).
-// Results of float16 (2e-4) have both parts of all operands multiplied in the last two steps, 1e-4, those of 32 bits in all, 1e-6 beside the sums' own: three
-// products for one.
+// three launches.  What the steps cost in precision was looked at with each value rounded by itself (gradients of few directions, of few strong and many weak ones, and of all alike;
+// sides 4 to 2816, five usual steps).  Rounding X to float16 between steps leaves an error of 1e-3 to 1e-2 of the result, as the small singular values grow up to 485-fold and what is
+// rounded off the large ones' part grows with them. So X is kept in two parts, 22 bits, of which products read the first; the second costs a read and a write a
+// step.  Rounding S, P and the products' operands then leaves 1e-4 to 3e-3, most where all singular values are alike or the smaller side is short, beside the 1.7e-3 that bfloat16 rounds off a
+// result: that is what bfloat16 tensors get.  Float16 rounds off 2e-4, and where only the last two steps multiplied both parts of their operands the first three left up to 2e-3 (16 x 16; 6e-4 at 512 x 512, 4e-4
+// of 64 equal directions of 1024 x 2816).  So all steps of float16 and 32-bit tensors multiply both parts, three products for one, which leaves 3e-7 to 4e-5 beside the sums' own.
 //
 // The elementwise passes are bound by memory: 4096 x 11264 with its momentum 93 and 86 us, 460 MB each, 4.9 and 5.3 TB/s.  The norm is known only behind the first, so the
 // second reads gradient and momentum again.
@@ -151,7 +151,7 @@ struct evg_ortho {
   float* sums = nullptr;   // partial sums of products
   uint64_t room = 0;       // how many
   uint32_t blocks = 1;
-  uint32_t split_from = 0;   // the first step whose products are of both parts
+  bool split = false;      // products of both parts
   float scale_x = 1.f, scale_s = 1.f, scale_p = 1.f;
 };
 
@@ -233,18 +233,15 @@ evg_status evg_ortho_init(evg_ortho** out, const evg_ortho_config* cfg, void* hi
   c->scale_x = scale_for(bound);
   c->scale_s = scale_for(bound * bound);
   c->scale_p = scale_for(1.01 * most_quadratic(cfg->b, cfg->c, bound * bound));
-  c->split_from = cfg->type == EVG_F32 ? 0 : cfg->type == EVG_BF16 ? cfg->steps : cfg->steps > 2 ? cfg->steps - 2 : 0;
+  c->split = cfg->type != EVG_BF16;
   const uint64_t across = ((uint64_t)cfg->cols + 64 * kVector - 1) / (64 * kVector), jobs = (cfg->rows * across + kWaves - 1) / kWaves;
   c->blocks = (uint32_t)(jobs < kBlocks ? jobs : kBlocks);
   const uint64_t W = cfg->matrices, x = W * cfg->rows * pitch_of(cfg->cols) * 2 * sizeof(uint16_t), s = W * n * pitch_of(n) * 2 * sizeof(uint16_t);
   const uint32_t k = cfg->rows < cfg->cols ? cfg->cols : cfg->rows;
-  for (int split = 0; split < 2; ++split) {
-    const OrthoShape gram{n, n, k, cfg->matrices, kMostSums}, square{n, n, n, cfg->matrices, kMostSums}, apply{cfg->rows, cfg->cols, n, cfg->matrices, kMostSums};
-    if (split ? c->split_from >= cfg->steps : c->split_from == 0) continue;   // no such step
-    for (const uint64_t need : {ortho_partial(gram, true, choose_ortho(gram, true, split)), ortho_partial(square, true, choose_ortho(square, true, split)),
-                                ortho_partial(apply, false, choose_ortho(apply, false, split))})
-      if (need > c->room) c->room = need;
-  }
+  const OrthoShape gram{n, n, k, cfg->matrices, kMostSums}, square{n, n, n, cfg->matrices, kMostSums}, apply{cfg->rows, cfg->cols, n, cfg->matrices, kMostSums};
+  for (const uint64_t need : {ortho_partial(gram, true, choose_ortho(gram, true, c->split)), ortho_partial(square, true, choose_ortho(square, true, c->split)),
+                              ortho_partial(apply, false, choose_ortho(apply, false, c->split))})
+    if (need > c->room) c->room = need;
   auto whole = [](uint64_t bytes) { return (bytes + 255) / 256 * 256; };
   struct { void** to; uint64_t bytes; } parts[] = {{(void**)&c->partials, W * c->blocks * sizeof(double)}, {(void**)&c->x[0], x}, {(void**)&c->x[1], x},
                                                    {(void**)&c->s, s}, {(void**)&c->p, s}, {(void**)&c->sums, c->room * sizeof(float)}};
@@ -295,8 +292,8 @@ evg_status evg_ortho_update(evg_ortho* c, const evg_mat* grad, const evg_mat* mo
   u.partials = c->partials;
   const bool tall = R > C;
   const uint32_t n = tall ? C : R, k = tall ? R : C;
-  auto split_at = [&](uint32_t step) { return step >= c->split_from; };
-  auto x_at = [&](uint32_t step) { return halves(c->x[step & 1], W, R, C, split_at(step), true); };   // as the step's products take it
+  const bool split = c->split;
+  auto x_at = [&](uint32_t step) { return halves(c->x[step & 1], W, R, C, split, true); };
   u.x = x_at(0);
   HIP_TRY(g.type == EVG_F32   ? launch_start<float>(u, W, c->stream)
           : g.type == EVG_F16 ? launch_start<half_t>(u, W, c->stream)
@@ -304,7 +301,7 @@ evg_status evg_ortho_update(evg_ortho* c, const evg_mat* grad, const evg_mat* mo
 
   const float sx = c->scale_x, ss = c->scale_s, sp = c->scale_p;
   for (uint32_t i = 0; i < g.steps; ++i) {
-    const bool last = i + 1 == g.steps, split = split_at(i);
+    const bool last = i + 1 == g.steps;
     const Halves x = x_at(i), S = halves(c->s, W, n, n, split, false), P = halves(c->p, W, n, n, split, false);
     OrthoArgs a{};
     a.matrices = W;
