@@ -12,7 +12,7 @@ Every worker has its own copy of the parameters in the ring's arena and its own 
 Each expert's matrices are tensors of their own, so that the ring's events are too: an expert that few tokens reach seldom sends.
 The plain products, of the router's and the vocabulary's logits, and the loss are torch's, in 32 bits.
 
-Tokens of -1 are padding: rows of zeros, no experts, no loss; targets of -1 have none either.  Types, the loss scale of float16 and streams are as in
+Tokens outside the vocabulary, as -1, are padding: rows of zeros, no experts, no loss; targets outside it have none either.  Types, the loss scale of float16 and streams are as in
 ``ffn_ring``.
 
     python -m paper_2103_07454_amd.mixture_ring --workers 4 --width 256 --hidden 512 --experts 8 --tokens 256 --dtype bf16
@@ -91,6 +91,10 @@ class MixtureRing(FFNRing):
         """An expert's slots of all workers."""
         return rows[:, e * self.capacity:(e + 1) * self.capacity]
 
+    def _real(self, numbers):
+        """Which are in the vocabulary?"""
+        return (numbers >= 0) & (numbers < self.vocab)
+
     def forward(self, tokens):
         """The last norm's rows [workers, tokens, width] of the ring's present parameters, and what the backward pass needs."""
         with self._ordered() as hand_over:
@@ -100,7 +104,7 @@ class MixtureRing(FFNRing):
             residual = self.embed.forward(tokens, p[0, "table"])
             residual, normed = self.norm.forward(residual, pre=p[0, "pre"])
             for b in range(self.blocks):
-                logits = torch.bmm(normed.float(), p[b, "router"].float().mT.contiguous()).masked_fill_((tokens < 0)[..., None], -math.inf)
+                logits = torch.bmm(normed.float(), p[b, "router"].float().mT.contiguous()).masked_fill_(~self._real(tokens)[..., None], -math.inf)
                 chosen, weights = self.router.forward(logits)
                 rows, plan = self.sort.dispatch(normed, chosen)
                 done, saved = torch.empty_like(rows), []
@@ -139,9 +143,9 @@ class MixtureRing(FFNRing):
     def loss(self, out, tokens, target):
         """Each worker's mean cross entropy of the targets, the gradient of ``out`` (times the loss scale), and the table's, in its arena."""
         with self._ordered() as hand_over:
-            real = (tokens >= 0) & (target >= 0)
+            real = self._real(tokens) & self._real(target)
             share = real / real.sum(1, keepdim=True).clamp(min=1)
-            at = target.clamp(min=0).long()[..., None]
+            at = torch.where(real, target, 0).long()[..., None]
             table, rows = self.params[0, "table"].float(), out.float()
             logp = torch.log_softmax(torch.bmm(rows, table.mT.contiguous()), -1)
             loss = -(logp.gather(-1, at)[..., 0] * share).sum(1)
