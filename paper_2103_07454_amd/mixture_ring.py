@@ -33,6 +33,8 @@ class MixtureRing(FFNRing):
     def __init__(self, workers=4, *, vocab=256, width=64, hidden=96, experts=4, top=2, capacity_factor=1.5, blocks=2, tokens=32, dtype=torch.float32,
                  activation="silu", lr=0.05, momentum=0.0, max_norm=1.0, orthogonal=True, orthogonal_scale=0.2, seed=0, loss_scale=None, device="cuda:0",
                  stream=None, **ring_options):
+        if not capacity_factor > 0:
+            raise ValueError("capacity_factor must be positive: experts have equal room")    # ExpertSort's capacity of 0 is another layout
         self.workers, self.vocab, self.width, self.hidden, self.blocks, self.tokens = workers, vocab, width, hidden, blocks, tokens
         self.experts, self.top, self.dtype, self.max_norm = experts, top, dtype, max_norm
         self.capacity = min(tokens, math.ceil(capacity_factor * tokens * top / experts))

@@ -35,3 +35,10 @@ def test_numbers_outside_the_vocabulary_have_no_loss(kind):
     logp = torch.log_softmax(out[0] @ run.params[0, "table"][0].T, -1)
     assert torch.allclose(want, torch.stack([-(logp[0, 1] + logp[1, 2]) / 2, torch.zeros(())]), rtol=1e-5)
     assert bool((d[0, 2:] == 0).all()) and bool((d[1] == 0).all())
+
+
+@pytest.mark.parametrize("factor", [0, 0.0, -1.0, float("nan")])
+def test_experts_without_room_are_refused(factor):
+    """A capacity of 0 would be ExpertSort's packed rows, of which no expert would get any."""
+    with pytest.raises(ValueError, match="capacity_factor"):
+        mixture_ring.MixtureRing(2, capacity_factor=factor)
