@@ -6,8 +6,9 @@
 //
 // Backward: the tokens are sorted by their number, those of one number stay in their order; then a wavefront adds up the rows of a
 // chunk of 16 sorted tokens, 64 vectors wide, and writes a sum where the number changes.  Numbers that go on in the next chunk leave partial sums in 32 bits,
-// which a launch behind adds in the chunks' order: no atomics, so the same tokens give the same bits, and a number that half of all
-// tokens have costs no more than others.  The rows that no token names are zeroed by the same launch; a mark for each number says which.
+// which a launch behind adds in the chunks' order, a wavefront all those of a number and 256 columns: no atomics, so the same tokens give the same bits.  A number that
+// very many tokens have is waited for there: of 16384 tokens 2048 wide a gradient takes 87 us with up to a sixteenth of them the same, 106 with a quarter, 129 with half, 174 with all.
+// The rows that no token names are zeroed by the launch of the sums; a mark for each number says which.
 // Bound by memory: dy once, the gradient's table once.
 //
 // 16384 tokens, 50257 x 2048 in bfloat16, half of the tokens of 224 numbers: rows 20 us (87 MB, 4.4 TB/s), sorting 2 x (5 + 11), sums and zeros 45 (273 MB, 6.1 TB/s; 82
