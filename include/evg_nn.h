@@ -264,17 +264,17 @@ evg_status evg_experts_destroy(evg_experts* c);
  *     steps times:  S = X X^T,  X <- a X + (b S + c S S) X                      (S = X^T X, X <- a X + X (b S + c S S) where R > C)
  *     out = scale * X
  * which takes every singular value s of X to p(s) = a s + b s^3 + c s^5, again and again: with the usual constants close to 1, singular vectors stay.
- * Products are of float16 operands with sums in 32 bits.  X is kept as two of them, 22 bits; for float16 and 32-bit tensors S, b S + c S S and the products' operands are
- * two as well.  What five steps with the constants 3.4445, -4.7750 and 2.0315 leave beside the rounding of the result, of its norm, sides 4 to 2816: 1e-4 to 3e-3 for bfloat16 tensors (a 32-bit result of
- * theirs is no more exact), 3e-7 to 4e-5 for others; sums in 32 bits come on top.  Other constants and more steps stretch errors as they stretch singular values, and what they make much smaller
- * than the largest that a singular value can become is known to so many bits fewer.  A zero matrix stays zero, a matrix with a NaN or an infinity becomes NaN. */
+ * Products are of float16 operands with sums in 32 bits.  X is kept as two of them, 22 bits; S, b S + c S S and the products' operands are two as well, but for bfloat16 tensors
+ * whose smaller side is above 256.  What five steps with the constants 3.4445, -4.7750 and 2.0315 leave, of the result's norm, beside its rounding and what sums in 32 bits do: 3e-7 to 4e-5, for
+ * those bfloat16 tensors 1e-4 to 1.8e-3 (a 32-bit result of theirs is no more exact).  Other constants and more steps stretch errors as they stretch singular values, and what they make much
+ * smaller than the largest that a singular value can become is known to so many bits fewer.  A zero matrix stays zero, a matrix with a NaN or an infinity becomes NaN. */
 typedef struct evg_ortho evg_ortho;
 
 typedef struct {
   uint32_t matrices; /* W, 1 .. 65535                                                     */
   uint32_t rows, cols; /* 1 .. 65536, the smaller of them at most 16384                   */
   uint32_t type;     /* of G                                                              */
-  uint32_t out_type; /* type or EVG_F32; the products' precision goes by type             */
+  uint32_t out_type; /* type or EVG_F32; the products' precision goes by type and sides   */
   uint32_t steps;    /* 1 .. 64                                                           */
   float a, b, c;     /* finite; constants under which a singular value of 0 .. 1 passes 3 are refused */
   float momentum;    /* finite                                                            */

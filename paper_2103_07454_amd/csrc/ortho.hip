@@ -6,9 +6,11 @@
 // three launches.  What the steps cost in precision was looked at with each value rounded by itself (gradients of few directions, of few strong and many weak ones, and of all alike;
 // sides 4 to 2816, five usual steps).  Rounding X to float16 between steps leaves an error of 1e-3 to 1e-2 of the result, as the small singular values grow up to 485-fold and what is
 // rounded off the large ones' part grows with them. So X is kept in two parts, 22 bits, of which products read the first; the second costs a read and a write a
-// step.  Rounding S, P and the products' operands then leaves 1e-4 to 3e-3, most where all singular values are alike or the smaller side is short, beside the 1.7e-3 that bfloat16 rounds off a
-// result: that is what bfloat16 tensors get.  Float16 rounds off 2e-4, and where only the last two steps multiplied both parts of their operands the first three left up to 2e-3 (16 x 16; 6e-4 at 512 x 512, 4e-4
-// of 64 equal directions of 1024 x 2816).  So all steps of float16 and 32-bit tensors multiply both parts, three products for one, which leaves 3e-7 to 4e-5 beside the sums' own.
+// step.  Rounding S, P and the products' operands then leaves 1e-4 to 3e-3, most where all singular values are alike and the smaller side is short (2.5e-3 at 16, 2.1e-3 at 64, 1.8e-3 at
+// 256, 1.4e-3 at 1024).  Multiplying both parts of all operands, three products for one, leaves 3e-7 to 4e-5 beside the sums' own.
+//   bfloat16 rounds 1.7e-3 off a result.  Above a smaller side of 256 products are of one part, which leaves no more than that (8 of 1024 x 2816: 731 us, 1498 with both parts); up to there of
+//   both, which costs little (128 x 128: 76 us with one part, 82 with both; four of 128 x 784 97 and 103; 256 x 1024 100 and 115, eight of them 110 and 154).
+//   float16 rounds off 2e-4.  Where only the last two steps multiplied both parts, the first three left up to 2e-3 (16 x 16; 6e-4 at 512 x 512, 4e-4 of 64 equal directions of 1024 x 2816): all do.
 //
 // The elementwise passes are bound by memory: 4096 x 11264 with its momentum 93 and 86 us, 460 MB each, 4.9 and 5.3 TB/s.  The norm is known only behind the first, so the
 // second reads gradient and momentum again.
@@ -31,6 +33,7 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr uint32_t kBlocks = 2048;  // of a matrix, at most: each of the second pass adds up what those of the first left
 constexpr int kVector = 8;          // elements of a lane
+constexpr uint32_t kBothSide = 256;   // largest smaller side of bfloat16 matrices whose products are of both parts
 
 struct UpdateArgs {
   evg_mat grad, momentum, momentum_out;
@@ -233,7 +236,7 @@ evg_status evg_ortho_init(evg_ortho** out, const evg_ortho_config* cfg, void* hi
   c->scale_x = scale_for(bound);
   c->scale_s = scale_for(bound * bound);
   c->scale_p = scale_for(1.01 * most_quadratic(cfg->b, cfg->c, bound * bound));
-  c->split = cfg->type != EVG_BF16;
+  c->split = cfg->type != EVG_BF16 || n <= kBothSide;
   const uint64_t across = ((uint64_t)cfg->cols + 64 * kVector - 1) / (64 * kVector), jobs = (cfg->rows * across + kWaves - 1) / kWaves;
   c->blocks = (uint32_t)(jobs < kBlocks ? jobs : kBlocks);
   const uint64_t W = cfg->matrices, x = W * cfg->rows * pitch_of(cfg->cols) * 2 * sizeof(uint16_t), s = W * n * pitch_of(n) * 2 * sizeof(uint16_t);

@@ -14,8 +14,8 @@ STEPS = 2
 MORE = [(16, 641, 545), (25, 706, 764)]
 
 
-def both_parts(dtype):
-    return dtype is not torch.bfloat16
+def both_parts(dtype, rows, cols):
+    return dtype is not torch.bfloat16 or min(rows, cols) <= 256
 
 
 @pytest.mark.parametrize("types", TYPES, ids=IDS)
@@ -31,8 +31,8 @@ def test_every_kernel(types, size):
     for w in sorted({0, W // 2, W - 1}):
         u = grad[w].float()
         options = dict(steps=STEPS, scale=-1.5)
-        want = emulation.emulate(u, both_parts(dtype), out_dtype, **options)
-        room = emulation.tolerance(want, u, both_parts(dtype), out_dtype, **options)
+        want = emulation.emulate(u, both_parts(dtype, R, C), out_dtype, **options)
+        room = emulation.tolerance(want, u, both_parts(dtype, R, C), out_dtype, **options)
         off, size_of = float((out[w].double() - want).norm()), float(want.norm())
         print(f"[ortho products] {size} {dtype} {out_dtype}: off by {off / size_of:.1e} of the update, {off / room:.2f} of the tolerance", flush=True)
         assert off <= room
@@ -49,8 +49,8 @@ def test_the_usual_five_steps(types, size):
     out = nn.Orthogonal(R, C, matrices=W, dtype=dtype, out_dtype=out_dtype).update(grad)
     for w in range(W):
         u = grad[w].float()
-        want = emulation.emulate(u, both_parts(dtype), out_dtype)
-        room = emulation.tolerance(want, u, both_parts(dtype), out_dtype)
+        want = emulation.emulate(u, both_parts(dtype, R, C), out_dtype)
+        room = emulation.tolerance(want, u, both_parts(dtype, R, C), out_dtype)
         off, size_of = float((out[w].double() - want).norm()), float(want.norm())
         print(f"[ortho five] {size} {dtype} {out_dtype}: off by {off / size_of:.1e} of the update, {off / room:.2f} of the tolerance of {room / size_of:.1e}", flush=True)
         assert off <= room

@@ -20,8 +20,9 @@ using namespace evg;
 // A kernel: both parts or one, which product, its tile, and whether k is shared out; wide or tall where that changes the operands' way through LDS.
 static void tell(uint32_t W, uint32_t a, uint32_t b) {
   const uint32_t n = a < b ? a : b, k = a < b ? b : a;
-  for (int split = 0; split < 2; ++split)
+  for (int type = 0; type < 2; ++type)   // bfloat16, others
     for (int op = 0; op < 3; ++op) {
+      const bool split = type || n <= 256;
       const OrthoShape s = op == 0 ? OrthoShape{n, n, k, W, 1u << 26} : op == 1 ? OrthoShape{n, n, n, W, 1u << 26} : OrthoShape{a, b, n, W, 1u << 26};
       const OrthoChoice c = choose_ortho(s, op != 2, split);
       printf("%d %d %d %u %d\n", split, op, op == 1 ? 0 : a > b, c.tile, c.parts > 1);
@@ -54,7 +55,7 @@ def test_the_products_tests_run_every_kernel(tmp_path):
     tested = {kernel for size in SIZES + MORE for kernel in run(*size)}
     missing = sorted(run() - tested)
     assert not missing, missing
-    assert STEPS >= 2 and {both_parts(a) for a, _ in TYPES} == {False, True}
+    assert STEPS >= 2 and {both_parts(a, 300, 300) for a, _ in TYPES} == {False, True}
 
 
 @pytest.mark.parametrize("size", [(1, 1), (3, 5), (20, 30), (64, 64), (130, 65)], ids=lambda s: "x".join(map(str, s)))
@@ -71,7 +72,7 @@ def test_emulation_against_the_formula(size):
 def test_mistakes_are_far_outside_the_tolerance(types, size):
     dtype, out_dtype = types
     u = emulation.gradient(torch.Generator().manual_seed(1), 1, *size)[0].to(dtype).float()
-    both = both_parts(dtype)
+    both = both_parts(dtype, *size)
     want = emulation.emulate(u, both, out_dtype, steps=STEPS)
     room = emulation.tolerance(want, u, both, out_dtype, steps=STEPS)
     off = lambda mistake: float((emulation.emulate(u, both, out_dtype, steps=STEPS, mistake=mistake) - want).norm())  # noqa: E731
