@@ -7,7 +7,7 @@
 //
 // S and P are symmetric: tiles below the diagonal are not computed, those above it are written twice, the second time turned round.
 //
-// Bound by the matrix cores and the clock that power leaves them: 4096 x 11264, hi alone, X 386 us (0.98 PFLOP/s; 425 with what is added read four columns a lane), S 207 + 24
+// Bound by the matrix cores, the clock that power leaves them and rounds of workgroups that do not fill the CUs (P of 4096 has 136 tiles of 256 for 256 CUs, S 408, X 704): 4096 x 11264, hi alone, X 386 us (0.98 PFLOP/s; 425 with what is added read four columns a lane), S 207 + 24
 // (0.82), P 105.  Small ones by the steps' latency, 0.45 us each.
 //
 // Where tiles are few, k is shared out to several workgroups, whose sums go to memory in the accumulators' order; a launch behind adds them up in a fixed order.

@@ -6,7 +6,8 @@
 // A logit of 16 bits and its number fit a word of 32 bits, one of 32 needs 64.
 //
 // Bound by the choices' instructions, some thirty each, and by latency: 128 experts of 32768 tokens in bfloat16, top 8, 9.9 us (8 MB in, 2 MB out), of which a wavefront
-// keeps what was chosen in LDS (13.2 with each lane noting the places of its own experts; 22 with words of 64 bits); the gradient 8.2.
+// keeps what was chosen in LDS (13.2 with each lane noting the places of its own experts; 22 with words of 64 bits); the gradient 8.2, with three
+// reductions over a row's lanes by exchanges through LDS, each waiting for the last.
 #include <hip/hip_runtime.h>
 
 #include <new>
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void k_router_backward(RouterArgs a) {
   if (most == -INFINITY) most = 0.f;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    v[i] = sizeof(T) == 2 ? __expf(v[i] - most) : expf(v[i] - most);   // results of 16 bits: the hardware's, a few units of 2^-23 off
+    v[i] = sizeof(T) == 2 ? __expf(v[i] - most) : expf(v[i] - most);   // results of 16 bits: the hardware's, off by some 2^-23 for each unit of the exponent
     total += v[i];
   }
   total = lanes_total<LANES>(total);
