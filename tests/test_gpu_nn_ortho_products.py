@@ -54,3 +54,22 @@ def test_the_usual_five_steps(types, size):
         off, size_of = float((out[w].double() - want).norm()), float(want.norm())
         print(f"[ortho five] {size} {dtype} {out_dtype}: off by {off / size_of:.1e} of the update, {off / room:.2f} of the tolerance of {room / size_of:.1e}", flush=True)
         assert off <= room
+
+
+@pytest.mark.parametrize("types", [TYPES[0], TYPES[3]], ids=[IDS[0], IDS[3]])
+def test_matrices_beyond_32_bits(types):
+    """The last matrix's X, gradient and update lie more than 2^32 bytes behind the first's."""
+    from paper_2103_07454_amd import nn
+    dtype, out_dtype = types
+    W, R, C = (17 if dtype is torch.float32 else 33), 1024, 65536
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    grad = torch.empty(W, R, C, dtype=dtype, device="cuda")
+    for w in range(W):
+        grad[w] = emulation.gradient(gen, 1, R, C)[0]
+    momentum = torch.zeros(W, R, C, device="cuda")
+    out = nn.Orthogonal(R, C, matrices=W, dtype=dtype, out_dtype=out_dtype, steps=STEPS, nesterov=False).update(grad, momentum=momentum)
+    for w in (0, W - 1):
+        u = grad[w].float()
+        assert torch.equal(momentum[w], u)
+        want = emulation.emulate(u, both_parts(dtype, R, C), out_dtype, steps=STEPS)
+        assert float((out[w].double() - want).norm()) <= emulation.tolerance(want, u, both_parts(dtype, R, C), out_dtype, steps=STEPS)
