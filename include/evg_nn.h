@@ -266,8 +266,8 @@ evg_status evg_experts_destroy(evg_experts* c);
  * which takes every singular value s of X to p(s) = a s + b s^3 + c s^5, again and again: with the usual constants close to 1, singular vectors stay.
  * Products are of float16 operands with sums in 32 bits.  X is kept as two of them, 22 bits; S, b S + c S S and the products' operands are two as well, but for bfloat16 tensors
  * whose smaller side is above 256.  What five steps with the constants 3.4445, -4.7750 and 2.0315 leave, of the result's norm, beside its rounding and what sums in 32 bits do: 3e-7 to 4e-5, for
- * those bfloat16 tensors 1e-4 to 1.8e-3 (a 32-bit result of theirs is no more exact).  Other constants and more steps stretch errors as they stretch singular values, and what they make much
- * smaller than the largest that a singular value can become is known to so many bits fewer.  A zero matrix stays zero, a matrix with a NaN or an infinity becomes NaN. */
+ * those bfloat16 tensors 1e-4 to 1.8e-3 (a 32-bit result of theirs is no more exact).  Other constants and more steps stretch errors as they stretch singular values, and what they, or an eps far
+ * above |u|, make much smaller than the largest that a singular value can become is known to so many bits fewer.  A zero matrix stays zero, a matrix with a NaN or an infinity becomes NaN. */
 typedef struct evg_ortho evg_ortho;
 
 typedef struct {
@@ -280,7 +280,7 @@ typedef struct {
   float momentum;    /* finite                                                            */
   uint32_t nesterov;
   float eps;         /* >= 0, finite                                                      */
-  float scale;       /* finite                                                            */
+  float scale;       /* finite, 0 or at least 2^-80 in magnitude                          */
 } evg_ortho_config;
 
 evg_status evg_ortho_init(evg_ortho** out, const evg_ortho_config* cfg, void* hip_stream);

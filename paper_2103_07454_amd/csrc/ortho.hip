@@ -225,6 +225,8 @@ evg_status evg_ortho_init(evg_ortho** out, const evg_ortho_config* cfg, void* hi
   for (float v : {cfg->a, cfg->b, cfg->c, cfg->momentum, cfg->scale})
     if (!std::isfinite(v)) return fail(EVG_ERR_INVALID, "a, b, c, momentum and scale must be finite");
   if (!(cfg->eps >= 0.f) || std::isinf(cfg->eps)) return fail(EVG_ERR_INVALID, "eps must be finite and not negative");
+  // It is multiplied with the powers of two that X and P are kept times, at most 2^38, taken back.
+  if (cfg->scale != 0.f && std::fabs(cfg->scale) < 0x1p-80f) return fail(EVG_ERR_INVALID, "scale must be 0 or at least 2^-80 in magnitude");
   // Singular values begin at no more than the norm, 1; what rounding adds is less than the hundredth that is allowed for.
   double bound = 1.01;
   for (uint32_t i = 0; i < cfg->steps && bound <= 3.0; ++i) bound = std::fmax(bound, 1.01 * most_quintic(cfg->a, cfg->b, cfg->c, bound));

@@ -37,3 +37,15 @@ def test_one_element(nn):
         grad[0, 1, 2] = value
         out = nn.Orthogonal(3, 5, eps=0.0, steps=1, polynomial=(1.0, 0.0, 0.0)).update(grad)
         assert abs(float(out[0, 1, 2]) - 1.0) <= 2.0 ** -20 and int((out != 0).sum()) == 1
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("power", [-80, -70, -30, 30, 100])
+@pytest.mark.parametrize("polynomial", [(3.4445, -4.7750, 2.0315), (1.0, 0.0, 0.0)], ids=["usual", "none"])
+def test_a_scale_that_is_a_power_of_two_is_exact(nn, dtype, power, polynomial):
+    """Down to the smallest scale that is taken: what it is multiplied with on the way keeps all bits.  Updates of 16 significant bits or more stay normal numbers."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    grad = torch.randn(1, 40, 300, generator=gen, device="cuda").to(dtype)
+    make = lambda scale: nn.Orthogonal(40, 300, dtype=dtype, polynomial=polynomial, scale=scale).update(grad)  # noqa: E731
+    assert torch.equal(make(2.0 ** power).double(), make(1.0).double() * 2.0 ** power)
+    assert float(make(0.0).abs().max()) == 0.0
