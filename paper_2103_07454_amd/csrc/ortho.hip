@@ -8,7 +8,7 @@
 // rounded off the large ones' part grows with them. So X is kept in two parts, 22 bits, of which products read the first; the second costs a read and a write a
 // step.  Rounding S, P and the products' operands then leaves 1e-4 to 3e-3, most where all singular values are alike and the smaller side is short (2.5e-3 at 16, 2.1e-3 at 64, 1.8e-3 at
 // 256, 1.4e-3 at 1024).  Multiplying both parts of all operands, three products for one, leaves 3e-7 to 4e-5 beside the sums' own.
-//   bfloat16 rounds 1.7e-3 off a result.  Above a smaller side of 256 products are of one part, which leaves no more than that (8 of 1024 x 2816: 731 us, 1498 with both parts); up to there of
+//   bfloat16 rounds 1.7e-3 off a result.  Above a smaller side of 256 products are of one part, which leaves about as much at most (1.8e-3 of 512 x 4000; time: 8 of 1024 x 2816: 731 us, 1498 with both parts); up to there of
 //   both, which costs little (128 x 128: 76 us with one part, 82 with both; four of 128 x 784 97 and 103; 256 x 1024 100 and 115, eight of them 110 and 154).
 //   float16 rounds off 2e-4.  Where only the last two steps multiplied both parts, the first three left up to 2e-3 (16 x 16; 6e-4 at 512 x 512, 4e-4 of 64 equal directions of 1024 x 2816): all do.
 //

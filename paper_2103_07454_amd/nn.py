@@ -572,7 +572,7 @@ class Orthogonal(_Operator):
     ``X <- a X + (b S + c S S) X`` with ``S = X X^T`` and ``polynomial = (a, b, c)``; the update is ``scale * X``.  grad and the update:
     [matrices, rows, cols], the latter of ``out_dtype``, which is ``dtype`` or float32; m: float32.
     With the usual polynomial and five steps, float16 and float32 updates, and bfloat16 ones of matrices with a smaller side of at most 256, are as exact as sums in 32 bits;
-    those of larger bfloat16 matrices may be off by as much as their rounding once more, whatever ``out_dtype``.
+    those of larger bfloat16 matrices may be off by about as much as their rounding once more, whatever ``out_dtype``.
     """
 
     _destroy = "evg_ortho_destroy"
